@@ -388,6 +388,129 @@ int cas_attention_static(cas_ctx* ctx, cas_kv* kv, int layer, int seq, int full,
 /* Host only: size in bytes of that array. */
 size_t cas_attention_static_capacity(void);
 
+/* ---- rotary positions for the stand-alone calls ------------------------------------------- */
+
+/*
+ * The model passes rotate q and k themselves, at the position that the cache's length gives.  The calls
+ * below do it for code that drives cas_kv_append and cas_attention* on its own, at positions given one by
+ * one (after an eviction a token's position is no longer its place in the cache).
+ *
+ * Channel pair i of the `rot` channels that turn (i < rot/2) has the frequency f_i = base^(-2i/rot), changed
+ * for contexts `factor` times as long as the trained one:
+ *   CAS_ROPE_PLAIN  : f_i                                        (factor is not used)
+ *   CAS_ROPE_LINEAR : f_i / factor                               (positions squeezed)
+ *   CAS_ROPE_BASE   : base * factor^(rot/(rot-2)) for the base   (rot >= 4)
+ *   CAS_ROPE_BANDS  : with r = trained * f_i / (2 pi), the turns of the pair within the trained context, and
+ *                     g = (r - low) / (high - low) clamped to [0, 1]: g f_i + (1 - g) f_i / factor
+ * and an angle p f_i at position p.  magnitude: what cos and sin are multiplied by (1 for none).
+ */
+enum { CAS_ROPE_PLAIN = 0, CAS_ROPE_LINEAR = 1, CAS_ROPE_BASE = 2, CAS_ROPE_BANDS = 3 };
+enum { CAS_ROPE_HALF = 0, CAS_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  int32_t rot;      /* channels that turn: even, 2..256 */
+  int32_t scaling;  /* CAS_ROPE_PLAIN .. CAS_ROPE_BANDS */
+  double base;      /* >= 1, finite */
+  double factor;    /* >= 1, finite */
+  int32_t trained;  /* CAS_ROPE_BANDS: positions of the trained context, >= 1 */
+  double low, high; /* CAS_ROPE_BANDS: turns below which a pair is squeezed whole and above which it is left; 0 <= low < high */
+  double magnitude; /* > 0, finite */
+} cas_rope_cfg;
+
+/* Host only: the rot/2 frequencies f_i after scaling. */
+int cas_rope_freqs(const cas_rope_cfg* cfg, double* h_freqs);
+
+/* cos and sin of the positions pos0 .. pos0+n_pos-1: d_table float [n_pos][rot/2][2].  With rot = 128 this is
+ * the d_rope of cas_model_weights.  Angles are reduced in 64 bits: an entry is within 2e-7 * magnitude of the
+ * exact value at every position.  0 <= pos0, pos0 + n_pos <= 2^24. */
+int cas_rope_table(cas_ctx* ctx, const cas_rope_cfg* cfg, int pos0, int n_pos, float* d_table);
+
+/* Heads of n_tok tokens that lie ldx values apart in d_x and are written ldy apart to d_y, the heads of a
+ * token side by side (head_dim values each).  x_fp32: d_x holds floats (an output of cas_gemm_verify), which are
+ * rounded to bf16 first, otherwise bf16.  turn = 0: the heads are taken over unrotated (v).  d_y may be d_x
+ * itself where d_x is bf16 and ldx = ldy; otherwise no output may overlap an input or another output. */
+typedef struct {
+  const void* d_x;
+  uint16_t* d_y;
+  int64_t ldx, ldy; /* >= n_heads * head_dim */
+  int32_t n_heads, x_fp32, turn, reserved;
+} cas_rope_part;
+
+/* Rotates the heads of 1..4 parts (q, k and v of one projection, say) in one launch.  A token's position is
+ * d_pos[token] (device, int32) or, with d_pos = NULL, pos0 + token; row p of d_table (n_pos rows, as
+ * cas_rope_table writes them for pos0 = 0) holds position p.  A token whose position is outside 0 .. n_pos-1
+ * is padding: nothing of it is written.  layout: CAS_ROPE_HALF pairs channels i and i + rot/2 of a head,
+ * CAS_ROPE_INTERLEAVED channels 2i and 2i+1; channels from rot on are taken over.
+ *   y_a = x_a cos - x_b sin,  y_b = x_b cos + x_a sin      (fp32, rounded to bf16 once)
+ * transposed != 0: sin with the other sign, which takes a rotation back (magnitude 1) and is what gradients of
+ * rotated heads go through.  rot <= head_dim <= 256 (CAS_ENOTSUP above).  The h_parts are HOST structs; their data
+ * pointers need the alignment of their elements only.  CAS_EINVAL unless the context's device is current. */
+int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout, int transposed,
+             const int32_t* d_pos, int pos0, int n_tok, int head_dim, int n_parts, const cas_rope_part* h_parts);
+
+/* ---- attention of a batch over a prefix that its sequences share --------------------------- */
+
+/*
+ * cas_attention for n_seqs (1..32) distinct sequences of one layer whose first prefix_len positions hold the
+ * same vectors (their page tables usually name the same pages there): the pages that lie whole in the prefix
+ * are read through the row of h_seqs[0] and decoded once for the queries of all sequences, what follows
+ * through each sequence's own row.  0 <= prefix_len <= the length of every sequence; the caller answers
+ * for the vectors being the same.  Arguments as for cas_attention_multi, except that a sequence may bring up to
+ * 16 columns, and a kv head have up to 48 query heads, in both forms.
+ * Outputs are those of cas_attention within its tolerance, not bit for bit: pages are added in runs whose length
+ * depends on prefix_len and n_kv_heads, and probabilities are rounded to bf16.  A sequence's values do not
+ * depend on the other sequences' lengths and values.
+ * Workspace: cas_attention_shared_bytes (host only; 0 for arguments that cas_attention_shared refuses).  Like
+ * every call that uses the context's workspace, two of them that may overlap (two streams, two captured
+ * graphs replayed side by side) need contexts with workspaces of their own.  CAS_EINVAL unless the context's device is current.
+ */
+int cas_attention_shared(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const int32_t* h_seqs, int prefix_len,
+                         int full, const uint16_t* const* h_d_Q, const int32_t* h_ncols, int n_q_heads,
+                         const uint16_t* const* h_d_Knew, const uint16_t* const* h_d_Vnew, const int32_t* h_n_new,
+                         uint16_t* const* h_d_O);
+size_t cas_attention_shared_bytes(const cas_kv* kv, int n_seqs, const int32_t* h_seqs, int prefix_len,
+                                  const int32_t* h_ncols, int n_q_heads, const int32_t* h_n_new);
+
+/* ---- eviction from the cache by accumulated attention weight ------------------------------ */
+
+/*
+ * cas_attention for one sequence that also adds up what every position received: with p[c][h][i] the softmax
+ * weight of position i in column c and query head h (0 where the column does not see it),
+ *   d_score_out[g][i] = (i < len ? d_score_in[g][i] : 0) + sum over the columns c and the query heads h of
+ *                       kv head g of p[c][h][i],                       i = 0 .. len + n_new - 1.
+ * d_score_in, d_score_out: float [n_kv_heads][ld], ld >= len + n_new, either the same or disjoint; d_score_in
+ * = NULL stands for zeros.  What stands behind the committed length in d_score_in is not read: the sums of
+ * in-flight positions that were not accepted are gone with them, those of accepted ones are kept.  Every
+ * column of the call counts, also one that is rejected later.  Entries from len + n_new on stay as they were.
+ * Other arguments, outputs and workspace rules as for cas_attention_shared (workspace: cas_attention_weights_bytes, host only;
+ * 0 for arguments that cas_attention_weights refuses).  Sums are fp32 in a fixed order.
+ */
+int cas_attention_weights(cas_ctx* ctx, cas_kv* kv, int layer, int seq, int full, const uint16_t* d_Q, int ncols,
+                          int n_q_heads, const uint16_t* d_Knew, const uint16_t* d_Vnew, int n_new, uint16_t* d_O,
+                          const float* d_score_in, float* d_score_out, int64_t ld);
+size_t cas_attention_weights_bytes(const cas_kv* kv, int seq, int ncols, int n_q_heads, int n_new);
+
+/* Which positions stay.  Per row of d_score (float [n_rows][ld], ld >= len; a row per kv head, or per layer and kv
+ * head): the first n_first positions, the last n_last and, of those between, the n_keep - n_first - n_last with
+ * the highest scores; of equal scores the lower positions stay, -0 equals +0 and NaN is above all.
+ * d_index: int32 [n_rows][n_keep], positions in ascending order.  d_kept: NULL or float [n_rows][ld_kept],
+ * receives the scores of the kept positions (ld_kept >= n_keep); it may be d_score itself with ld_kept = ld,
+ * whose entries from n_keep on then stay as they were.  0 <= n_first, n_last; n_first + n_last <= n_keep <= len.
+ * CAS_EINVAL unless the context's device is current. */
+int cas_kv_select(cas_ctx* ctx, const float* d_score, int64_t ld, int n_rows, int len, int n_keep, int n_first,
+                  int n_last, int32_t* d_index, float* d_kept, int64_t ld_kept);
+
+/* Moves the vectors that stay: in n_layers layers from layer0 on, position i of kv head g of dst_seq
+ * becomes position d_index[layer - layer0][g][i] of seq, K and V, still encoded as they are; i < n_keep,
+ * d_index: int32 [n_layers][n_kv_heads][n_keep], clamped into 0 .. len(seq)-1.  dst_seq = seq moves in
+ * place, for which the indices of a head have to ascend strictly, as cas_kv_select writes them; otherwise the pages of the
+ * two sequences must not be the same, and indices may be in any order and repeat.  Page table entries outside the pool are
+ * clamped for reading and not written to.  Nothing behind position n_keep of dst_seq changes, and no length does: cas_kv_set_len(dst_seq,
+ * n_keep) once all layers are done.  Pages that other sequences name too (a shared prefix) must not be evicted in place.
+ * The model passes place a token at the position that the cache's length gives; after an eviction use the
+ * stand-alone calls, with cas_rope at the positions that the tokens have.  CAS_EINVAL unless the context's device is current. */
+int cas_kv_evict(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, int seq, int dst_seq, const int32_t* d_index,
+                 int n_keep);
+
 /* ---- model-level steps of one speculative round (Sec. 2.2, Sec. 4.1) --------------------- */
 
 /* Llama-3 style decoder (Fig. 2_1): RMSNorm -> q,k,v projection -> rotary embedding ->

@@ -11,6 +11,8 @@ LIB_PATH = os.path.join(_HERE, "libcassandra_hip.so")
 
 CAS_OK, CAS_EINVAL, CAS_ENOTSUP, CAS_ENOMEM, CAS_EHIP = 0, -1, -2, -3, -4
 CAS_EXP_RAW, CAS_EXP_SHARED = 0, 2   # cas_fmt.exp_mode
+CAS_ROPE_PLAIN, CAS_ROPE_LINEAR, CAS_ROPE_BASE, CAS_ROPE_BANDS = 0, 1, 2, 3   # cas_rope_cfg.scaling
+CAS_ROPE_HALF, CAS_ROPE_INTERLEAVED = 0, 1
 
 
 class CasError(RuntimeError):
@@ -46,6 +48,16 @@ class cas_kv_desc(C.Structure):
                 ("K", C.c_int32), ("sw", C.c_int32), ("lw", C.c_int32), ("pw", C.c_int32),
                 ("tile_spec_bytes", C.c_int64), ("tile_verif_bytes", C.c_int64),
                 ("spec_pool_bytes", C.c_int64), ("verif_pool_bytes", C.c_int64)]
+
+
+class cas_rope_cfg(C.Structure):
+    _fields_ = [("rot", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("trained", C.c_int32), ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double)]
+
+
+class cas_rope_part(C.Structure):
+    _fields_ = [("d_x", C.c_void_p), ("d_y", C.c_void_p), ("ldx", C.c_int64), ("ldy", C.c_int64), ("n_heads", C.c_int32),
+                ("x_fp32", C.c_int32), ("turn", C.c_int32), ("reserved", C.c_int32)]
 
 
 class cas_model_cfg(C.Structure):
@@ -114,6 +126,21 @@ _SIGNATURES = {
     "cas_attention_static": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int,
                                        C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
     "cas_attention_static_capacity": (C.c_size_t, []),
+    "cas_rope_freqs": (C.c_int, [C.POINTER(cas_rope_cfg), C.POINTER(C.c_double)]),
+    "cas_rope_table": (C.c_int, [C.c_void_p, C.POINTER(cas_rope_cfg), C.c_int, C.c_int, C.c_void_p]),
+    "cas_rope": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int,
+                           C.c_int, C.c_int, C.POINTER(cas_rope_part)]),
+    "cas_attention_shared": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.POINTER(C.c_int32), C.c_int, C.c_int,
+                                       C.POINTER(C.c_void_p), C.POINTER(C.c_int32), C.c_int, C.POINTER(C.c_void_p),
+                                       C.POINTER(C.c_void_p), C.POINTER(C.c_int32), C.POINTER(C.c_void_p)]),
+    "cas_attention_shared_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.POINTER(C.c_int32), C.c_int, C.POINTER(C.c_int32),
+                                                C.c_int, C.POINTER(C.c_int32)]),
+    "cas_attention_weights": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int,
+                                        C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64]),
+    "cas_attention_weights_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int]),
+    "cas_kv_select": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p,
+                                C.c_void_p, C.c_int64]),
+    "cas_kv_evict": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int]),
     "cas_model_act_bytes": (C.c_int, [C.POINTER(cas_model_cfg), C.POINTER(C.c_size_t)]),
     "cas_model_create": (C.c_int, [C.POINTER(cas_model_cfg), C.POINTER(cas_model_weights), C.c_void_p, C.c_size_t,
                                    C.POINTER(C.c_void_p)]),
@@ -510,7 +537,9 @@ class KVCache:
     """Pools, page table and the cas_kv handle of a compressed paged cache."""
 
     def __init__(self, ctx: Context, n_layers, n_kv_heads, n_pages, max_seqs, max_pages_per_seq,
-                 keep_permille=600, trunc_bits=4, head_dim=128, page_tokens=64, page_table=None, exp_mode=0):
+                 keep_permille=600, trunc_bits=4, head_dim=128, page_tokens=64, page_table=None, exp_mode=0,
+                 spec_pool=None, verif_pool=None):
+        """spec_pool, verif_pool: device tensors to use as the pools (both or none), e.g. of a stored cache."""
         torch = ctx._torch
         d = cas_kv_desc()
         d.n_layers, d.n_kv_heads, d.head_dim, d.page_tokens = n_layers, n_kv_heads, head_dim, page_tokens
@@ -521,8 +550,12 @@ class KVCache:
             raise CasError(rc, "cas_kv_desc_init")
         self.desc = d
         self.ctx = ctx
-        self.spec_pool = torch.empty(d.spec_pool_bytes, dtype=torch.uint8, device="cuda")
-        self.verif_pool = torch.empty(d.verif_pool_bytes, dtype=torch.uint8, device="cuda")
+        if spec_pool is None:
+            spec_pool = torch.empty(d.spec_pool_bytes, dtype=torch.uint8, device="cuda")
+            verif_pool = torch.empty(d.verif_pool_bytes, dtype=torch.uint8, device="cuda")
+        for pool, nbytes in ((spec_pool, d.spec_pool_bytes), (verif_pool, d.verif_pool_bytes)):
+            assert pool.is_cuda and pool.is_contiguous() and pool.numel() * pool.element_size() >= nbytes
+        self.spec_pool, self.verif_pool = spec_pool, verif_pool
         if page_table is None:
             assert max_seqs * max_pages_per_seq <= n_pages
             page_table = torch.arange(max_seqs * max_pages_per_seq, dtype=torch.int32).reshape(
@@ -614,6 +647,143 @@ def cas_attention_static(ctx: Context, kv: KVCache, layer, seq, full, Q, Knew, V
 
 def cas_attention_static_capacity() -> int:
     return int(_lib().cas_attention_static_capacity())
+
+
+def cas_rope_freqs(cfg: cas_rope_cfg):
+    """The rot/2 frequencies after scaling, as a list (host only)."""
+    f = (C.c_double * max(1, cfg.rot // 2))()
+    rc = _lib().cas_rope_freqs(C.byref(cfg), f)
+    if rc != CAS_OK:
+        raise CasError(rc, "cas_rope_freqs")
+    return list(f)
+
+
+def cas_rope_table(ctx: Context, cfg: cas_rope_cfg, pos0, n_pos, out=None):
+    """cos, sin of positions pos0 .. pos0 + n_pos - 1: float32 [n_pos, rot/2, 2] (with rot = 128 a Model's rope table)."""
+    torch = ctx._torch
+    if out is None:
+        out = torch.empty((n_pos, cfg.rot // 2, 2), dtype=torch.float32, device="cuda")
+    assert out.is_cuda and out.is_contiguous() and out.dtype == torch.float32 and out.shape == (n_pos, cfg.rot // 2, 2)
+    ctx._check(_lib().cas_rope_table(ctx.h, C.byref(cfg), int(pos0), n_pos, _ptr(out)), "cas_rope_table")
+    return out
+
+
+def cas_rope(ctx: Context, table, xs, pos=None, pos0=0, layout=CAS_ROPE_HALF, transposed=False, turn=None, outs=None):
+    """Rotates up to four tensors [n_tok, heads, head_dim] (float32, or two-byte bf16 bits) of the same tokens; the heads
+    of a token side by side, tokens any stride apart.  table: float32 [n_pos, rot/2, 2] from position 0 on; pos: int32
+    [n_tok] on the GPU, or None for pos0 + token.  turn: per tensor, False to take it over unrotated.  Returns bf16
+    tensors (bits as int16 for float32 inputs, the input's type otherwise); outs may be given, xs[i] itself included
+    for two-byte tensors."""
+    torch = ctx._torch
+    assert table.is_cuda and table.is_contiguous() and table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2
+    n_tok, _, dim = xs[0].shape
+    assert pos is None or (pos.is_cuda and pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == n_tok)
+    if outs is None:
+        outs = [torch.empty(x.shape, dtype=torch.int16 if x.dtype == torch.float32 else x.dtype, device=x.device) for x in xs]
+    parts = (cas_rope_part * len(xs))()
+    for i, (x, y) in enumerate(zip(xs, outs, strict=True)):
+        assert x.is_cuda and y.is_cuda and x.shape == y.shape and x.shape[0] == n_tok and x.shape[2] == dim
+        assert y.element_size() == 2 and (x.element_size() == 2 or x.dtype == torch.float32)
+        for t in (x, y):  # a dimension of one element has no stride to speak of
+            assert (t.stride(2) == 1 or dim == 1) and (t.stride(1) == dim or t.shape[1] <= 1)
+        row = x.shape[1] * dim
+        ld = [t.stride(0) if n_tok > 1 else row for t in (x, y)]
+        parts[i] = cas_rope_part(x.data_ptr(), y.data_ptr(), ld[0], ld[1], x.shape[1], int(x.dtype == torch.float32),
+                                 int(turn is None or bool(turn[i])), 0)
+    ctx._check(_lib().cas_rope(ctx.h, _ptr(table), table.shape[0], 2 * table.shape[1], layout, int(bool(transposed)), _ptr(pos),
+                               int(pos0), n_tok, dim, len(xs), parts), "cas_rope")
+    return outs
+
+
+def _i32(v):
+    v = [int(x) for x in v]
+    return (C.c_int32 * len(v))(*v)
+
+
+def _ptrs(ts):
+    return (C.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
+
+
+def cas_attention_shared(ctx: Context, kv: KVCache, layer, seqs, prefix_len, full, Qs, Knews, Vnews, outs=None):
+    """Attention of several sequences whose first prefix_len positions are the same: lists of per-sequence tensors as in
+    cas_attention."""
+    torch = ctx._torch
+    seqs, Qs, Knews, Vnews = list(seqs), list(Qs), list(Knews), list(Vnews)
+    outs = [torch.empty_like(q) for q in Qs] if outs is None else list(outs)
+    assert len(seqs) == len(Qs) == len(Knews) == len(Vnews) == len(outs)
+    heads = Qs[0].shape[1]
+    for q, k, v, o in zip(Qs, Knews, Vnews, outs):
+        _check_attention(kv, q, k, v, o)
+        assert q.shape[1] == heads
+    ctx._check(_lib().cas_attention_shared(ctx.h, kv.h, layer, len(seqs), _i32(seqs), int(prefix_len), 1 if full else 0, _ptrs(Qs),
+                                           _i32(q.shape[0] for q in Qs), heads, _ptrs(Knews), _ptrs(Vnews),
+                                           _i32(k.shape[0] for k in Knews), _ptrs(outs)), "cas_attention_shared")
+    return outs
+
+
+def _check_attention(kv: KVCache, q, k, v, o):
+    h, d = kv.desc.n_kv_heads, kv.desc.head_dim
+    for t in (q, k, v, o):
+        assert t.is_cuda and t.is_contiguous() and t.element_size() == 2 and t.dim() == 3 and t.shape[2] == d
+    assert k.shape == v.shape and k.shape[1] == h and o.shape == q.shape
+
+
+def cas_attention_shared_bytes(kv: KVCache, seqs, prefix_len, ncols, n_q_heads, n_new) -> int:
+    """Workspace of cas_attention_shared for these sequences at their present lengths (0: arguments it refuses)."""
+    seqs = _i32(seqs)
+    return int(_lib().cas_attention_shared_bytes(kv.h, len(seqs), seqs, int(prefix_len), _i32(ncols), n_q_heads, _i32(n_new)))
+
+
+def cas_attention_weights(ctx: Context, kv: KVCache, layer, seq, full, Q, Knew, Vnew, score_in=None, score_out=None, out=None):
+    """cas_attention that also adds the weights every position received, per kv head, to score_in (float32
+    [n_kv_heads, >= len + n_new], None for zeros; only committed positions of it are read).  score_out: a tensor of
+    that form to write to, score_in itself included.  Returns (output, score_out)."""
+    torch = ctx._torch
+    if out is None:
+        out = torch.empty_like(Q)
+    _check_attention(kv, Q, Knew, Vnew, out)
+    total = cas_kv_len(kv, seq) + Knew.shape[0]
+    if score_out is None:
+        ld = total if score_in is None else score_in.stride(0)
+        score_out = torch.empty((kv.desc.n_kv_heads, ld), dtype=torch.float32, device=Q.device)[:, :total]
+    for s in (score_out,) if score_in is None else (score_in, score_out):
+        assert s.is_cuda and s.dtype == torch.float32 and s.shape[0] == kv.desc.n_kv_heads and s.shape[1] >= total
+        assert s.stride(1) == 1 and s.stride(0) == score_out.stride(0)
+    ctx._check(_lib().cas_attention_weights(ctx.h, kv.h, layer, seq, 1 if full else 0, _ptr(Q), Q.shape[0], Q.shape[1], _ptr(Knew),
+                                            _ptr(Vnew), Knew.shape[0], _ptr(out), _ptr(score_in), _ptr(score_out),
+                                            score_out.stride(0)), "cas_attention_weights")
+    return out, score_out
+
+
+def cas_attention_weights_bytes(kv: KVCache, seq, ncols, n_q_heads, n_new) -> int:
+    """Workspace of cas_attention_weights at the sequence's present length (0: arguments it refuses)."""
+    return int(_lib().cas_attention_weights_bytes(kv.h, seq, ncols, n_q_heads, n_new))
+
+
+def cas_kv_select(ctx: Context, score, length, n_keep, n_first=0, n_last=0, kept=None, index=None):
+    """score: float32 [rows, >= length] -> int32 [rows, n_keep], the positions that stay, ascending.  kept: float32
+    [rows, >= n_keep] for their scores, score itself included."""
+    torch = ctx._torch
+    rows = score.shape[0]
+    for s, n in ((score, length),) if kept is None else ((score, length), (kept, n_keep)):
+        assert s.is_cuda and s.dtype == torch.float32 and s.dim() == 2 and s.shape[0] == rows and s.shape[1] >= n
+        assert (s.stride(1) == 1 or s.shape[1] <= 1) and (s.stride(0) >= s.shape[1] or rows <= 1)
+    if index is None:
+        index = torch.empty((rows, n_keep), dtype=torch.int32, device=score.device)
+    assert index.is_cuda and index.is_contiguous() and index.dtype == torch.int32 and index.shape == (rows, n_keep)
+    ld = [max(s.stride(0), s.shape[1]) for s in (score, score if kept is None else kept)]
+    ctx._check(_lib().cas_kv_select(ctx.h, _ptr(score), ld[0], rows, length, n_keep, n_first, n_last, _ptr(index), _ptr(kept), ld[1]),
+               "cas_kv_select")
+    return index
+
+
+def cas_kv_evict(ctx: Context, kv: KVCache, layer0, n_layers, seq, dst_seq, index):
+    """Position i of dst_seq becomes position index[layer - layer0, head, i] of seq; index: int32 [n_layers, n_kv_heads,
+    n_keep] on the GPU.  Does not change a length."""
+    torch = ctx._torch
+    assert index.is_cuda and index.is_contiguous() and index.dtype == torch.int32 and index.dim() == 3
+    assert index.shape[:2] == (n_layers, kv.desc.n_kv_heads)
+    ctx._check(_lib().cas_kv_evict(ctx.h, kv.h, layer0, n_layers, seq, dst_seq, _ptr(index), index.shape[2]), "cas_kv_evict")
 
 
 def _tensor(ew: EncodedWeight) -> cas_tensor:

@@ -80,6 +80,11 @@ inline int allow_lds(cas_ctx* ctx, const void* kernel, size_t lds, LdsLimit& lim
 }
 
 inline bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
+// whether the context's device is the current one, which its stream and buffers belong to
+inline bool on_device(const cas_ctx* ctx) {
+  int dev = -1;
+  return hipGetDevice(&dev) == hipSuccess && dev == ctx->device;
+}
 
 int launch_encode_weight(cas_ctx*, const uint16_t* W, int64_t ld, const float* act, const cas_wdesc&, void* spec, void* verif);
 int launch_decode_weight(cas_ctx*, const cas_wdesc&, const void* spec, const void* verif, uint16_t* out, int64_t ld);

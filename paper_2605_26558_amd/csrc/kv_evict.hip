@@ -1,0 +1,316 @@
+// Eviction from the compressed cache: which positions of a row of scores stay, and the encoded vectors of these moved
+// to the front of a sequence's pages as they are (no stream is decoded).
+#include <algorithm>
+#include "cas_device.hpp"
+#include "cas_internal.hpp"
+
+namespace cas {
+
+// ---- selection ----------------------------------------------------------------------------------
+// One workgroup per row.  The scores between the first and the last positions are mapped to integers of the same order;
+// the threshold (the highest value that enough of them reach) is found two bits at a time by counting, and of its equals
+// the lower positions are taken.  Kept positions are dealt their places by counting those before them: ballots within a
+// wave, one table of counts per wave and step for the workgroup.
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+
+__device__ __forceinline__ uint32_t score_key(float v) {  // NaN on top, -0 as +0; 0 is below every key
+  if (v != v) return 0xFFFFFFFFu;
+  const uint32_t u = __float_as_uint(v + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+struct SelectArgs {
+  const float* score;
+  int64_t ld, ld_kept;
+  int len, n_keep, n_first, n_last;
+  int32_t* index;
+  float* kept;
+};
+
+// PER: scores of a thread kept in registers; 0: read again wherever they are needed (rows too long for registers)
+template <int PER>
+__global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
+  constexpr int N = PER > 0 ? PER : 1;
+  __shared__ uint32_t cnt[2][kSelWaves][3];
+  __shared__ uint32_t tot[kSelWaves][2];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const float* row = a.score + (int64_t)blockIdx.x * a.ld;
+  int32_t* index = a.index + (int64_t)blockIdx.x * a.n_keep;
+  float* kept = a.kept ? a.kept + (int64_t)blockIdx.x * a.ld_kept : nullptr;
+  const int lo = a.n_first, hi = a.len - a.n_last;   // the middle: positions lo .. hi - 1
+  const uint32_t want = (uint32_t)(a.n_keep - a.n_first - a.n_last);
+  const int steps = (a.len + kSelThreads - 1) / kSelThreads;
+  float v[N];
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int p = i * kSelThreads + tid;
+      v[i] = p < a.len ? row[p] : 0.f;
+    }
+  }
+  auto value = [&](int i) { const int p = i * kSelThreads + tid; return p < a.len ? row[p] : 0.f; };
+  auto key_of = [&](int i, float x) {  // 0 outside the middle
+    const int p = i * kSelThreads + tid;
+    return p >= lo && p < hi ? score_key(x) : 0u;
+  };
+  uint32_t key[N];
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = key_of(i, v[i]);
+  }
+  // the largest T with at least `want` keys >= T (1 where none are wanted: then no tie is taken either)
+  uint32_t T = 0, above = 0;
+  for (int bit = 30, turn = 0; bit >= 0 && want > 0; bit -= 2, turn ^= 1) {
+    uint32_t n[3] = {0, 0, 0};
+    const uint32_t t1 = T | 1u << bit, t2 = T | 2u << bit, t3 = T | 3u << bit;
+    auto count = [&](uint32_t k) {
+      n[0] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t1));
+      n[1] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t2));
+      n[2] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t3));
+    };
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) count(key[i]);
+    } else {
+      for (int i = 0; i < steps; ++i) count(key_of(i, value(i)));
+    }
+    if (lane < 3) cnt[turn][wv][lane] = lane == 0 ? n[0] : lane == 1 ? n[1] : n[2];
+    __syncthreads();
+    uint32_t s[3] = {0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kSelWaves; ++w) {
+#pragma unroll
+      for (int q = 0; q < 3; ++q) s[q] += cnt[turn][w][q];
+    }
+    T = s[2] >= want ? t3 : s[1] >= want ? t2 : s[0] >= want ? t1 : T;
+  }
+  if (want > 0) {  // keys above the threshold
+    uint32_t n = 0;
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) n += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(key[i] > T));
+    } else {
+      for (int i = 0; i < steps; ++i) n += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(key_of(i, value(i)) > T));
+    }
+    __syncthreads();
+    if (lane == 0) cnt[0][wv][0] = n;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kSelWaves; ++w) above += cnt[0][w][0];
+  }
+  const uint32_t ties = want - above;  // equals of the threshold that stay
+  uint32_t base = 0, tie_base = 0;     // kept positions and equals before this step
+  for (int i = 0; i < steps; ++i) {
+    float x;
+    uint32_t k;
+    if constexpr (PER > 0) {
+      x = v[0]; k = key[0];
+#pragma unroll
+      for (int q = 1; q < PER; ++q) {
+        if (i == q) { x = v[q]; k = key[q]; }
+      }
+    } else {
+      x = value(i);
+      k = key_of(i, x);
+    }
+    const int p = i * kSelThreads + tid;
+    const bool edge = p < a.len && (p < lo || p >= hi), sure = edge || (want > 0 && k > T);
+    const bool tie = want > 0 && k != 0u && k == T;
+    const uint64_t ms = __builtin_amdgcn_ballot_w64(sure), mt = __builtin_amdgcn_ballot_w64(tie);
+    __syncthreads();  // the counts of the step before have been read
+    if (lane == 0) {
+      tot[wv][0] = (uint32_t)__popcll(ms);
+      tot[wv][1] = (uint32_t)__popcll(mt);
+    }
+    __syncthreads();
+    uint32_t s_before = base, t_before = tie_base, s_all = base, t_all = tie_base;
+#pragma unroll
+    for (int w = 0; w < kSelWaves; ++w) {
+      s_before += w < wv ? tot[w][0] : 0u;
+      t_before += w < wv ? tot[w][1] : 0u;
+      s_all += tot[w][0];
+      t_all += tot[w][1];
+    }
+    const uint64_t below = (1ull << lane) - 1ull;
+    const uint32_t s_rank = s_before + (uint32_t)__popcll(ms & below), t_rank = t_before + (uint32_t)__popcll(mt & below);
+    if (sure || (tie && t_rank < ties)) {
+      const uint32_t at = s_rank + min(t_rank, ties);
+      index[at] = p;
+      if (kept) kept[at] = x;  // never behind p, and this step's scores have been read by all
+    }
+    base = s_all;
+    tie_base = t_all;
+  }
+}
+
+// ---- moving ---------------------------------------------------------------------------------------
+// A tile (64 vectors of one head) is two runs of words, its parts of the two pools, each made of streams of w words per
+// vector in vector order.  A thread moves four words of the destination that follow one another and were, where they do
+// not reach into the next vector, four words that followed one another in the source: 16 bytes either way.
+struct MoveStream {
+  int begin, w;       // first word in the pool's part of a tile, words of a vector
+  uint32_t inv;       // ceil(2^18 / w): word e < 4096 of the stream belongs to vector e * inv >> 18
+};
+struct MoveArgs {
+  KvGeom g;
+  uint32_t* pool[2];
+  int tile_words[2];
+  int n_streams[2];
+  MoveStream s[2][3];
+  int words[2];       // words of a tile that hold vectors
+  const int32_t* src_row;
+  const int32_t* dst_row;
+  const int32_t* index;
+  int layer0, n_keep, len;
+};
+
+constexpr int kMoveThreads = 256;
+constexpr int kMoveGroups = 5;  // groups of four words of a thread and pool: 64 x 68 words and fewer in 4 x 256 + 64 groups
+
+struct MoveGroup {
+  uint32_t v[4];
+};
+
+// The words of group q of one pool's part: gathered from the vectors that stay.  src: first word of the pool's part of the
+// tile that vector r of the destination comes from; row: its place there.
+__device__ __forceinline__ MoveGroup move_load(const MoveArgs& a, int pool, int q, const uint32_t* const* src, const int* row,
+                                               int rows) {
+  MoveGroup m;
+  const int word = 4 * q;
+  MoveStream s = a.s[pool][0];
+#pragma unroll
+  for (int i = 1; i < 3; ++i)
+    if (i < a.n_streams[pool] && word >= a.s[pool][i].begin) s = a.s[pool][i];
+  const uint32_t e = (uint32_t)(word - s.begin);
+  int r = (int)(e * s.inv >> 18), c = (int)e - r * s.w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m.v[i] = 0;
+    if (r < rows) m.v[i] = src[r][s.begin + row[r] * s.w + c];
+    if (++c == s.w) { c = 0; ++r; }
+  }
+  return m;
+}
+
+__device__ __forceinline__ void move_store(const MoveArgs& a, int pool, int q, uint32_t* dst, const MoveGroup& m, int rows) {
+  const int word = 4 * q;
+  MoveStream s = a.s[pool][0];
+#pragma unroll
+  for (int i = 1; i < 3; ++i)
+    if (i < a.n_streams[pool] && word >= a.s[pool][i].begin) s = a.s[pool][i];
+  const int left = s.begin + rows * s.w - word;  // words of the stream from here on that belong to the vectors moved
+  if (left >= 4) {
+    *reinterpret_cast<uint4*>(dst + word) = make_uint4(m.v[0], m.v[1], m.v[2], m.v[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < left) dst[word + i] = m.v[i];
+  }
+}
+
+// blockIdx.y: K heads, then V heads; blockIdx.z: 2 * layer + pool.  IN_PLACE: one workgroup takes all tiles of a head in
+// order, tile i being read whole before it is written.  Position i moves to or before the place it comes from (the
+// indices ascend), so a tile is never written before a later one has been read from it.
+template <bool IN_PLACE>
+__global__ __launch_bounds__(kMoveThreads) void move_kernel(MoveArgs a) {
+  __shared__ const uint32_t* src[64];
+  __shared__ int row[64];
+  const KvGeom& g = a.g;
+  const int pool = blockIdx.z & 1, layer = blockIdx.z >> 1, kvh = blockIdx.y, tid = threadIdx.x;
+  const int head = kvh % g.n_kv_heads, kv = kvh / g.n_kv_heads;
+  const int32_t* index = a.index + ((int64_t)layer * g.n_kv_heads + head) * a.n_keep;
+  auto part = [&](int page) {
+    const size_t tile = (((size_t)(a.layer0 + layer) * g.n_pages + page) * 2 + kv) * g.n_kv_heads + head;
+    return a.pool[pool] + tile * a.tile_words[pool];
+  };
+  const int tiles = (a.n_keep + 63) / 64, groups = a.words[pool] / 4;
+  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const int rows = min(64, a.n_keep - 64 * t);
+    if (tid < 64) {
+      const int p = min(max(index[64 * t + min(tid, rows - 1)], 0), a.len - 1);
+      src[tid] = part(min(max(a.src_row[p >> 6], 0), g.n_pages - 1));
+      row[tid] = p & 63;
+    }
+    __syncthreads();
+    MoveGroup m[kMoveGroups];
+#pragma unroll
+    for (int i = 0; i < kMoveGroups; ++i) {
+      const int q = tid + i * kMoveThreads;
+      if (q < groups) m[i] = move_load(a, pool, q, src, row, rows);
+    }
+    if (IN_PLACE) __syncthreads();  // the whole tile is in registers
+    const int page = a.dst_row[t];
+    if (page >= 0 && page < g.n_pages) {
+      uint32_t* dst = part(page);
+#pragma unroll
+      for (int i = 0; i < kMoveGroups; ++i) {
+        const int q = tid + i * kMoveThreads;
+        if (q < groups) move_store(a, pool, q, dst, m[i], rows);
+      }
+    }
+    __syncthreads();  // the table of this tile is done with, and its words are written
+  }
+}
+
+static int launch_select(cas_ctx* ctx, const SelectArgs& a, int n_rows) {
+  const dim3 grid(n_rows), block(kSelThreads);
+  if (a.len <= 8 * kSelThreads) hipLaunchKernelGGL(select_kernel<8>, grid, block, 0, ctx->stream, a);
+  else if (a.len <= 32 * kSelThreads) hipLaunchKernelGGL(select_kernel<32>, grid, block, 0, ctx->stream, a);
+  else hipLaunchKernelGGL(select_kernel<0>, grid, block, 0, ctx->stream, a);
+  CAS_HIP(ctx, hipGetLastError());
+  return CAS_OK;
+}
+
+static void add_stream(MoveArgs& a, int pool, int begin, int w) {
+  if (w == 0) return;
+  a.s[pool][a.n_streams[pool]++] = MoveStream{begin, w, ((1u << 18) + (uint32_t)w - 1u) / (uint32_t)w};
+  a.words[pool] = begin + 64 * w;
+}
+
+static int launch_evict(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, int seq, int dst_seq, const int32_t* d_index, int n_keep) {
+  const KvGeom& g = kv->geom;
+  MoveArgs a{};
+  a.g = g;
+  a.pool[0] = (uint32_t*)kv->d_spec; a.pool[1] = (uint32_t*)kv->d_verif;
+  a.tile_words[0] = g.tile_spec_words; a.tile_words[1] = g.tile_verif_words;
+  add_stream(a, 0, 0, 4);
+  if (g.mx) add_stream(a, 0, 64 * 4, 1);
+  add_stream(a, 0, g.spec_off, g.sw);
+  add_stream(a, 1, 0, g.lw);
+  add_stream(a, 1, 64 * g.lw, g.pw);
+  a.src_row = kv->d_page_table + (size_t)seq * g.max_pages_per_seq;
+  a.dst_row = kv->d_page_table + (size_t)dst_seq * g.max_pages_per_seq;
+  a.index = d_index;
+  a.layer0 = layer0; a.n_keep = n_keep; a.len = kv->h_len[seq];
+  const int tiles = (n_keep + 63) / 64;
+  if (seq == dst_seq) hipLaunchKernelGGL(move_kernel<true>, dim3(1, 2 * g.n_kv_heads, 2 * n_layers), dim3(kMoveThreads), 0, ctx->stream, a);
+  else hipLaunchKernelGGL(move_kernel<false>, dim3(tiles, 2 * g.n_kv_heads, 2 * n_layers), dim3(kMoveThreads), 0, ctx->stream, a);
+  CAS_HIP(ctx, hipGetLastError());
+  return CAS_OK;
+}
+
+}  // namespace cas
+
+extern "C" {
+
+int cas_kv_select(cas_ctx* ctx, const float* d_score, int64_t ld, int n_rows, int len, int n_keep, int n_first, int n_last,
+                  int32_t* d_index, float* d_kept, int64_t ld_kept) {
+  if (!ctx || n_rows < 0 || len < 0 || ld < len || n_first < 0 || n_last < 0 || n_keep < 0 || n_keep > len) return CAS_EINVAL;
+  if ((int64_t)n_first + n_last > n_keep || (d_kept && ld_kept < n_keep)) return CAS_EINVAL;
+  if (d_kept && d_kept == d_score && ld_kept != ld) return CAS_EINVAL;
+  if (n_rows == 0 || n_keep == 0) return CAS_OK;
+  if (len > 1 << 30) return CAS_ENOTSUP;
+  if (!d_score || !d_index || !cas::on_device(ctx)) return CAS_EINVAL;
+  cas::SelectArgs a{d_score, ld, ld_kept, len, n_keep, n_first, n_last, d_index, d_kept};
+  return cas::launch_select(ctx, a, n_rows);
+}
+
+int cas_kv_evict(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, int seq, int dst_seq, const int32_t* d_index, int n_keep) {
+  if (!ctx || !kv || seq < 0 || seq >= kv->desc.max_seqs || dst_seq < 0 || dst_seq >= kv->desc.max_seqs) return CAS_EINVAL;
+  if (layer0 < 0 || n_layers < 0 || n_layers > kv->desc.n_layers - layer0 || n_keep < 0 || n_keep > kv->h_len[seq]) return CAS_EINVAL;
+  if (n_layers == 0 || n_keep == 0) return CAS_OK;
+  if (!d_index || !cas::on_device(ctx)) return CAS_EINVAL;
+  return cas::launch_evict(ctx, kv, layer0, n_layers, seq, dst_seq, d_index, n_keep);
+}
+
+}  // extern "C"

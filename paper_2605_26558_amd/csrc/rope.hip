@@ -1,0 +1,281 @@
+// Rotary positions for callers that drive the cache and the attention themselves: the table of cos and sin of a range of
+// positions, with the frequencies scaled for long contexts, and the rotation of the heads of a projection at positions
+// given one by one.  (The model passes rotate inside their own kernels, at the positions of the cache.)
+#include <algorithm>
+#include <cmath>
+#include "cas_device.hpp"
+#include "cas_internal.hpp"
+
+namespace cas {
+
+constexpr int kRopePairs = 128;       // most pairs of a head
+constexpr int kRopeTablePos = 16;     // positions of a thread
+
+struct RopeFreqs {
+  double quarter[kRopePairs];  // quarter turns per position of every pair
+};
+
+// sin and cos of a in [-pi/4, pi/4] (a little beyond for rounding) by their Taylor series: the first term left out is below
+// 2e-9 and 2e-10.  Fused multiply-adds, so the error is that of the last two operations, about a unit in the last place.
+__device__ __forceinline__ void sincos_eighth(float a, float& s, float& c) {
+  const float z = a * a;
+  s = fmaf(a * z, fmaf(z, fmaf(z, fmaf(z, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), a);
+  c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);
+}
+
+// Angles are formed and reduced to an eighth turn in 64 bits (four operations; position times frequency reaches 2^24 quarter
+// turns of which 32 bits would leave nothing), the rest is fp32.  Bound by the writes: 67 MB for 131072 positions of 64 pairs.
+// A thread keeps its pair (PAIRS = 2: two, written as 16 bytes) over kRopeTablePos positions, so the frequency is read once.
+template <int PAIRS>
+__global__ __launch_bounds__(256) void rope_table_kernel(RopeFreqs f, int units, int rows, int pos0, int n_pos, float mag,
+                                                         float* __restrict__ table) {
+  const int row = (int)threadIdx.x / units, u = (int)threadIdx.x - row * units;
+  if (row >= rows) return;  // units that do not divide the workgroup
+  double fr[PAIRS];
+#pragma unroll
+  for (int k = 0; k < PAIRS; ++k) fr[k] = f.quarter[u * PAIRS + k];
+  const int p0 = (int)blockIdx.x * rows * kRopeTablePos + row;
+#pragma unroll 4
+  for (int i = 0; i < kRopeTablePos; ++i) {
+    const int p = p0 + i * rows;
+    if (p >= n_pos) return;
+    float v[2 * PAIRS];
+#pragma unroll
+    for (int k = 0; k < PAIRS; ++k) {
+      const double t = (double)(pos0 + p) * fr[k], q = rint(t);
+      const int quad = (int)(long long)q;
+      float s, c;
+      sincos_eighth((float)((t - q) * 1.5707963267948966), s, c);
+      const float x = quad & 1 ? s : c, y = quad & 1 ? c : s;  // |cos|, |sin| change places every quarter turn
+      v[2 * k] = mag * ((quad + 1) & 2 ? -x : x);
+      v[2 * k + 1] = mag * (quad & 2 ? -y : y);
+    }
+    float* dst = table + ((size_t)p * units + u) * (2 * PAIRS);
+    if constexpr (PAIRS == 2) *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<float2*>(dst) = make_float2(v[0], v[1]);
+  }
+}
+
+constexpr int kRopeParts = 4;
+struct RopeArgs {
+  cas_rope_part part[kRopeParts];
+  int head0[kRopeParts + 1];  // heads of a token before each part
+  const float* table;
+  const int32_t* pos;
+  int pos0, n_pos, n_tok, half, dim, parts, blocks;  // half: pairs of a head; blocks: workgroups of a token
+  float sign;
+};
+
+// V consecutive values as floats: bf16 (exact) or floats rounded to bf16, as every tensor that passes from one operation to
+// the next is
+template <int V>
+__device__ __forceinline__ void rope_load(const cas_rope_part& p, size_t at, float (&v)[V]) {
+  if (p.x_fp32) {
+    const float* x = static_cast<const float*>(p.d_x) + at;
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      if constexpr (V == 1) v[i] = x[i];
+      else {
+        const float4 q = *reinterpret_cast<const float4*>(x + i);
+        v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = round_bf16(v[i]);
+  } else {
+    const uint16_t* x = static_cast<const uint16_t*>(p.d_x) + at;
+    if constexpr (V == 1) v[0] = bf16_to_f32(x[0]);
+    else {
+      const uint4 q = *reinterpret_cast<const uint4*>(x);
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      }
+    }
+  }
+}
+template <int V>
+__device__ __forceinline__ void rope_store(uint16_t* y, const float (&v)[V]) {
+  if constexpr (V == 1) y[0] = f32_to_bf16(v[0]);
+  else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)f32_to_bf16(v[2 * i]) | ((uint32_t)f32_to_bf16(v[2 * i + 1]) << 16);
+    *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// The places of a head that one thread takes: with halves, V pairs (V values of either half) or V values behind the turning
+// ones; interleaved, V/2 pairs (one for V = 1) or V values behind.
+template <int V, bool INTER>
+struct RopeUnits {
+  static constexpr int kPairs = INTER && V > 1 ? V / 2 : V;
+  static __host__ __device__ int turning(int half) { return half / kPairs; }
+  static __host__ __device__ int of_head(int half, int dim) { return turning(half) + (dim - 2 * half) / V; }
+};
+
+// Bound by memory: every value is read and written once, a token's row of the table comes from a cache for all heads but
+// the first.  A workgroup takes some heads of one token: `units` threads to a head, each with its part of the table's row in
+// registers for all heads that it goes through.
+template <int V, bool INTER>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+  using U = RopeUnits<V, INTER>;
+  const int units = U::of_head(a.half, a.dim), turning = U::turning(a.half);
+  const int slots = 256 / units, slot = (int)threadIdx.x / units, u = (int)threadIdx.x - slot * units;
+  const int tok = (int)blockIdx.x / a.blocks, block = (int)blockIdx.x - tok * a.blocks;
+  const int p = a.pos ? a.pos[tok] : a.pos0 + tok;
+  if (p < 0 || p >= a.n_pos || slot >= slots) return;  // padding, or a thread without a place
+  const int heads = a.head0[a.parts];
+  const bool turns = u < turning;
+  float c[U::kPairs], s[U::kPairs];
+  if (turns) {
+    const float2* row = reinterpret_cast<const float2*>(a.table) + (size_t)p * a.half + u * U::kPairs;
+#pragma unroll
+    for (int i = 0; i < U::kPairs; ++i) {
+      const float2 cs = row[i];
+      c[i] = cs.x;
+      s[i] = a.sign * cs.y;
+    }
+  }
+  for (int h = block * slots + slot; h < heads; h += a.blocks * slots) {
+    int k = 0;
+#pragma unroll
+    for (int i = 1; i < kRopeParts; ++i) k += i < a.parts && h >= a.head0[i] ? 1 : 0;
+    const cas_rope_part& part = a.part[k];
+    const int at = (h - a.head0[k]) * a.dim;
+    const size_t x0 = (size_t)tok * part.ldx + at;
+    uint16_t* y = part.d_y + (size_t)tok * part.ldy + at;
+    if (!turns) {
+      const int e = 2 * a.half + (u - turning) * V;
+      float v[V];
+      rope_load<V>(part, x0 + e, v);
+      rope_store<V>(y + e, v);
+      continue;
+    }
+    if constexpr (INTER && V > 1) {
+      float v[V];
+      rope_load<V>(part, x0 + u * V, v);
+      if (part.turn) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+          const float p0 = v[2 * i], p1 = v[2 * i + 1];
+          v[2 * i] = p0 * c[i] - p1 * s[i];
+          v[2 * i + 1] = p1 * c[i] + p0 * s[i];
+        }
+      }
+      rope_store<V>(y + u * V, v);
+    } else {
+      const int e0 = INTER ? 2 * u : u * V, e1 = INTER ? 2 * u + 1 : a.half + u * V;
+      float v0[V], v1[V];
+      rope_load<V>(part, x0 + e0, v0);
+      rope_load<V>(part, x0 + e1, v1);
+      if (part.turn) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float p0 = v0[i], p1 = v1[i];
+          v0[i] = p0 * c[i] - p1 * s[i];
+          v1[i] = p1 * c[i] + p0 * s[i];
+        }
+      }
+      rope_store<V>(y + e0, v0);
+      rope_store<V>(y + e1, v1);
+    }
+  }
+}
+
+template <int V, bool INTER>
+static int launch_rope(cas_ctx* ctx, RopeArgs& a) {
+  const int units = RopeUnits<V, INTER>::of_head(a.half, a.dim), slots = 256 / units;
+  // few tokens: a workgroup for every 256/units heads; many: one for all heads of a token, whose table row is then read once
+  const int most = (a.head0[a.parts] + slots - 1) / slots;
+  a.blocks = std::max(1, std::min(most, 1024 / a.n_tok));
+  const int64_t grid = (int64_t)a.n_tok * a.blocks;
+  if (grid > 0x7FFFFFFF) return CAS_ENOTSUP;
+  hipLaunchKernelGGL((rope_kernel<V, INTER>), dim3((unsigned)grid), dim3(256), 0, ctx->stream, a);
+  CAS_HIP(ctx, hipGetLastError());
+  return CAS_OK;
+}
+
+}  // namespace cas
+
+static bool rope_cfg_ok(const cas_rope_cfg* c) {
+  if (!c || c->rot < 2 || c->rot > 2 * cas::kRopePairs || (c->rot & 1)) return false;
+  if (c->scaling < CAS_ROPE_PLAIN || c->scaling > CAS_ROPE_BANDS) return false;
+  if (!(c->base >= 1.0) || !std::isfinite(c->base) || !(c->magnitude > 0.0) || !std::isfinite(c->magnitude)) return false;
+  if (c->scaling != CAS_ROPE_PLAIN && (!(c->factor >= 1.0) || !std::isfinite(c->factor))) return false;
+  if (c->scaling == CAS_ROPE_BASE && c->rot < 4) return false;
+  if (c->scaling == CAS_ROPE_BANDS &&
+      (c->trained < 1 || !(c->low >= 0.0) || !(c->high > c->low) || !std::isfinite(c->high)))
+    return false;
+  return true;
+}
+
+extern "C" {
+
+int cas_rope_freqs(const cas_rope_cfg* cfg, double* h_freqs) {
+  if (!rope_cfg_ok(cfg) || !h_freqs) return CAS_EINVAL;
+  const double base = cfg->scaling == CAS_ROPE_BASE ? cfg->base * std::pow(cfg->factor, (double)cfg->rot / (cfg->rot - 2)) : cfg->base;
+  for (int i = 0; i < cfg->rot / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / cfg->rot);
+    if (cfg->scaling == CAS_ROPE_LINEAR) f /= cfg->factor;
+    if (cfg->scaling == CAS_ROPE_BANDS) {
+      const double turns = cfg->trained * f / 6.283185307179586;
+      const double g = std::min(1.0, std::max(0.0, (turns - cfg->low) / (cfg->high - cfg->low)));
+      f = g * f + (1.0 - g) * f / cfg->factor;
+    }
+    h_freqs[i] = f;
+  }
+  return CAS_OK;
+}
+
+int cas_rope_table(cas_ctx* ctx, const cas_rope_cfg* cfg, int pos0, int n_pos, float* d_table) {
+  if (!ctx || !rope_cfg_ok(cfg) || pos0 < 0 || n_pos < 0 || (int64_t)pos0 + n_pos > (1 << 24)) return CAS_EINVAL;
+  if (n_pos == 0) return CAS_OK;
+  if (!d_table || !cas::aligned256(d_table) || !cas::on_device(ctx)) return CAS_EINVAL;
+  cas::RopeFreqs f{};
+  const int rc = cas_rope_freqs(cfg, f.quarter);
+  if (rc != CAS_OK) return rc;
+  for (int i = 0; i < cfg->rot / 2; ++i) f.quarter[i] *= 0.6366197723675814;  // 2 / pi
+  const int half = cfg->rot / 2, pairs = half & 1 ? 1 : 2, units = half / pairs, rows = 256 / units;
+  const dim3 grid((n_pos + rows * cas::kRopeTablePos - 1) / (rows * cas::kRopeTablePos));
+  hipLaunchKernelGGL(pairs == 2 ? cas::rope_table_kernel<2> : cas::rope_table_kernel<1>, grid, dim3(256), 0, ctx->stream, f,
+                     units, rows, pos0, n_pos, (float)cfg->magnitude, d_table);
+  CAS_HIP(ctx, hipGetLastError());
+  return CAS_OK;
+}
+
+int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout, int transposed, const int32_t* d_pos,
+             int pos0, int n_tok, int head_dim, int n_parts, const cas_rope_part* h_parts) {
+  if (!ctx || n_pos < 0 || n_tok < 0 || rot < 2 || (rot & 1) || head_dim < rot || n_parts < 1 || n_parts > cas::kRopeParts || !h_parts)
+    return CAS_EINVAL;
+  if (layout != CAS_ROPE_HALF && layout != CAS_ROPE_INTERLEAVED) return CAS_EINVAL;
+  if (!d_pos && (int64_t)pos0 + n_tok > 0x7FFFFFFF) return CAS_EINVAL;
+  if (head_dim > 2 * cas::kRopePairs) return CAS_ENOTSUP;
+  cas::RopeArgs a{};
+  const int half = rot / 2;
+  // eight values at a time where every access then is 16 bytes on a multiple of 16; single pairs otherwise
+  bool wide = head_dim % 8 == 0 && (layout == CAS_ROPE_HALF ? half % 8 == 0 : rot % 8 == 0);
+  for (int i = 0; i < n_parts; ++i) {
+    const cas_rope_part& p = h_parts[i];
+    if (p.n_heads < 0 || p.n_heads > (1 << 16)) return CAS_EINVAL;
+    const int64_t row = (int64_t)p.n_heads * head_dim;
+    if (p.ldx < row || p.ldy < row) return CAS_EINVAL;
+    a.part[i] = p;
+    a.head0[i + 1] = a.head0[i] + p.n_heads;
+    if (row == 0 || n_tok == 0) continue;
+    const uintptr_t x = (uintptr_t)p.d_x, y = (uintptr_t)p.d_y;
+    if (!x || !y || x % (p.x_fp32 ? 4 : 2) || y % 2) return CAS_EINVAL;
+    if (x == y && (p.x_fp32 || p.ldx != p.ldy)) return CAS_EINVAL;
+    wide = wide && x % 16 == 0 && y % 16 == 0 && p.ldx % 8 == 0 && p.ldy % 8 == 0;
+  }
+  if (n_tok == 0 || n_pos == 0 || a.head0[n_parts] == 0) return CAS_OK;
+  if (!d_table || !cas::aligned256(d_table) || !cas::on_device(ctx)) return CAS_EINVAL;
+  a.table = d_table; a.pos = d_pos; a.pos0 = pos0; a.n_pos = n_pos; a.n_tok = n_tok;
+  a.half = half; a.dim = head_dim; a.parts = n_parts; a.sign = transposed ? -1.f : 1.f;
+  if (layout == CAS_ROPE_HALF) return wide ? cas::launch_rope<8, false>(ctx, a) : cas::launch_rope<1, false>(ctx, a);
+  return wide ? cas::launch_rope<8, true>(ctx, a) : cas::launch_rope<1, true>(ctx, a);
+}
+
+}  // extern "C"
