@@ -21,85 +21,172 @@ extern template int launch_rows_partial<true, false>(cas_ctx*, const RowsArgs&, 
 extern template int launch_rows_partial<false, false>(cas_ctx*, const RowsArgs&, int);
 extern template int launch_rows_partial<true, true>(cas_ctx*, const RowsArgs&, int);
 extern template int launch_rows_partial<false, true>(cas_ctx*, const RowsArgs&, int);
+extern template int launch_prefix_partial<true, false>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_prefix_partial<false, false>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_prefix_partial<true, true>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_prefix_partial<false, true>(cas_ctx*, const RowsArgs&, int, int);
 
-// One wave per (query row, kv head); lane: two channels.  Splits in the order prefix, then the sequence's own; lane i keeps
-// the pairs of splits i, i + 64, ... for maximum and sum.
-__global__ __launch_bounds__(256) void rows_merge_kernel(RowsArgs a) {
-  const int rr = 4 * (int)blockIdx.x + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), head = blockIdx.y, lane = threadIdx.x & 63;
-  if (rr >= a.rows) return;
-  int si = 0;
-  while (si + 1 < a.n_seqs && rr >= a.s[si + 1].row0) ++si;
-  const RowsSeq& me = a.s[si];
-  const int r = rr - me.row0, rows = me.ncols * a.grp;
-  const float2* mlp = a.ml_prefix + ((size_t)head * a.rows + rr) * a.prefix_splits;
+// Joins the partial results of a row: PARTS waves per row (4 or 1) take every PARTS-th split each, lane two channels, and
+// add them in order; then the parts in order.  Bound by latency: the pairs and kMergeAhead outputs are requested at once, the
+// outputs through buffer descriptors, of no length past the end of the part: what lies there reads as 0 without a branch.
+constexpr int kMergeAhead = 16;
+template <int PARTS>
+__device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head) {
+  __shared__ float2 joined[4][64];
+  const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int rr = block * (4 / PARTS) + wv / PARTS, part = wv % PARTS;
+  if (rr >= a.rows) return;  // with four parts no wave of the workgroup is left
+  const int si = which_of(a.row0, rr);
+  struct {
+    uint16_t* O;
+    int ncols, row0, splits;
+    uint32_t part0;
+  } const me = {a.O[si], a.ncols[si], a.row0[si], a.splits[si], a.part0[si]};
+  const int r = rr - me.row0, rows = me.ncols * a.grp, ps = a.prefix_splits, n = ps + me.splits;
+  const float2* mlp = a.ml_prefix + ((size_t)head * a.rows + rr) * ps;
   const float2* mlt = a.ml_tail + me.part0 + ((size_t)head * rows + r) * me.splits;
-  const int n = a.prefix_splits + me.splits;
-  auto pair = [&](int i) { return i < a.prefix_splits ? mlp[i] : mlt[i - a.prefix_splits]; };
-  float M = kLowest;
-  for (int i = lane; i < n; i += 64) M = fmaxf(M, pair(i).x);
+  auto pair = [&](int i) { return i < ps ? mlp[i] : mlt[i - ps]; };
+  const char* op = reinterpret_cast<const char*>(a.out_prefix + ((size_t)head * a.rows + rr) * 128);
+  const char* ot = reinterpret_cast<const char*>(a.out_tail + (me.part0 + (size_t)head * rows + r) * 128);
+  const size_t sp = (size_t)a.g.n_kv_heads * a.rows * 512, st = (size_t)a.g.n_kv_heads * rows * 512;
+  const int cnt = (n - part + PARTS - 1) / PARTS;  // splits of this part: part, part + PARTS, ...
+  float2 o[kMergeAhead];
+  auto request = [&](int q0) {
+#pragma unroll
+    for (int q = 0; q < kMergeAhead; ++q) {
+      const int s = __builtin_amdgcn_readfirstlane(part + PARTS * (q0 + q));
+      const char* at = s < ps ? op + s * sp : ot + (s - ps) * st;
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, q0 + q < cnt ? 512 : 0, kRawBufferFlags);
+      const auto two = __builtin_amdgcn_raw_buffer_load_b64(rs, 8 * lane, 0, 0);
+      o[q] = make_float2(__uint_as_float(two[0]), __uint_as_float(two[1]));
+    }
+  };
+  float2 own = make_float2(kLowest, 0.f), all = make_float2(kLowest, 0.f);  // pairs of split `lane` of the part, of the row
+  if (lane < cnt) own = pair(part + PARTS * lane);
+  if (lane < n) all = pair(lane);
+  request(0);
+  float M = all.x;
+  for (int i = lane + 64; i < n; i += 64) M = fmaxf(M, pair(i).x);
   M = wave_max(M);
-  float den = 0.f;
-  float2 num = make_float2(0.f, 0.f);
-  const float2* op = reinterpret_cast<const float2*>(a.out_prefix) + ((size_t)head * a.rows + rr) * 64 + lane;
-  const float2* ot = reinterpret_cast<const float2*>(a.out_tail) + (me.part0 + (size_t)head * rows + r) * 64 + lane;
-  const size_t sp = (size_t)a.g.n_kv_heads * a.rows * 64, st = (size_t)a.g.n_kv_heads * rows * 64;
-  for (int i0 = 0; i0 < n; i0 += 64) {
-    float w = 0.f;
-    if (i0 + lane < n) {
-      const float2 ml = pair(i0 + lane);
-      w = __builtin_amdgcn_exp2f(ml.x - M);
-      den += w * ml.y;
-    }
-    for (int i = 0; i < min(64, n - i0); ++i) {
-      const int s = i0 + i;
-      const float2 o = s < a.prefix_splits ? op[s * sp] : ot[(s - a.prefix_splits) * st];
-      const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), i));
-      num.x += ws * o.x;
-      num.y += ws * o.y;
-    }
+  float den = __builtin_amdgcn_exp2f(all.x - M) * all.y;
+  for (int i = lane + 64; i < n; i += 64) {
+    const float2 p = pair(i);
+    den += __builtin_amdgcn_exp2f(p.x - M) * p.y;
   }
   den = wave_sum(den);
+  float2 num = make_float2(0.f, 0.f);
+  for (int q0 = 0; q0 < cnt; q0 += kMergeAhead) {
+    if (q0 > 0) {
+      if ((q0 & 63) == 0) own = q0 + lane < cnt ? pair(part + PARTS * (q0 + lane)) : make_float2(kLowest, 0.f);
+      request(q0);
+    }
+    const int w = __float_as_int(__builtin_amdgcn_exp2f(own.x - M));
+#pragma unroll
+    for (int q = 0; q < kMergeAhead; ++q) {
+      const float ws = __int_as_float(__builtin_amdgcn_readlane(w, (q0 & 63) + q));
+      num.x += ws * o[q].x;
+      num.y += ws * o[q].y;
+    }
+  }
+  if constexpr (PARTS > 1) {
+    joined[part][lane] = num;
+    __syncthreads();
+    if (part != 0) return;
+#pragma unroll
+    for (int p = 1; p < PARTS; ++p) {
+      num.x += joined[p][lane].x;
+      num.y += joined[p][lane].y;
+    }
+  }
   const int c = r / a.grp, gi = r - c * a.grp;
   uint32_t* out = reinterpret_cast<uint32_t*>(me.O + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128) + lane;
   *out = (uint32_t)f32_to_bf16(num.x / den) | ((uint32_t)f32_to_bf16(num.y / den) << 16);
 }
 
-// Weights of 256 positions of a kv head: every row's maximum and sum first (a wave per row), then a thread per position.
-__global__ __launch_bounds__(256) void rows_weights_kernel(RowsArgs a, const float* in, float* out, int64_t ld) {
-  extern __shared__ float2 row_ml[];
-  const RowsSeq& me = a.s[0];
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, head = blockIdx.y, rows = a.rows, n = me.splits;
-  for (int r = wv; r < rows; r += 4) {
-    const float2* ml = a.ml_tail + ((size_t)head * rows + r) * n;
-    float M = kLowest, L = 0.f;
-    for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[i].x);
-    M = wave_max(M);
-    for (int i = lane; i < n; i += 64) L += __builtin_amdgcn_exp2f(ml[i].x - M) * ml[i].y;
-    L = wave_sum(L);
-    if (lane == 0) row_ml[r] = make_float2(M, 1.f / L);
+template <int PARTS>
+__global__ __launch_bounds__(256) void rows_merge_kernel(RowsArgs a) { merge_row<PARTS>(a, blockIdx.x, blockIdx.y); }
+
+// Weights of 256 positions of a kv head: every row's maximum and sum first (four rows of a wave at a time), then a thread
+// per position, eight rows requested at once.
+constexpr int kWeightsRows = 16 * 48;  // most query rows of a kv head
+__device__ __forceinline__ void add_weights(const RowsArgs& a, int block, int head, const float* in, float* out, int64_t ld) {
+  __shared__ float2 row_ml[kWeightsRows];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), rows = a.rows, ps = a.prefix_splits, n = ps + a.splits[0];
+  const int pos = block * 256 + tid;
+  const bool there = pos < a.len[0] + a.n_new[0];
+  const int64_t at = (int64_t)head * ld + pos;
+  const float before = there && in && pos < a.len[0] ? in[at] : 0.f;
+  for (int r0 = 4 * wv; r0 < rows; r0 += 16) {
+    float2 p[4];
+    float M[4], L[4];
+    auto pair = [&](int k, int i) {  // split i of row r0 + k, those of the prefix first
+      const size_t row = (size_t)head * rows + min(r0 + k, rows - 1);
+      return i < ps ? a.ml_prefix[row * ps + i] : a.ml_tail[row * a.splits[0] + i - ps];
+    };
+#pragma unroll
+    for (int k = 0; k < 4; ++k) p[k] = lane < n ? pair(k, lane) : make_float2(kLowest, 0.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) M[k] = p[k].x;
+    for (int i = lane + 64; i < n; i += 64) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) M[k] = fmaxf(M[k], pair(k, i).x);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      M[k] = wave_max(M[k]);
+      L[k] = __builtin_amdgcn_exp2f(p[k].x - M[k]) * p[k].y;
+    }
+    for (int i = lane + 64; i < n; i += 64) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 q = pair(k, i);
+        L[k] += __builtin_amdgcn_exp2f(q.x - M[k]) * q.y;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      L[k] = wave_sum(L[k]);
+      if (lane == 0 && r0 + k < rows) row_ml[r0 + k] = make_float2(M[k], 1.f / L[k]);
+    }
   }
   __syncthreads();
-  const int pos = (int)blockIdx.x * 256 + tid;
-  if (pos >= me.len + me.n_new) return;
+  if (!there) return;
   const float* x = a.score + (size_t)head * rows * a.score_ld + pos;
   float w = 0.f;
-  for (int r = 0; r < rows; ++r) w += __builtin_amdgcn_exp2f(x[(size_t)r * a.score_ld] - row_ml[r].x) * row_ml[r].y;
-  const int64_t at = (int64_t)head * ld + pos;
-  out[at] = (in && pos < me.len ? in[at] : 0.f) + w;
+  for (int r0 = 0; r0 < rows; r0 += 8) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = x[(size_t)min(r0 + k, rows - 1) * a.score_ld];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float2 ml = row_ml[min(r0 + k, rows - 1)];
+      w += r0 + k < rows ? __builtin_amdgcn_exp2f(v[k] - ml.x) * ml.y : 0.f;
+    }
+  }
+  out[at] = before + w;
+}
+
+// both in one launch: neither needs the other
+template <int PARTS>
+__global__ __launch_bounds__(256) void rows_merge_weights_kernel(RowsArgs a, int merge_blocks, const float* in, float* out, int64_t ld) {
+  if ((int)blockIdx.x < merge_blocks) merge_row<PARTS>(a, blockIdx.x, blockIdx.y);
+  else add_weights(a, (int)blockIdx.x - merge_blocks, blockIdx.y, in, out, ld);
 }
 
 // ---- host ---------------------------------------------------------------------------------------
+constexpr int kPrefixItems = 256;
 constexpr int kTailRun = 2;  // pages of a run behind the prefix: fixed, so that a sequence's values do not depend on its length
 
 struct RowsPlan {
   RowsArgs a;
-  int nt, items;
+  int tiles;          // of 16 query rows of a workgroup in the prefix's launch
+  int items, prefix_items;
   size_t bytes;
 };
 
 static int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 
-// What a call will launch and need; the pointers of a.s[] are left to the caller.
+// What a call will launch and need; Q, Knew, Vnew and O are left to the caller.
 static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int prefix_len, const int32_t* ncols, int n_q_heads,
                      const int32_t* n_new, bool weights, int num_cu, RowsPlan* out) {
   if (!kv || n_seqs < 1 || n_seqs > kRowsSeqs || !seqs || !ncols || !n_new || prefix_len < 0) return CAS_EINVAL;
@@ -114,48 +201,52 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   a.grp_inv = (65536u + (uint32_t)a.grp - 1u) / (uint32_t)a.grp;
   a.scale2 = (float)(1.4426950408889634 * 0.08838834764831845);
   a.n_seqs = n_seqs;
-  a.prefix_pages = prefix_len / 64;
+  // a sequence on its own: its whole pages are the prefix
+  a.prefix_pages = (weights && seqs[0] >= 0 && seqs[0] < kv->desc.max_seqs ? kv->h_len[seqs[0]] : prefix_len) / 64;
   a.tail_run = kTailRun;
   int64_t rows = 0, parts = 0, items = 0;
   for (int i = 0; i < n_seqs; ++i) {
-    RowsSeq& s = a.s[i];
     if (seqs[i] < 0 || seqs[i] >= kv->desc.max_seqs) return CAS_EINVAL;
     for (int k = 0; k < i; ++k)
       if (seqs[k] == seqs[i]) return CAS_EINVAL;
     if (ncols[i] < 1 || ncols[i] > 16 || n_new[i] < ncols[i] || n_new[i] > 64) return CAS_EINVAL;
-    s.seq = seqs[i]; s.len = kv->h_len[seqs[i]]; s.ncols = ncols[i]; s.n_new = n_new[i];
-    if (prefix_len > s.len) return CAS_EINVAL;
-    const int64_t pages = ((int64_t)s.len + s.n_new + 63) / 64;
+    a.seq[i] = seqs[i]; a.len[i] = kv->h_len[seqs[i]]; a.ncols[i] = ncols[i]; a.n_new[i] = n_new[i];
+    if (prefix_len > a.len[i]) return CAS_EINVAL;
+    const int64_t pages = ((int64_t)a.len[i] + a.n_new[i] + 63) / 64;
     if (pages > g.max_pages_per_seq) return CAS_ENOMEM;
-    s.splits = (int)(pages - a.prefix_pages + kTailRun - 1) / kTailRun;
-    s.row0 = (int)rows;
-    rows += s.ncols * a.grp;
+    a.splits[i] = (int)(pages - a.prefix_pages + kTailRun - 1) / kTailRun;
+    a.row0[i] = (int)rows;
+    rows += ncols[i] * a.grp;
   }
   a.rows = (int)rows;
-  p.nt = 1;
   if (a.prefix_pages > 0) {
-    a.prefix_run = 2;
+    // one workgroup per CU takes the rows of a tile count; as many runs as that gives, of two pages a step
+    const int runs = std::max(1, kPrefixItems / g.n_kv_heads);
+    a.prefix_run = ((a.prefix_pages + runs - 1) / runs + 1) / 2 * 2;
     a.prefix_splits = (a.prefix_pages + a.prefix_run - 1) / a.prefix_run;
-    a.prefix_items = a.prefix_splits * ((a.rows + 16 * p.nt - 1) / (16 * p.nt));
+    p.tiles = a.rows <= 32 ? 2 : a.rows <= 64 ? 4 : a.rows <= 128 ? 8 : 16;
+    p.prefix_items = a.prefix_splits * ((a.rows + 16 * p.tiles - 1) / (16 * p.tiles));
   }
   for (int i = 0; i < n_seqs; ++i) {
-    RowsSeq& s = a.s[i];
-    const int r = s.ncols * a.grp;
-    s.item0 = (int)items;
-    s.part0 = (uint32_t)parts;
-    items += (int64_t)s.splits * ((r + 16 * p.nt - 1) / (16 * p.nt));
-    parts += (int64_t)s.splits * g.n_kv_heads * r;
+    const int r = ncols[i] * a.grp;
+    a.item0[i] = (int)items;
+    a.part0[i] = (uint32_t)parts;
+    items += (int64_t)a.splits[i] * ((r + 15) / 16);
+    parts += (int64_t)a.splits[i] * g.n_kv_heads * r;
+    if (items > 0x7FFFFFFF || parts > 0xFFFFFFFFll) return CAS_ENOTSUP;
   }
+  for (int i = n_seqs; i < kRowsSeqs; ++i) a.row0[i] = a.item0[i] = 0x7FFFFFFF;
   const int64_t first = (int64_t)a.prefix_splits * g.n_kv_heads * a.rows;
-  if (parts > 0xFFFFFFFFll || (items + a.prefix_items) * g.n_kv_heads > 0x7FFFFFFF) return CAS_ENOTSUP;
-  p.items = (int)items + a.prefix_items;
+  if (items * g.n_kv_heads > 0x7FFFFFFF ||
+      (int64_t)p.prefix_items * g.n_kv_heads > 0x7FFFFFFF) return CAS_ENOTSUP;
+  p.items = (int)items;
   // workspace: outputs, pairs, and the exponents of the rows
   int64_t off = up256((first + parts) * 512);
   const int64_t off_ml = off;
   off += up256((first + parts) * 8);
   const int64_t off_score = off;
   if (weights) {
-    a.score_ld = ((int64_t)a.s[0].len + a.s[0].n_new + 63) / 64 * 64;
+    a.score_ld = ((int64_t)a.len[0] + a.n_new[0] + 63) / 64 * 64;
     off += up256(a.score_ld * g.n_kv_heads * a.rows * 4);
   }
   p.bytes = (size_t)off;
@@ -175,7 +266,13 @@ static void place(RowsArgs& a, void* ws) {  // offsets into the workspace become
   if (a.score) at(a.score);
 }
 
-static int launch_rows(cas_ctx* ctx, cas_kv* kv, RowsPlan& p, int layer, int full) {
+// weights: where the sums of a call for one sequence go
+struct RowsWeights {
+  const float* in;
+  float* out;
+  int64_t ld;
+};
+static int launch_rows(cas_ctx* ctx, cas_kv* kv, RowsPlan& p, int layer, int full, const RowsWeights* weights = nullptr) {
   if (!ctx->d_ws || !aligned256(ctx->d_ws) || p.bytes > ctx->ws_bytes) return ctx->d_ws && !aligned256(ctx->d_ws) ? CAS_EINVAL : CAS_ENOMEM;
   RowsArgs& a = p.a;
   place(a, ctx->d_ws);
@@ -183,10 +280,24 @@ static int launch_rows(cas_ctx* ctx, cas_kv* kv, RowsPlan& p, int layer, int ful
   a.verif_pool = (const uint32_t*)kv->d_verif;
   a.table = kv->d_page_table;
   a.layer = layer;
-  const int rc = a.g.mx ? (full ? launch_rows_partial<true, true>(ctx, a, p.items) : launch_rows_partial<false, true>(ctx, a, p.items))
-                        : (full ? launch_rows_partial<true, false>(ctx, a, p.items) : launch_rows_partial<false, false>(ctx, a, p.items));
+  int rc = CAS_OK;
+  if (p.prefix_items > 0)
+    rc = a.g.mx ? (full ? launch_prefix_partial<true, true>(ctx, a, p.tiles, p.prefix_items) : launch_prefix_partial<false, true>(ctx, a, p.tiles, p.prefix_items))
+                : (full ? launch_prefix_partial<true, false>(ctx, a, p.tiles, p.prefix_items) : launch_prefix_partial<false, false>(ctx, a, p.tiles, p.prefix_items));
+  if (rc == CAS_OK)
+    rc = a.g.mx ? (full ? launch_rows_partial<true, true>(ctx, a, p.items) : launch_rows_partial<false, true>(ctx, a, p.items))
+                : (full ? launch_rows_partial<true, false>(ctx, a, p.items) : launch_rows_partial<false, false>(ctx, a, p.items));
   if (rc != CAS_OK) return rc;
-  hipLaunchKernelGGL(rows_merge_kernel, dim3((a.rows + 3) / 4, a.g.n_kv_heads), dim3(256), 0, ctx->stream, a);
+  int most = 0;  // splits of a row: one wave can have 16 outputs in flight, so longer rows are shared by four
+  for (int i = 0; i < a.n_seqs; ++i) most = std::max(most, a.prefix_splits + a.splits[i]);
+  const int parts = most <= kMergeAhead ? 1 : 4, blocks = (a.rows * parts + 3) / 4;
+  if (weights) {
+    const dim3 grid(blocks + (a.len[0] + a.n_new[0] + 255) / 256, a.g.n_kv_heads);
+    hipLaunchKernelGGL(parts == 1 ? rows_merge_weights_kernel<1> : rows_merge_weights_kernel<4>, grid, dim3(256), 0, ctx->stream, a, blocks,
+                       weights->in, weights->out, weights->ld);
+  } else {
+    hipLaunchKernelGGL(parts == 1 ? rows_merge_kernel<1> : rows_merge_kernel<4>, dim3(blocks, a.g.n_kv_heads), dim3(256), 0, ctx->stream, a);
+  }
   CAS_HIP(ctx, hipGetLastError());
   return CAS_OK;
 }
@@ -204,10 +315,9 @@ int cas_attention_shared(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const 
   const int rc = cas::plan_rows(kv, n_seqs, h_seqs, prefix_len, h_ncols, n_q_heads, h_n_new, false, ctx->num_cu, &p);
   if (rc != CAS_OK) return rc;
   for (int i = 0; i < n_seqs; ++i) {
-    cas::RowsSeq& s = p.a.s[i];
-    s.Q = h_d_Q[i]; s.Knew = h_d_Knew[i]; s.Vnew = h_d_Vnew[i]; s.O = h_d_O[i];
-    if (!s.Q || !s.Knew || !s.Vnew || !s.O || !cas::aligned256(s.Q) || !cas::aligned256(s.Knew) || !cas::aligned256(s.Vnew) || !cas::aligned256(s.O))
-      return CAS_EINVAL;
+    p.a.Q[i] = h_d_Q[i]; p.a.Knew[i] = h_d_Knew[i]; p.a.Vnew[i] = h_d_Vnew[i]; p.a.O[i] = h_d_O[i];
+    for (const void* d : {(const void*)h_d_Q[i], (const void*)h_d_Knew[i], (const void*)h_d_Vnew[i], (const void*)h_d_O[i]})
+      if (!d || !cas::aligned256(d)) return CAS_EINVAL;
   }
   if (!cas::on_device(ctx)) return CAS_EINVAL;
   return cas::launch_rows(ctx, kv, p, layer, full);
@@ -224,20 +334,15 @@ int cas_attention_weights(cas_ctx* ctx, cas_kv* kv, int layer, int seq, int full
                           float* d_score_out, int64_t ld) {
   if (!ctx || !kv || layer < 0 || layer >= kv->desc.n_layers || !d_Q || !d_Knew || !d_Vnew || !d_O || !d_score_out) return CAS_EINVAL;
   cas::RowsPlan p;
-  int rc = cas::plan_rows(kv, 1, &seq, 0, &ncols, n_q_heads, &n_new, true, ctx->num_cu, &p);
+  const int rc = cas::plan_rows(kv, 1, &seq, 0, &ncols, n_q_heads, &n_new, true, ctx->num_cu, &p);
   if (rc != CAS_OK) return rc;
-  cas::RowsSeq& s = p.a.s[0];
-  const int total = s.len + n_new;
+  const int total = p.a.len[0] + n_new;
   if (ld < total) return CAS_EINVAL;
   if (!cas::aligned256(d_Q) || !cas::aligned256(d_Knew) || !cas::aligned256(d_Vnew) || !cas::aligned256(d_O)) return CAS_EINVAL;
   if (!cas::on_device(ctx)) return CAS_EINVAL;
-  s.Q = d_Q; s.Knew = d_Knew; s.Vnew = d_Vnew; s.O = d_O;
-  rc = cas::launch_rows(ctx, kv, p, layer, full);
-  if (rc != CAS_OK) return rc;
-  hipLaunchKernelGGL(cas::rows_weights_kernel, dim3((total + 255) / 256, p.a.g.n_kv_heads), dim3(256), sizeof(float2) * p.a.rows,
-                     ctx->stream, p.a, d_score_in, d_score_out, ld);
-  CAS_HIP(ctx, hipGetLastError());
-  return CAS_OK;
+  p.a.Q[0] = d_Q; p.a.Knew[0] = d_Knew; p.a.Vnew[0] = d_Vnew; p.a.O[0] = d_O;
+  const cas::RowsWeights w{d_score_in, d_score_out, ld};
+  return cas::launch_rows(ctx, kv, p, layer, full, &w);
 }
 
 size_t cas_attention_weights_bytes(const cas_kv* kv, int seq, int ncols, int n_q_heads, int n_new) {

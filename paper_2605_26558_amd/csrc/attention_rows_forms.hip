@@ -3,4 +3,5 @@
 
 namespace cas {
 template int launch_rows_partial<true, false>(cas_ctx*, const RowsArgs&, int);
+template int launch_prefix_partial<true, false>(cas_ctx*, const RowsArgs&, int, int);
 }  // namespace cas

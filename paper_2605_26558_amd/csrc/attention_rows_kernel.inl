@@ -14,17 +14,9 @@ typedef unsigned int rows_u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kRowsSeqs = 32;      // sequences of a launch
 constexpr float kLowest = -3.402823466e38f;
 
-struct RowsSeq {
-  const uint16_t* Q;
-  const uint16_t* Knew;
-  const uint16_t* Vnew;
-  uint16_t* O;
-  int seq, len, n_new, ncols;
-  int row0;       // query rows (columns x group) of the sequences before
-  int splits;     // runs of pages behind the prefix
-  int item0;      // work items behind the prefix, of the sequences before
-  uint32_t part0; // partial results (row, run, kv head) behind the prefix, of the sequences before
-};
+// Kernel arguments lie in host memory: what a workgroup looks for in them is found by scalar loads at fixed places (which_of,
+// query_of), since a loop of dependent loads, or a load per lane, crosses the bus every time (11 of the 27 us that 16
+// sequences took over a prefix of 8192 positions).
 struct RowsArgs {
   KvGeom g;
   const uint32_t* spec_pool;
@@ -34,7 +26,7 @@ struct RowsArgs {
   uint32_t grp_inv;          // row / grp = row * grp_inv >> 16
   float scale2;              // log2(e) / sqrt(128): scores are kept as exponents of two
   int n_seqs, rows;          // rows: of all sequences
-  int prefix_pages, prefix_run, prefix_splits, prefix_items, tail_run;
+  int prefix_pages, prefix_run, prefix_splits, tail_run;
   // partial results: 128 outputs each, [split][kv head][row] of the prefix, then the same sequence by sequence; and the
   // pairs (maximum, sum) in the same two regions as [kv head][row][split]
   float* out_prefix;
@@ -43,8 +35,25 @@ struct RowsArgs {
   float2* ml_tail;
   float* score;              // NULL or [kv head][row][score_ld]: exponents of every position behind the prefix
   int64_t score_ld;
-  RowsSeq s[kRowsSeqs];
+  // the sequences
+  int row0[kRowsSeqs];       // query rows (columns x group) of the sequences before; the largest number behind the last
+  int item0[kRowsSeqs];      // work items behind the prefix, of the sequences before; as above
+  const uint16_t* Q[kRowsSeqs];
+  const uint16_t* Knew[kRowsSeqs];
+  const uint16_t* Vnew[kRowsSeqs];
+  uint16_t* O[kRowsSeqs];
+  int seq[kRowsSeqs], len[kRowsSeqs], n_new[kRowsSeqs], ncols[kRowsSeqs];
+  int splits[kRowsSeqs];     // runs of pages behind the prefix
+  uint32_t part0[kRowsSeqs]; // partial results (row, run, kv head) behind the prefix, of the sequences before
 };
+
+// the sequence whose share of first[] holds n
+__device__ __forceinline__ int which_of(const int (&first)[kRowsSeqs], int n) {
+  int s = 0;
+#pragma unroll
+  for (int i = 1; i < kRowsSeqs; ++i) s += n >= first[i] ? 1 : 0;
+  return s;
+}
 
 // K and V of a wave's 16 tokens in LDS as in attention_kernel.inl: [1 + 32 positions][64 values], for K the four words of a
 // token at one position side by side, for V the tokens of a word; row 0 takes what lanes without a value left write.
@@ -65,8 +74,36 @@ __device__ __forceinline__ float over_groups_sum(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-__device__ __forceinline__ uint32_t rows_low(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05040100u); }
-__device__ __forceinline__ uint32_t rows_high(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); }
+// Product kk of a page takes 8 positions of the four words; lane group mq takes two of them, two apart, so that the 32 lanes
+// which the LDS serves at once read places that follow one another (its 64 banks hold two positions).
+__device__ __forceinline__ int k_position(int kk, int mq) { return 8 * kk + (mq & 1) + 4 * (mq >> 1); }
+__device__ __forceinline__ rows_bf16x8 k_fragment(const uint16_t* slab, int kk, int mi, int mq) {
+  const uint16_t* src = slab + (1 + k_position(kk, mq)) * kRowsPos + 4 * mi;
+  const uint2 k0 = *reinterpret_cast<const uint2*>(src), k1 = *reinterpret_cast<const uint2*>(src + 2 * kRowsPos);
+  return __builtin_bit_cast(rows_bf16x8, rows_u32x4{k0.x, k0.y, k1.x, k1.y});
+}
+// The queries go through LDS, [row][position][word]: a load per lane of its own row takes an address unit some 20 ns, and a
+// wave needs 16 of them (16 waves: 5 us).  Sixteen threads to a row, two positions of the four words each; rows that are
+// not there are zeros.
+constexpr int kQueryPitch = 136;
+struct QueryPart {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const uint16_t* row, int i) {  // row = NULL: zeros
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = row ? *reinterpret_cast<const uint32_t*>(row + 32 * k + 2 * i) : 0u;
+  }
+  __device__ __forceinline__ void store(uint16_t* row, int i) const {
+    auto low = [](uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05040100u); };
+    auto high = [](uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); };
+    *reinterpret_cast<uint4*>(row + 8 * i) = make_uint4(low(w[0], w[1]), low(w[2], w[3]), high(w[0], w[1]), high(w[2], w[3]));
+  }
+};
+// the values of a row that product kk takes
+__device__ __forceinline__ rows_bf16x8 q_fragment(const uint16_t* row, int kk, int mq) {
+  const uint16_t* src = row + 4 * k_position(kk, mq);
+  const uint2 q0 = *reinterpret_cast<const uint2*>(src), q1 = *reinterpret_cast<const uint2*>(src + 8);
+  return __builtin_bit_cast(rows_bf16x8, rows_u32x4{q0.x, q0.y, q1.x, q1.y});
+}
 
 // A workgroup: one kv head, one run of pages, up to 16 NT query rows.  Wave w owns tokens 16 w .. 16 w + 15 of every page,
 // from their streams to its own running maxima, sums and outputs: the page loop has no barrier, and the four waves' results
@@ -88,54 +125,59 @@ __global__ __launch_bounds__(256, NT > 1 ? 2 : FULL ? 3 : 4) void attn_rows_kern
   uint16_t* const vcol = slab + kRowsPos + j * 16 + (r & 15);
 
   // ---- what this workgroup works on (uniform)
-  const bool prefix = item < a.prefix_items;
-  int si = 0, split, row_base, rows;
-  if (prefix) {
-    const int tiles = (a.rows + 16 * NT - 1) / (16 * NT);
-    split = item / tiles;
-    row_base = (item - split * tiles) * 16 * NT;
-    rows = a.rows;
-  } else {
-    item -= a.prefix_items;
-    while (si + 1 < a.n_seqs && item >= a.s[si + 1].item0) ++si;
-    item -= a.s[si].item0;
-    rows = a.s[si].ncols * a.grp;
-    const int tiles = (rows + 16 * NT - 1) / (16 * NT);
-    split = item / tiles;
-    row_base = (item - split * tiles) * 16 * NT;
-  }
-  const RowsSeq& me = a.s[si];
-  const int len = prefix ? a.prefix_pages * 64 : me.len, total = prefix ? len : me.len + me.n_new;
-  const int pg0 = prefix ? split * a.prefix_run : a.prefix_pages + split * a.tail_run;
-  const int pg1 = min(pg0 + (prefix ? a.prefix_run : a.tail_run), prefix ? a.prefix_pages : (total + 63) / 64);
-  const int32_t* page_row = a.table + (size_t)me.seq * g.max_pages_per_seq;
+  const int si = which_of(a.item0, item);
+  struct {
+    const uint16_t *Q, *Knew, *Vnew;
+    int len, n_new, ncols, splits, item0;
+    uint32_t part0;
+  } const me = {a.Q[si], a.Knew[si], a.Vnew[si], a.len[si], a.n_new[si], a.ncols[si], a.splits[si], a.item0[si], a.part0[si]};
+  item -= me.item0;
+  const int rows = me.ncols * a.grp, blocks = (rows + 16 * NT - 1) / (16 * NT);
+  const int split = item / blocks, row_base = (item - split * blocks) * 16 * NT;
+  const int len = me.len, total = me.len + me.n_new;
+  const int pg0 = a.prefix_pages + split * a.tail_run, pg1 = min(pg0 + a.tail_run, (total + 63) / 64);
+  const int32_t* page_row = a.table + (size_t)a.seq[si] * g.max_pages_per_seq;
 
-  // ---- queries: fragment kk of a lane holds positions 8 kk + 2 mq, + 1 of the four words of its row
+  // Pool pages two pages ahead, bitmap words one page ahead: a page's own round trip is that of its windows alone.  The pools
+  // are touched only for pages that hold committed positions.
+  auto page_of = [&](int pg) { return pg < pg1 && pg * 64 < len ? min(max(page_row[pg], 0), g.n_pages - 1) : 0; };
+  auto tile_of = [&](int page) { return (((size_t)a.layer * g.n_pages + page) * 2) * g.n_kv_heads + head; };
+  uint32_t next_k = 0, next_v = 0, next_ek = 0, next_ev = 0;
+  auto request_masks = [&](int pg, int page) {
+    next_k = next_v = next_ek = next_ev = 0;
+    if (pg < pg1 && pg * 64 + r < len) {
+      const uint32_t* ks = a.spec_pool + tile_of(page) * g.tile_spec_words;
+      const uint32_t* vs = ks + (size_t)g.n_kv_heads * g.tile_spec_words;
+      next_k = ks[r * 4 + j];
+      next_v = vs[r * 4 + j];
+      if constexpr (MX) {
+        next_ek = ks[64 * 4 + r];
+        next_ev = vs[64 * 4 + r];
+      }
+    }
+  };
+  int page_next = page_of(pg0), page_after = page_of(pg0 + 1);
+  request_masks(pg0, page_next);
+
+  // ---- queries
   rows_bf16x8 q[NT][4];
   int seen[NT];  // last position that the row sees
+  static_assert(16 * NT * kQueryPitch <= 4 * kRowsSlab, "");
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    int rr = row_base + nt * 16 + mi;
-    const bool there = rr < rows;
-    int at = si;
-    if (prefix) {  // a row of all sequences
-      for (int s = 1; s < a.n_seqs; ++s) at = rr >= a.s[s].row0 ? s : at;
-      rr -= a.s[at].row0;
-    }
-    const int c = (int)((uint32_t)rr * a.grp_inv >> 16), gi = rr - c * a.grp;
-    seen[nt] = prefix ? 0x7FFFFFFF : total - me.ncols + c;
-    const uint16_t* src = a.s[at].Q + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128 + 2 * mq;
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      uint32_t w[4] = {0, 0, 0, 0};
-      if (there) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint32_t*>(src + 32 * i + 8 * kk);
-      }
-      q[nt][kk] = __builtin_bit_cast(rows_bf16x8, rows_u32x4{rows_low(w[0], w[1]), rows_low(w[2], w[3]), rows_high(w[0], w[1]),
-                                                              rows_high(w[2], w[3])});
-    }
+    const int rr = row_base + nt * 16 + (tid >> 4), c = (int)((uint32_t)rr * a.grp_inv >> 16), gi = rr - c * a.grp;
+    QueryPart part;
+    part.load(rr < rows ? me.Q + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128 : nullptr, tid & 15);
+    part.store(tile + (nt * 16 + (tid >> 4)) * kQueryPitch, tid & 15);
+    seen[nt] = total - me.ncols + (int)((uint32_t)(row_base + nt * 16 + mi) * a.grp_inv >> 16);
   }
+  __syncthreads();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) q[nt][kk] = q_fragment(tile + (nt * 16 + mi) * kQueryPitch, kk, mq);
+  }
+  __syncthreads();  // the tile is free
 
   rows_f32x4 o[NT][8];
   float m[NT], l[NT];
@@ -171,33 +213,26 @@ __global__ __launch_bounds__(256, NT > 1 ? 2 : FULL ? 3 : 4) void attn_rows_kern
   for (int pg = pg0; pg < pg1; ++pg) {
     const int tok0 = pg * 64, pos = tok0 + r;
     const bool has_live = tok0 < len, live = pos < len, fresh = !live && pos < total;
-    // ---- streams of the thread's word of K and V.  The pools are touched only for pages that hold committed positions
-    uint32_t mk = 0, mv = 0;
+    // ---- streams of the thread's word of K and V
+    const uint32_t mk = taken(next_k), mv = taken(next_v);
     int ek = 0, ev = 0;
+    if constexpr (MX) {
+      ek = (int)((taken(next_ek) >> (8 * j)) & 0xFFu);
+      ev = (int)((taken(next_ev) >> (8 * j)) & 0xFFu);
+    }
+    const size_t tk = tile_of(page_next), tv = tk + g.n_kv_heads;
+    page_next = page_after;
+    page_after = page_of(pg + 2);
     WordWindows<T, FULL, MX> wk, wvw;
-    const uint32_t *ks = nullptr, *vs = nullptr, *kvf = nullptr, *vvf = nullptr;
-    auto load = [&](WordWindows<T, FULL, MX>& w, uint32_t mask, const uint32_t* sp, const uint32_t* vf) {
+    auto load = [&](WordWindows<T, FULL, MX>& w, uint32_t mask, size_t t) {
       const uint32_t p = word_prefix(mask);
+      const uint32_t* sp = a.spec_pool + t * g.tile_spec_words;
+      const uint32_t* vf = a.verif_pool + t * g.tile_verif_words;
       if (has_live) w.load(p, 32u * j - p, sp + g.spec_off + r * g.sw, vf + r * g.lw, vf + 64 * g.lw + r * g.pw);
     };
-    if (has_live) {
-      const int page = min(max(page_row[pg], 0), g.n_pages - 1);
-      const size_t tk = (((size_t)a.layer * g.n_pages + page) * 2 + 0) * g.n_kv_heads + head, tv = tk + g.n_kv_heads;
-      ks = a.spec_pool + tk * g.tile_spec_words;
-      vs = a.spec_pool + tv * g.tile_spec_words;
-      kvf = a.verif_pool + tk * g.tile_verif_words;
-      vvf = a.verif_pool + tv * g.tile_verif_words;
-      if (live) {
-        mk = ks[r * 4 + j];
-        mv = vs[r * 4 + j];
-        if constexpr (MX) {
-          ek = (int)((ks[64 * 4 + r] >> (8 * j)) & 0xFFu);
-          ev = (int)((vs[64 * 4 + r] >> (8 * j)) & 0xFFu);
-        }
-      }
-    }
-    load(wk, mk, ks, kvf);
-    if constexpr (!FULL) load(wvw, mv, vs, vvf);
+    load(wk, mk, tk);
+    if constexpr (!FULL) load(wvw, mv, tv);
+    request_masks(pg + 1, page_next);
     // the exact form writes all channels of a page of committed tokens; otherwise what is not written has to read as 0
     const bool clear = !FULL || tok0 + 64 > len;
     auto clear_slab = [&]() {
@@ -212,7 +247,7 @@ __global__ __launch_bounds__(256, NT > 1 ? 2 : FULL ? 3 : 4) void attn_rows_kern
     if (fresh) copy_fresh(me.Knew, pos - me.len, kcol, [](uint16_t v) { return v; });
     wk.k.decode(mk, [&](int bp, uint16_t v) { kcol[bp * kRowsPos] = v; }, ek);
     if constexpr (FULL) wk.pr.decode(live ? ~mk : 0u, [&](int bp, uint16_t v) { kcol[bp * kRowsPos] = v; });
-    if constexpr (FULL) load(wvw, mv, vs, vvf);
+    if constexpr (FULL) load(wvw, mv, tv);
     ordered();
     // ---- exponents of the wave's 16 tokens: lane (mi, mq) holds tokens 4 mq + e of row mi
     rows_f32x4 x[NT];
@@ -220,9 +255,7 @@ __global__ __launch_bounds__(256, NT > 1 ? 2 : FULL ? 3 : 4) void attn_rows_kern
     for (int nt = 0; nt < NT; ++nt) x[nt] = rows_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
-      const uint16_t* src = slab + (1 + 8 * kk + 2 * mq) * kRowsPos + 4 * mi;
-      const uint2 k0 = *reinterpret_cast<const uint2*>(src), k1 = *reinterpret_cast<const uint2*>(src + kRowsPos);
-      const rows_bf16x8 kf = __builtin_bit_cast(rows_bf16x8, rows_u32x4{k0.x, k0.y, k1.x, k1.y});
+      const rows_bf16x8 kf = k_fragment(slab, kk, mi, mq);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) x[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[nt][kk], x[nt], 0, 0, 0);
     }
@@ -351,10 +384,8 @@ __global__ __launch_bounds__(256, NT > 1 ? 2 : FULL ? 3 : 4) void attn_rows_kern
     __syncthreads();
   }
   if (wv != 0) return;
-  const size_t first = prefix ? 0 : me.part0;
-  float* const out = (prefix ? a.out_prefix : a.out_tail) + (first + ((size_t)split * g.n_kv_heads + head) * rows) * 128;
-  float2* const ml = (prefix ? a.ml_prefix : a.ml_tail) + first;
-  const int splits = prefix ? a.prefix_splits : me.splits;
+  float* const out = a.out_tail + ((size_t)me.part0 + ((size_t)split * g.n_kv_heads + head) * rows) * 128;
+  float2* const ml = a.ml_tail + me.part0;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int rr = row_base + nt * 16 + mi;
@@ -362,10 +393,289 @@ __global__ __launch_bounds__(256, NT > 1 ? 2 : FULL ? 3 : 4) void attn_rows_kern
     rows_f32x4* const dst = reinterpret_cast<rows_f32x4*>(out + (size_t)rr * 128 + 32 * mq);
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) dst[ct] = o[nt][ct];
-    if (mq == 0) ml[((size_t)head * rows + rr) * splits + split] = make_float2(top[nt], sum[nt]);
+    if (mq == 0) ml[((size_t)head * rows + rr) * me.splits + split] = make_float2(top[nt], sum[nt]);
   }
 }
 
+// LDS writes at base + i * pitch bytes with the address in one operation (the compiler's code takes two)
+typedef __attribute__((address_space(3))) uint16_t lds_u16;
+__device__ __forceinline__ uint32_t lds_address(uint16_t* p) { return (uint32_t)(uintptr_t)(lds_u16*)p; }
+__device__ __forceinline__ void lds_write(uint32_t base, int i, int pitch, uint16_t v) {
+  uint32_t at;
+  asm("v_mad_i32_i24 %0, %1, %2, %3" : "=v"(at) : "v"(i), "s"(pitch), "v"(base));
+  *(lds_u16*)(uintptr_t)at = v;
+}
+
+// The whole pages of a prefix, for up to 16 RT query rows of all sequences.  Sixteen waves, the most that a CU holds at 128
+// registers, take two pages a step: each decodes 16 tokens of K or of V of one of them into a tile that all read, and forms
+// the products of 16 rows with both pages (RT = 16), with one (8), or with half (4) or a quarter (2) of one.  There are two
+// sets of tiles: a step's products, the decode of the next and the loads of the one after it are between the same two
+// barriers.  The waves of a row are joined at the end.
+//
+// With many rows the reads of the tiles are what the LDS is busy with, and 16 lanes are served at once.  K: as above, with
+// slabs 32 bytes off each other, so that a product's 16 tokens may be four of every eight of two slabs: lane group mq then
+// holds the weights of eight tokens that follow one another.  V: eight tokens of a channel in one read; the 8 lanes served
+// at once take two positions of the four words, and positions lie 144 bytes apart, so that these do not meet.  (128 apart, with
+// reads of four tokens, four lanes met in every bank: 104 of the 286 thousand cycles that a CU was busy with 256 rows over
+// 32768 positions.)  The walks' writes meet more often for it (some 4 lanes in place of 2), which is less.
+constexpr int kPrefixWaves = 16;
+constexpr int kVPos = 72;                                   // values from a position of V to the next
+constexpr int kKSlab = 33 * kRowsPos + 16, kVSlab = 33 * kVPos;
+constexpr int kPrefixPage = 4 * (kKSlab + kVSlab);          // [K, V][slab]
+constexpr int kPrefixSet = 2 * kPrefixPage;
+constexpr int kStageCt = 65;                                // values of four of a group of channels (64 lanes), padded
+constexpr size_t kPrefixLds = sizeof(uint16_t) * 2 * kPrefixSet;    // 141 KB; the joining of 16 waves needs 130
+static_assert(sizeof(float) * 4 * kStageCt * 8 * kPrefixWaves <= kPrefixLds, "");
+
+template <int T, bool FULL, bool MX, int RT>
+__global__ __launch_bounds__(64 * kPrefixWaves) void attn_prefix_kernel(RowsArgs a) {
+  extern __shared__ __align__(16) uint16_t tiles[];
+  __shared__ float red[2][kPrefixWaves][16];
+  constexpr int NS = RT >= 8 ? 4 : RT / 2;  // slabs of 16 tokens that a wave's products take of a page
+  const KvGeom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = (int)blockIdx.x % g.n_kv_heads, item = (int)blockIdx.x / g.n_kv_heads;
+  const int slot = wv >> 3, u = wv & 7;                // page of the step, place among its waves
+  const int kv = u >> 2, r = (u & 3) * 16 + (lane >> 2), j = lane & 3;  // decode role: K or V, token, word
+  const int mi = lane & 15, mq = lane >> 4;
+  const int tile = RT == 16 ? wv : u % RT, slab0 = RT >= 8 ? 0 : (u / RT) * NS;   // role in the products
+  const int blocks = (a.rows + 16 * RT - 1) / (16 * RT), split = item / blocks, row_base = (item - split * blocks) * 16 * RT;
+  const int pg0 = split * a.prefix_run, pg1 = min(pg0 + a.prefix_run, a.prefix_pages), steps = (pg1 - pg0 + 1) / 2;
+  const int32_t* page_row = a.table + (size_t)a.seq[0] * g.max_pages_per_seq;
+  // where the thread's word begins in a set, and what a position adds
+  const int col = slot * kPrefixPage + (kv ? 4 * kKSlab + (u & 3) * kVSlab + kVPos + j * 16 + (lane >> 2)
+                                           : (u & 3) * kKSlab + kRowsPos + (lane >> 2) * 4 + j);
+  const int pitch = 2 * (kv ? kVPos : kRowsPos);  // bytes
+
+  // ---- the wave's unit of a step: pool pages two steps ahead, bitmap words one, fields as soon as those are there
+  auto page_of = [&](int step) {
+    const int pg = pg0 + 2 * step + slot;
+    return pg < pg1 ? min(max(page_row[pg], 0), g.n_pages - 1) : -1;
+  };
+  auto tile_of = [&](int page) { return (((size_t)a.layer * g.n_pages + page) * 2 + kv) * g.n_kv_heads + head; };
+  uint32_t next_mask = 0, next_exp = 0;
+  auto request_mask = [&](int page) {
+    if (page < 0) return;
+    const uint32_t* sp = a.spec_pool + tile_of(page) * g.tile_spec_words;
+    next_mask = sp[r * 4 + j];
+    if constexpr (MX) next_exp = sp[64 * 4 + r];
+  };
+  // the exact form with many rows has no registers for all fields during the products: those of the values that were not
+  // kept are requested behind them, under the decode of the kept ones
+  constexpr bool kLate = RT >= 4;
+  WordWindows<T, FULL, MX> win;
+  uint32_t mask = 0, pruned_at = 0;
+  const uint32_t* pruned_row = nullptr;
+  int shared_exp = 0;
+  auto request_fields = [&](int page) {
+    if (page < 0) return;
+    mask = taken(next_mask);
+    if constexpr (MX) shared_exp = (int)((taken(next_exp) >> (8 * j)) & 0xFFu);
+    const int cnt = __popc(mask);
+    const int b0 = quad_dpp<0x00>(cnt), b1 = quad_dpp<0x55>(cnt), b2 = quad_dpp<0xAA>(cnt);
+    const uint32_t p = (uint32_t)((j > 0 ? b0 : 0) + (j > 1 ? b1 : 0) + (j > 2 ? b2 : 0));
+    const size_t t = tile_of(page);
+    const uint32_t* sp = a.spec_pool + t * g.tile_spec_words;
+    const uint32_t* vf = a.verif_pool + t * g.tile_verif_words;
+    win.k.load(p, sp + g.spec_off + r * g.sw, vf + r * g.lw);
+    pruned_row = vf + 64 * g.lw + r * g.pw;
+    pruned_at = 32u * j - p;
+    if constexpr (FULL && !kLate) win.pr.load(pruned_at, pruned_row);
+  };
+  auto decode = [&](int set) {
+    const uint32_t to = lds_address(tiles + set * kPrefixSet + col);
+    if constexpr (!FULL) {  // what is not written has to read as 0: 512 or 576 groups of eight values
+      uint16_t* const slab = tiles + set * kPrefixSet + slot * kPrefixPage + (kv ? 4 * kKSlab + (u & 3) * kVSlab + kVPos
+                                                                                 : (u & 3) * kKSlab + kRowsPos);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(slab)[lane + 64 * k] = make_uint4(0, 0, 0, 0);
+      if (kv && lane < 32) reinterpret_cast<uint4*>(slab)[lane + 256] = make_uint4(0, 0, 0, 0);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    if constexpr (FULL && kLate) win.pr.load(pruned_at, pruned_row);
+    win.k.decode(mask, [&](int bp, uint16_t v) { lds_write(to, bp, pitch, v); }, shared_exp);
+    if constexpr (FULL) win.pr.decode(~mask, [&](int bp, uint16_t v) { lds_write(to, bp, pitch, v); });
+  };
+  int page_a = page_of(0), page_b = page_of(1);
+  request_mask(page_a);
+
+  // ---- queries, through the second set of tiles, which the decode of the second step is the first to write
+  rows_bf16x8 q[4];
+  {
+    static_assert(16 * RT * kQueryPitch <= kPrefixSet, "");
+    constexpr int kParts = (RT * 256 + 64 * kPrefixWaves - 1) / (64 * kPrefixWaves);
+    uint16_t* const stage = tiles + kPrefixSet;
+    QueryPart part[kParts];
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      const int i = tid + k * 64 * kPrefixWaves;
+      int rr = row_base + (i >> 4), first = 0;
+      const bool there = rr < a.rows && i < RT * 256;
+      const uint16_t* src = a.Q[0];
+#pragma unroll
+      for (int s = 1; s < kRowsSeqs; ++s) {
+        const bool in = rr >= a.row0[s];
+        first = in ? a.row0[s] : first;
+        src = in ? a.Q[s] : src;
+      }
+      rr -= first;
+      const int c = (int)((uint32_t)rr * a.grp_inv >> 16), gi = rr - c * a.grp;
+      part[k].load(there ? src + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128 : nullptr, i & 15);
+    }
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      const int i = tid + k * 64 * kPrefixWaves;
+      if (i < RT * 256) part[k].store(stage + (i >> 4) * kQueryPitch, i & 15);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) q[kk] = q_fragment(stage + (tile * 16 + mi) * kQueryPitch, kk, mq);
+  }
+  rows_f32x4 o[8];
+  float m = kLowest, l = 0.f;
+#pragma unroll
+  for (int ct = 0; ct < 8; ++ct) o[ct] = rows_f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // places of the lane's reads in a page: K, tokens of the two parities of a product; V, channels 32 w + f of the four words w,
+  // f = 8 (mi / 4) + (ct ^ (mi / 4 & 1)), which lie in different halves of the banks
+  const int kq = NS == 1 ? slab0 * kKSlab + 4 * mi : (2 * (slab0 >> 1) + (mi >> 3)) * kKSlab + ((mi >> 2) & 1) * 32 + (mi & 3) * 4;
+  const int vq = 4 * kKSlab + (NS == 1 ? slab0 * kVSlab + 4 * mq : (2 * (slab0 >> 1) + (mq >> 1)) * kVSlab + 8 * (mq & 1)) +
+                 (1 + 8 * (mi >> 2)) * kVPos + (mi & 3) * 16;
+  const int odd = (mi >> 2) & 1 ? kVPos : 0;
+  auto products = [&](int set, int page, int pg) {
+    const uint16_t* const at = tiles + set * kPrefixSet + page * kPrefixPage;
+    // exponents: lane (mi, mq) holds four tokens of row mi a product, tt: 4 mq + e of the slab (NS = 1), or
+    // 32 (tt / 2) + 8 mq + 4 (tt & 1) + e
+    rows_f32x4 x[NS];
+#pragma unroll
+    for (int tt = 0; tt < NS; ++tt) {
+      x[tt] = rows_f32x4{0.f, 0.f, 0.f, 0.f};
+      asm volatile("" ::: "memory");  // the reads of one product at a time: those of all do not fit the registers
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        const uint16_t* src = at + kq + (tt >> 1) * 2 * kKSlab + (tt & 1) * 16 + (1 + k_position(kk, mq)) * kRowsPos;
+        const uint2 k0 = *reinterpret_cast<const uint2*>(src), k1 = *reinterpret_cast<const uint2*>(src + 2 * kRowsPos);
+        x[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(rows_bf16x8, rows_u32x4{k0.x, k0.y, k1.x, k1.y}), q[kk],
+                                                        x[tt], 0, 0, 0);
+      }
+    }
+    if (a.score != nullptr && row_base + tile * 16 + mi < a.rows) {
+      float* const to = a.score + ((size_t)head * a.rows + row_base + tile * 16 + mi) * a.score_ld + pg * 64;
+#pragma unroll
+      for (int tt = 0; tt < NS; ++tt)
+        *reinterpret_cast<rows_f32x4*>(to + (NS == 1 ? slab0 * 16 + 4 * mq : (slab0 >> 1) * 32 + (tt >> 1) * 32 + 8 * mq + 4 * (tt & 1))) =
+            x[tt] * a.scale2;
+    }
+    float mx = x[0][0];
+#pragma unroll
+    for (int i = 1; i < 4 * NS; ++i) mx = fmaxf(mx, x[i >> 2][i & 3]);
+    const float top = fmaxf(m, over_groups_max(mx) * a.scale2);
+    if (__builtin_amdgcn_ballot_w64(top > m)) {  // a factor of 1 for all rows otherwise
+      const float f = __builtin_amdgcn_exp2f(m - top);
+      l *= f;
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) o[ct] *= f;
+      m = top;
+    }
+    uint32_t h[2 * NS];
+#pragma unroll
+    for (int tt = 0; tt < NS; ++tt) {
+      float w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[e] = __builtin_amdgcn_exp2f(fmaf(x[tt][e], a.scale2, -top));
+        l += w[e];
+      }
+      h[2 * tt] = (uint32_t)f32_to_bf16(w[0]) | ((uint32_t)f32_to_bf16(w[1]) << 16);
+      h[2 * tt + 1] = (uint32_t)f32_to_bf16(w[2]) | ((uint32_t)f32_to_bf16(w[3]) << 16);
+    }
+    // outputs: value e of o[ct] is channel 32 e + 8 mq + (ct ^ (mq & 1))
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) {
+      const uint16_t* src = at + vq + ct * kVPos + (ct & 1 ? -odd : odd);
+      if constexpr (NS == 1) {
+        o[ct] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(*reinterpret_cast<const rows_s16x4*>(src),
+                                                          __builtin_bit_cast(rows_s16x4, make_uint2(h[0], h[1])), o[ct], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < NS / 2; ++kb)
+          o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              *reinterpret_cast<const rows_bf16x8*>(src + 2 * kb * kVSlab),
+              __builtin_bit_cast(rows_bf16x8, rows_u32x4{h[4 * kb], h[4 * kb + 1], h[4 * kb + 2], h[4 * kb + 3]}), o[ct], 0, 0, 0);
+      }
+    }
+  };
+
+  request_fields(page_a);
+  if (steps > 1) request_mask(page_b);
+  if (page_a >= 0) decode(0);
+  __syncthreads();
+  for (int step = 0; step < steps; ++step) {
+    const int set = step & 1;
+    page_a = page_b;
+    page_b = page_of(step + 2);
+    if (step + 1 < steps) request_fields(page_a);
+    if (step + 2 < steps) request_mask(page_b);
+    if constexpr (RT == 16) {
+      products(set, 0, pg0 + 2 * step);
+      if (pg0 + 2 * step + 1 < pg1) products(set, 1, pg0 + 2 * step + 1);
+    } else {
+      if (pg0 + 2 * step + slot < pg1) products(set, slot, pg0 + 2 * step + slot);
+    }
+    if (step + 1 < steps && page_a >= 0) decode(set ^ 1);
+    __syncthreads();
+  }
+
+  float* const out = a.out_prefix + (((size_t)split * g.n_kv_heads + head) * a.rows + row_base) * 128;
+  float2* const ml = a.ml_prefix + ((size_t)head * a.rows + row_base) * a.prefix_splits + split;
+  const int rows = a.rows - row_base;
+  l = over_groups_sum(l);
+  // eight channels that follow one another of each word: run[2 e], run[2 e + 1] are channels 32 e + 8 mq + 0 .. 3, 4 .. 7
+  rows_f32x4 run[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) run[2 * e + (i >> 2)][i & 3] = mq & 1 ? o[i ^ 1][e] : o[i][e];
+  }
+  if constexpr (RT == 16) {
+    const int rr = tile * 16 + mi;
+    if (rr >= rows) return;
+    rows_f32x4* const dst = reinterpret_cast<rows_f32x4*>(out + (size_t)rr * 128 + 8 * mq);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dst[(i >> 1) * 8 + (i & 1)] = run[i];
+    if (mq == 0) ml[(size_t)rr * a.prefix_splits] = make_float2(m, l);
+  } else {
+    // the waves of a tile of rows: RT apart, added in their order
+    if (mq == 0) {
+      red[0][wv][mi] = m;
+      red[1][wv][mi] = l;
+    }
+    __syncthreads();
+    float top = kLowest, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPrefixWaves / RT; ++w) top = fmaxf(top, red[0][w * RT + tile][mi]);
+#pragma unroll
+    for (int w = 0; w < kPrefixWaves / RT; ++w) sum += red[1][w * RT + tile][mi] * __builtin_amdgcn_exp2f(red[0][w * RT + tile][mi] - top);
+    const float f = __builtin_amdgcn_exp2f(m - top);
+    rows_f32x4* const stage = reinterpret_cast<rows_f32x4*>(tiles);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) stage[(wv * 8 + i) * kStageCt + lane] = run[i] * f;
+    if (wv < RT && mq == 0 && tile * 16 + mi < rows) ml[(size_t)(tile * 16 + mi) * a.prefix_splits] = make_float2(top, sum);
+    __syncthreads();
+    for (int e = tid; e < RT * 16 * 32; e += 64 * kPrefixWaves) {  // four channels c4 of row rr
+      const int rr = e >> 5, c4 = e & 31;
+      if (rr >= rows) break;
+      const rows_f32x4* const from = stage + ((rr >> 4) * 8 + (c4 >> 3) * 2 + (c4 & 1)) * kStageCt + ((c4 >> 1) & 3) * 16 + (rr & 15);
+      rows_f32x4 sum4 = from[0];
+#pragma unroll
+      for (int w = 1; w < kPrefixWaves / RT; ++w) sum4 += from[w * RT * 8 * kStageCt];
+      *reinterpret_cast<rows_f32x4*>(out + (size_t)rr * 128 + 4 * c4) = sum4;
+    }
+  }
+}
+
+// What follows the prefix
 template <bool FULL, bool MX>
 int launch_rows_partial(cas_ctx* ctx, const RowsArgs& a, int items) {
   const dim3 grid((unsigned)items * (unsigned)a.g.n_kv_heads);
@@ -380,6 +690,33 @@ int launch_rows_partial(cas_ctx* ctx, const RowsArgs& a, int items) {
 #undef CAS_LAUNCH
   CAS_HIP(ctx, hipGetLastError());
   return CAS_OK;
+}
+
+template <int T, bool FULL, bool MX, int RT>
+int launch_prefix_tiles(cas_ctx* ctx, const RowsArgs& a, dim3 grid) {
+  static LdsLimit lim;
+  const int rc = allow_lds(ctx, (const void*)attn_prefix_kernel<T, FULL, MX, RT>, kPrefixLds, lim);
+  if (rc != CAS_OK) return rc;
+  hipLaunchKernelGGL((attn_prefix_kernel<T, FULL, MX, RT>), grid, dim3(64 * kPrefixWaves), kPrefixLds, ctx->stream, a);
+  CAS_HIP(ctx, hipGetLastError());
+  return CAS_OK;
+}
+
+// The prefix, for tiles (2, 4, 8 or 16) of 16 query rows a workgroup
+template <bool FULL, bool MX>
+int launch_prefix_partial(cas_ctx* ctx, const RowsArgs& a, int tiles, int items) {
+  const dim3 grid((unsigned)items * (unsigned)a.g.n_kv_heads);
+#define CAS_LAUNCH(TV)                                                             \
+  case TV:                                                                         \
+    return tiles == 2   ? launch_prefix_tiles<TV, FULL, MX, 2>(ctx, a, grid)       \
+           : tiles == 4 ? launch_prefix_tiles<TV, FULL, MX, 4>(ctx, a, grid)       \
+           : tiles == 8 ? launch_prefix_tiles<TV, FULL, MX, 8>(ctx, a, grid)       \
+                        : launch_prefix_tiles<TV, FULL, MX, 16>(ctx, a, grid);
+  switch (a.g.t) {
+    CAS_LAUNCH(0) CAS_LAUNCH(1) CAS_LAUNCH(2) CAS_LAUNCH(3) CAS_LAUNCH(4) CAS_LAUNCH(5) CAS_LAUNCH(6) CAS_LAUNCH(7)
+    default: return CAS_EINVAL;
+  }
+#undef CAS_LAUNCH
 }
 
 }  // namespace cas

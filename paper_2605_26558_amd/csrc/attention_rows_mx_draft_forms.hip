@@ -3,4 +3,5 @@
 
 namespace cas {
 template int launch_rows_partial<false, true>(cas_ctx*, const RowsArgs&, int);
+template int launch_prefix_partial<false, true>(cas_ctx*, const RowsArgs&, int, int);
 }  // namespace cas

@@ -27,12 +27,16 @@ struct SelectArgs {
   float* kept;
 };
 
-// PER: scores of a thread kept in registers; 0: read again wherever they are needed (rows too long for registers)
+// Counts of the 16 waves meet in one LDS counter each (integer additions: no order in the result); three sets take turns, so
+// that one barrier a turn is enough: a set is cleared in the turn before it is added to, behind the barrier after which all have read it.
+// PER: scores of a thread kept in registers (as scores and as keys); 0: read again wherever they are needed, rows too
+// long for registers.
 template <int PER>
 __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
   constexpr int N = PER > 0 ? PER : 1;
-  __shared__ uint32_t cnt[2][kSelWaves][3];
-  __shared__ uint32_t tot[kSelWaves][2];
+  constexpr int kAhead = 8;  // scores requested at once where they are read again
+  __shared__ uint32_t cnt[3][4];
+  __shared__ uint32_t place[PER > 0 ? PER * kSelWaves : 2 * kSelWaves];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float* row = a.score + (int64_t)blockIdx.x * a.ld;
   int32_t* index = a.index + (int64_t)blockIdx.x * a.n_keep;
@@ -40,106 +44,137 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
   const int lo = a.n_first, hi = a.len - a.n_last;   // the middle: positions lo .. hi - 1
   const uint32_t want = (uint32_t)(a.n_keep - a.n_first - a.n_last);
   const int steps = (a.len + kSelThreads - 1) / kSelThreads;
-  float v[N];
-  if constexpr (PER > 0) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int p = i * kSelThreads + tid;
-      v[i] = p < a.len ? row[p] : 0.f;
-    }
-  }
-  auto value = [&](int i) { const int p = i * kSelThreads + tid; return p < a.len ? row[p] : 0.f; };
+  auto value = [&](int i) {
+    const int p = i * kSelThreads + tid;
+    return p < a.len ? row[p] : 0.f;
+  };
   auto key_of = [&](int i, float x) {  // 0 outside the middle
     const int p = i * kSelThreads + tid;
     return p >= lo && p < hi ? score_key(x) : 0u;
   };
+  float v[N];
   uint32_t key[N];
   if constexpr (PER > 0) {
 #pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = value(i);
+#pragma unroll
     for (int i = 0; i < PER; ++i) key[i] = key_of(i, v[i]);
   }
-  // the largest T with at least `want` keys >= T (1 where none are wanted: then no tie is taken either)
+  if (tid < 12) (&cnt[0][0])[tid] = 0;
+  __syncthreads();
+  // f(key) of every position, the workgroup's waves together
+  auto each = [&](auto&& f) {
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (i < steps) f(key[i]);
+    } else {
+      for (int i = 0; i < steps; i += kAhead) {
+        float x[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) x[q] = value(i + q);
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) f(key_of(i + q, x[q]));
+      }
+    }
+  };
+  // The largest T that at least `want` keys reach, two bits a turn; a last turn counts the keys above it.
   uint32_t T = 0, above = 0;
-  for (int bit = 30, turn = 0; bit >= 0 && want > 0; bit -= 2, turn ^= 1) {
-    uint32_t n[3] = {0, 0, 0};
-    const uint32_t t1 = T | 1u << bit, t2 = T | 2u << bit, t3 = T | 3u << bit;
-    auto count = [&](uint32_t k) {
-      n[0] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t1));
-      n[1] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t2));
-      n[2] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t3));
-    };
-    if constexpr (PER > 0) {
-#pragma unroll
-      for (int i = 0; i < PER; ++i) count(key[i]);
-    } else {
-      for (int i = 0; i < steps; ++i) count(key_of(i, value(i)));
+  if (want > 0) {
+    int set = 0;
+    for (int bit = 30; bit >= -2; bit -= 2) {
+      uint32_t n[3] = {0, 0, 0};
+      const uint32_t t1 = bit >= 0 ? T | 1u << bit : T + 1u, t2 = bit >= 0 ? T | 2u << bit : 0u, t3 = bit >= 0 ? T | 3u << bit : 0u;
+      each([&](uint32_t k) {
+        n[0] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t1));
+        n[1] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t2));
+        n[2] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t3));
+      });
+      if (lane < 3) atomicAdd(&cnt[set][lane], lane == 0 ? n[0] : lane == 1 ? n[1] : n[2]);
+      const int next = set == 2 ? 0 : set + 1;
+      __syncthreads();
+      const uint32_t s0 = cnt[set][0], s1 = cnt[set][1], s2 = cnt[set][2];
+      if (tid < 4) cnt[next == 2 ? 0 : next + 1][tid] = 0;
+      set = next;
+      if (bit >= 0) T = s2 >= want ? t3 : s1 >= want ? t2 : s0 >= want ? t1 : T;
+      else above = T == 0xFFFFFFFFu ? 0u : s0;
     }
-    if (lane < 3) cnt[turn][wv][lane] = lane == 0 ? n[0] : lane == 1 ? n[1] : n[2];
-    __syncthreads();
-    uint32_t s[3] = {0, 0, 0};
-#pragma unroll
-    for (int w = 0; w < kSelWaves; ++w) {
-#pragma unroll
-      for (int q = 0; q < 3; ++q) s[q] += cnt[turn][w][q];
-    }
-    T = s[2] >= want ? t3 : s[1] >= want ? t2 : s[0] >= want ? t1 : T;
-  }
-  if (want > 0) {  // keys above the threshold
-    uint32_t n = 0;
-    if constexpr (PER > 0) {
-#pragma unroll
-      for (int i = 0; i < PER; ++i) n += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(key[i] > T));
-    } else {
-      for (int i = 0; i < steps; ++i) n += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(key_of(i, value(i)) > T));
-    }
-    __syncthreads();
-    if (lane == 0) cnt[0][wv][0] = n;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kSelWaves; ++w) above += cnt[0][w][0];
   }
   const uint32_t ties = want - above;  // equals of the threshold that stay
-  uint32_t base = 0, tie_base = 0;     // kept positions and equals before this step
-  for (int i = 0; i < steps; ++i) {
-    float x;
-    uint32_t k;
-    if constexpr (PER > 0) {
-      x = v[0]; k = key[0];
-#pragma unroll
-      for (int q = 1; q < PER; ++q) {
-        if (i == q) { x = v[q]; k = key[q]; }
-      }
-    } else {
-      x = value(i);
-      k = key_of(i, x);
-    }
+  auto sure_of = [&](int i, uint32_t k) {
     const int p = i * kSelThreads + tid;
-    const bool edge = p < a.len && (p < lo || p >= hi), sure = edge || (want > 0 && k > T);
-    const bool tie = want > 0 && k != 0u && k == T;
-    const uint64_t ms = __builtin_amdgcn_ballot_w64(sure), mt = __builtin_amdgcn_ballot_w64(tie);
-    __syncthreads();  // the counts of the step before have been read
-    if (lane == 0) {
-      tot[wv][0] = (uint32_t)__popcll(ms);
-      tot[wv][1] = (uint32_t)__popcll(mt);
+    return (p < a.len && (p < lo || p >= hi)) || (want > 0 && k > T);
+  };
+  auto tie_of = [&](uint32_t k) { return want > 0 && k == T; };
+  // before: those kept for sure in the lower half, equals in the upper, of the positions in front of the wave's 64
+  auto put = [&](int i, float x, bool sure, bool tie, uint64_t ms, uint64_t mt, uint32_t s_before, uint32_t t_before) {
+    const uint64_t below = (1ull << lane) - 1ull;
+    const uint32_t t_rank = t_before + (uint32_t)__popcll(mt & below);
+    if (sure || (tie && t_rank < ties)) {
+      const uint32_t at = s_before + (uint32_t)__popcll(ms & below) + min(t_rank, ties);
+      index[at] = i * kSelThreads + tid;
+      if (kept) kept[at] = x;
+    }
+  };
+  if constexpr (PER > 0) {
+    // one table of the counts of every 64 positions, summed up by one wave (at most 2^15 of either kind)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (i < steps) {
+        const uint64_t ms = __builtin_amdgcn_ballot_w64(sure_of(i, key[i])), mt = __builtin_amdgcn_ballot_w64(tie_of(key[i]));
+        if (lane == 0) place[i * kSelWaves + wv] = (uint32_t)__popcll(ms) | (uint32_t)__popcll(mt) << 16;
+      }
     }
     __syncthreads();
-    uint32_t s_before = base, t_before = tie_base, s_all = base, t_all = tie_base;
+    if (wv == 0) {
+      constexpr int kEach = PER * kSelWaves / 64;  // entries of a lane
+      uint32_t c[kEach], sum = 0;
 #pragma unroll
-    for (int w = 0; w < kSelWaves; ++w) {
-      s_before += w < wv ? tot[w][0] : 0u;
-      t_before += w < wv ? tot[w][1] : 0u;
-      s_all += tot[w][0];
-      t_all += tot[w][1];
+      for (int q = 0; q < kEach; ++q) {
+        const int e = lane * kEach + q;
+        c[q] = e < steps * kSelWaves ? place[e] : 0u;
+        sum += c[q];
+      }
+      uint32_t before = (uint32_t)wave_incl_scan((int)sum) - sum;
+#pragma unroll
+      for (int q = 0; q < kEach; ++q) {
+        place[lane * kEach + q] = before;
+        before += c[q];
+      }
     }
-    const uint64_t below = (1ull << lane) - 1ull;
-    const uint32_t s_rank = s_before + (uint32_t)__popcll(ms & below), t_rank = t_before + (uint32_t)__popcll(mt & below);
-    if (sure || (tie && t_rank < ties)) {
-      const uint32_t at = s_rank + min(t_rank, ties);
-      index[at] = p;
-      if (kept) kept[at] = x;  // never behind p, and this step's scores have been read by all
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (i < steps) {
+        const bool sure = sure_of(i, key[i]), tie = tie_of(key[i]);
+        const uint32_t before = place[i * kSelWaves + wv];
+        put(i, v[i], sure, tie, __builtin_amdgcn_ballot_w64(sure), __builtin_amdgcn_ballot_w64(tie), before & 0xFFFFu, before >> 16);
+      }
     }
-    base = s_all;
-    tie_base = t_all;
+  } else {
+    uint32_t s_base = 0, t_base = 0;
+    for (int i = 0; i < steps; ++i) {
+      const float x = value(i);
+      const uint32_t k = key_of(i, x);
+      const bool sure = sure_of(i, k), tie = tie_of(k);
+      const uint64_t ms = __builtin_amdgcn_ballot_w64(sure), mt = __builtin_amdgcn_ballot_w64(tie);
+      __syncthreads();  // the counts of the step before have been read
+      if (lane == 0) {
+        place[2 * wv] = (uint32_t)__popcll(ms);
+        place[2 * wv + 1] = (uint32_t)__popcll(mt);
+      }
+      __syncthreads();  // and this step's scores, over which a kept one may be written
+      uint32_t s_before = s_base, t_before = t_base;
+#pragma unroll
+      for (int w = 0; w < kSelWaves; ++w) {
+        const uint32_t s = place[2 * w], t = place[2 * w + 1];
+        s_before += w < wv ? s : 0u;
+        t_before += w < wv ? t : 0u;
+        s_base += s;
+        t_base += t;
+      }
+      put(i, x, sure, tie, ms, mt, s_before, t_before);
+    }
   }
 }
 
@@ -183,6 +218,13 @@ __device__ __forceinline__ MoveGroup move_load(const MoveArgs& a, int pool, int 
     if (i < a.n_streams[pool] && word >= a.s[pool][i].begin) s = a.s[pool][i];
   const uint32_t e = (uint32_t)(word - s.begin);
   int r = (int)(e * s.inv >> 18), c = (int)e - r * s.w;
+  if (c + 4 <= s.w && r < rows) {
+    typedef unsigned int words4 __attribute__((ext_vector_type(4), aligned(4)));
+    const words4 v = *reinterpret_cast<const words4*>(src[r] + s.begin + row[r] * s.w + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m.v[i] = v[i];
+    return m;
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     m.v[i] = 0;
