@@ -128,11 +128,11 @@ _SIGNATURES = {
     "cas_attention_static_capacity": (C.c_size_t, []),
     "cas_rope_freqs": (C.c_int, [C.POINTER(cas_rope_cfg), C.POINTER(C.c_double)]),
     "cas_rope_table": (C.c_int, [C.c_void_p, C.POINTER(cas_rope_cfg), C.c_int, C.c_int, C.c_void_p]),
+    # host arrays as plain addresses here: the wrappers of these calls are on the way of single tokens
     "cas_rope": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int,
-                           C.c_int, C.c_int, C.POINTER(cas_rope_part)]),
-    "cas_attention_shared": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.POINTER(C.c_int32), C.c_int, C.c_int,
-                                       C.POINTER(C.c_void_p), C.POINTER(C.c_int32), C.c_int, C.POINTER(C.c_void_p),
-                                       C.POINTER(C.c_void_p), C.POINTER(C.c_int32), C.POINTER(C.c_void_p)]),
+                           C.c_int, C.c_int, C.c_void_p]),
+    "cas_attention_shared": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
+                                       C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "cas_attention_shared_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.POINTER(C.c_int32), C.c_int, C.POINTER(C.c_int32),
                                                 C.c_int, C.POINTER(C.c_int32)]),
     "cas_attention_weights": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int,
@@ -675,24 +675,33 @@ def cas_rope(ctx: Context, table, xs, pos=None, pos0=0, layout=CAS_ROPE_HALF, tr
     tensors (bits as int16 for float32 inputs, the input's type otherwise); outs may be given, xs[i] itself included
     for two-byte tensors."""
     torch = ctx._torch
-    assert table.is_cuda and table.is_contiguous() and table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2
+    n_pos, half, two = table.shape
+    assert table.is_cuda and table.is_contiguous() and table.dtype == torch.float32 and two == 2
     n_tok, _, dim = xs[0].shape
     assert pos is None or (pos.is_cuda and pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == n_tok)
-    if outs is None:
-        outs = [torch.empty(x.shape, dtype=torch.int16 if x.dtype == torch.float32 else x.dtype, device=x.device) for x in xs]
-    parts = (cas_rope_part * len(xs))()
-    for i, (x, y) in enumerate(zip(xs, outs, strict=True)):
-        assert x.is_cuda and y.is_cuda and x.shape == y.shape and x.shape[0] == n_tok and x.shape[2] == dim
-        assert y.element_size() == 2 and (x.element_size() == 2 or x.dtype == torch.float32)
-        for t in (x, y):  # a dimension of one element has no stride to speak of
-            assert (t.stride(2) == 1 or dim == 1) and (t.stride(1) == dim or t.shape[1] <= 1)
-        row = x.shape[1] * dim
-        ld = [t.stride(0) if n_tok > 1 else row for t in (x, y)]
-        parts[i] = cas_rope_part(x.data_ptr(), y.data_ptr(), ld[0], ld[1], x.shape[1], int(x.dtype == torch.float32),
-                                 int(turn is None or bool(turn[i])), 0)
-    ctx._check(_lib().cas_rope(ctx.h, _ptr(table), table.shape[0], 2 * table.shape[1], layout, int(bool(transposed)), _ptr(pos),
-                               int(pos0), n_tok, dim, len(xs), parts), "cas_rope")
-    return outs
+    assert outs is None or len(outs) == len(xs)
+    ys, parts = [], []
+    for i, x in enumerate(xs):
+        shape, (ldx, head, one), fp32 = x.shape, x.stride(), x.dtype == torch.float32
+        heads = shape[1]
+        if outs is None:
+            y = torch.empty(shape, dtype=torch.int16 if fp32 else x.dtype, device=x.device)
+            ldy = heads * dim
+        else:
+            y = outs[i]
+            ldy, yhead, yone = y.stride()
+            assert y.shape == shape and y.is_cuda and (yone == 1 or dim == 1) and (yhead == dim or heads <= 1)
+        assert x.is_cuda and shape[0] == n_tok and shape[2] == dim and (one == 1 or dim == 1) and (head == dim or heads <= 1)
+        assert y.element_size() == 2 and (fp32 or x.element_size() == 2)
+        if n_tok == 1:  # no second token that a distance would lead to
+            ldx, ldy = max(ldx, heads * dim), max(ldy, heads * dim)
+        ys.append(y)
+        # the words of a cas_rope_part
+        parts += (x.data_ptr(), y.data_ptr(), ldx, ldy, heads | fp32 << 32, int(turn is None or bool(turn[i])))
+    ctx._check(_lib().cas_rope(ctx.h, table.data_ptr(), n_pos, 2 * half, layout, int(bool(transposed)),
+                               None if pos is None else pos.data_ptr(), int(pos0), n_tok, dim, len(xs),
+                               (C.c_int64 * len(parts))(*parts)), "cas_rope")
+    return ys
 
 
 def _i32(v):
@@ -700,32 +709,36 @@ def _i32(v):
     return (C.c_int32 * len(v))(*v)
 
 
-def _ptrs(ts):
-    return (C.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
-
-
 def cas_attention_shared(ctx: Context, kv: KVCache, layer, seqs, prefix_len, full, Qs, Knews, Vnews, outs=None):
     """Attention of several sequences whose first prefix_len positions are the same: lists of per-sequence tensors as in
     cas_attention."""
     torch = ctx._torch
-    seqs, Qs, Knews, Vnews = list(seqs), list(Qs), list(Knews), list(Vnews)
+    n = len(seqs)
     outs = [torch.empty_like(q) for q in Qs] if outs is None else list(outs)
-    assert len(seqs) == len(Qs) == len(Knews) == len(Vnews) == len(outs)
-    heads = Qs[0].shape[1]
+    assert n == len(Qs) == len(Knews) == len(Vnews) == len(outs) and n > 0
+    heads, ints, ptrs = Qs[0].shape[1], [[], []], [[], [], [], []]
     for q, k, v, o in zip(Qs, Knews, Vnews, outs):
-        _check_attention(kv, q, k, v, o)
-        assert q.shape[1] == heads
-    ctx._check(_lib().cas_attention_shared(ctx.h, kv.h, layer, len(seqs), _i32(seqs), int(prefix_len), 1 if full else 0, _ptrs(Qs),
-                                           _i32(q.shape[0] for q in Qs), heads, _ptrs(Knews), _ptrs(Vnews),
-                                           _i32(k.shape[0] for k in Knews), _ptrs(outs)), "cas_attention_shared")
+        cols, new = _check_attention(kv, heads, q, k, v, o)
+        ints[0].append(cols)
+        ints[1].append(new)
+        for p, t in zip(ptrs, (q, k, v, o)):
+            p.append(t.data_ptr())
+    i32, u64 = C.c_int32 * n, C.c_void_p * n
+    q, k, v, o = (u64(*p) for p in ptrs)
+    ctx._check(_lib().cas_attention_shared(ctx.h, kv.h, layer, n, i32(*seqs), prefix_len, 1 if full else 0, q, i32(*ints[0]), heads, k, v,
+                                           i32(*ints[1]), o), "cas_attention_shared")
     return outs
 
 
-def _check_attention(kv: KVCache, q, k, v, o):
-    h, d = kv.desc.n_kv_heads, kv.desc.head_dim
+def _check_attention(kv: KVCache, heads, q, k, v, o):
+    """Shapes, types and layout of one sequence's tensors; its columns and in-flight vectors."""
+    cols, qh, d = q.shape
+    new, kh, kd = k.shape
+    assert qh == heads and kh == kv.desc.n_kv_heads and d == kd == kv.desc.head_dim
+    assert v.numel() == k.numel() and o.numel() == q.numel()
     for t in (q, k, v, o):
-        assert t.is_cuda and t.is_contiguous() and t.element_size() == 2 and t.dim() == 3 and t.shape[2] == d
-    assert k.shape == v.shape and k.shape[1] == h and o.shape == q.shape
+        assert t.is_contiguous() and t.is_cuda and t.element_size() == 2
+    return cols, new
 
 
 def cas_attention_shared_bytes(kv: KVCache, seqs, prefix_len, ncols, n_q_heads, n_new) -> int:
@@ -741,17 +754,22 @@ def cas_attention_weights(ctx: Context, kv: KVCache, layer, seq, full, Q, Knew, 
     torch = ctx._torch
     if out is None:
         out = torch.empty_like(Q)
-    _check_attention(kv, Q, Knew, Vnew, out)
-    total = cas_kv_len(kv, seq) + Knew.shape[0]
+    heads = Q.shape[1]
+    cols, new = _check_attention(kv, heads, Q, Knew, Vnew, out)
+    total, rows = cas_kv_len(kv, seq) + new, kv.desc.n_kv_heads
     if score_out is None:
         ld = total if score_in is None else score_in.stride(0)
-        score_out = torch.empty((kv.desc.n_kv_heads, ld), dtype=torch.float32, device=Q.device)[:, :total]
-    for s in (score_out,) if score_in is None else (score_in, score_out):
-        assert s.is_cuda and s.dtype == torch.float32 and s.shape[0] == kv.desc.n_kv_heads and s.shape[1] >= total
-        assert s.stride(1) == 1 and s.stride(0) == score_out.stride(0)
-    ctx._check(_lib().cas_attention_weights(ctx.h, kv.h, layer, seq, 1 if full else 0, _ptr(Q), Q.shape[0], Q.shape[1], _ptr(Knew),
-                                            _ptr(Vnew), Knew.shape[0], _ptr(out), _ptr(score_in), _ptr(score_out),
-                                            score_out.stride(0)), "cas_attention_weights")
+        score_out = torch.empty((rows, ld), dtype=torch.float32, device=Q.device)
+        if ld != total:
+            score_out = score_out[:, :total]
+    ld = score_out.stride(0)
+    for s in (score_out, score_in):
+        if s is not None:
+            assert s.is_cuda and s.dtype == torch.float32 and s.stride() == (ld, 1)
+            assert s.shape[0] == rows and s.shape[1] >= total
+    ctx._check(_lib().cas_attention_weights(ctx.h, kv.h, layer, seq, 1 if full else 0, Q.data_ptr(), cols, heads, Knew.data_ptr(),
+                                            Vnew.data_ptr(), new, out.data_ptr(), None if score_in is None else score_in.data_ptr(),
+                                            score_out.data_ptr(), ld), "cas_attention_weights")
     return out, score_out
 
 
@@ -764,26 +782,29 @@ def cas_kv_select(ctx: Context, score, length, n_keep, n_first=0, n_last=0, kept
     """score: float32 [rows, >= length] -> int32 [rows, n_keep], the positions that stay, ascending.  kept: float32
     [rows, >= n_keep] for their scores, score itself included."""
     torch = ctx._torch
-    rows = score.shape[0]
-    for s, n in ((score, length),) if kept is None else ((score, length), (kept, n_keep)):
-        assert s.is_cuda and s.dtype == torch.float32 and s.dim() == 2 and s.shape[0] == rows and s.shape[1] >= n
-        assert (s.stride(1) == 1 or s.shape[1] <= 1) and (s.stride(0) >= s.shape[1] or rows <= 1)
+    rows, ld = score.shape[0], []
+    for s, n in ((score, length), (kept, n_keep)):
+        if s is None:
+            ld.append(0)
+            continue
+        (r, w), (step, one) = s.shape, s.stride()
+        assert s.is_cuda and s.dtype == torch.float32 and r == rows and w >= n and (one == 1 or w <= 1) and (step >= w or rows <= 1)
+        ld.append(max(step, w))
     if index is None:
         index = torch.empty((rows, n_keep), dtype=torch.int32, device=score.device)
     assert index.is_cuda and index.is_contiguous() and index.dtype == torch.int32 and index.shape == (rows, n_keep)
-    ld = [max(s.stride(0), s.shape[1]) for s in (score, score if kept is None else kept)]
-    ctx._check(_lib().cas_kv_select(ctx.h, _ptr(score), ld[0], rows, length, n_keep, n_first, n_last, _ptr(index), _ptr(kept), ld[1]),
-               "cas_kv_select")
+    ctx._check(_lib().cas_kv_select(ctx.h, score.data_ptr(), ld[0], rows, length, n_keep, n_first, n_last, index.data_ptr(),
+                                    None if kept is None else kept.data_ptr(), ld[1]), "cas_kv_select")
     return index
 
 
 def cas_kv_evict(ctx: Context, kv: KVCache, layer0, n_layers, seq, dst_seq, index):
     """Position i of dst_seq becomes position index[layer - layer0, head, i] of seq; index: int32 [n_layers, n_kv_heads,
     n_keep] on the GPU.  Does not change a length."""
-    torch = ctx._torch
-    assert index.is_cuda and index.is_contiguous() and index.dtype == torch.int32 and index.dim() == 3
-    assert index.shape[:2] == (n_layers, kv.desc.n_kv_heads)
-    ctx._check(_lib().cas_kv_evict(ctx.h, kv.h, layer0, n_layers, seq, dst_seq, _ptr(index), index.shape[2]), "cas_kv_evict")
+    layers, heads, n_keep = index.shape
+    assert layers == n_layers and heads == kv.desc.n_kv_heads
+    assert index.is_cuda and index.is_contiguous() and index.dtype == ctx._torch.int32
+    ctx._check(_lib().cas_kv_evict(ctx.h, kv.h, layer0, n_layers, seq, dst_seq, index.data_ptr(), n_keep), "cas_kv_evict")
 
 
 def _tensor(ew: EncodedWeight) -> cas_tensor:

@@ -3,28 +3,24 @@
 //
 // cas_attention decodes a page of the cache for the query rows of one sequence.  Where a batch of sequences begins with the
 // same pages, the decode, which is most of the time (some nine vector operations per value), is the same for all of them:
-// here a workgroup decodes a page once for 16, 32 or 64 query rows whichever sequence they belong to, and goes through a run
+// here a workgroup decodes a page once for up to 256 query rows whichever sequence they belong to, and goes through a run
 // of pages with running maxima and sums, so that a row has one partial result per run and not per page.  What follows the
 // prefix goes through the same kernel, sequence by sequence, in the same launch.
-//   grid: (runs of the prefix x tiles of all rows, then per sequence runs x tiles of its rows) x kv heads
+//   grid: (runs of the prefix x blocks of all rows, then per sequence runs x blocks of its rows) x kv heads
 // A second kernel joins the partial results of a row in the order of the runs, prefix first.
 //
-// Attention weights: the partial kernel also writes the exponents of its scores, and once the maximum and the sum of a row
-// are known, a third kernel forms the weights of all rows of a kv head and adds them.  Exponents are 4 bytes per row and
-// position, a vector of K 131 in the draft form: cheaper than decoding K again.
+// Attention weights: the partial kernel also writes the exponents of its scores, and the second launch, beside joining the
+// rows, forms the weights of all rows of a kv head from them and adds them up.  Exponents are 4 bytes per row and position,
+// a vector of K 131 in the draft form: cheaper than decoding K again.
 #include <algorithm>
 #include "attention_rows_kernel.inl"
 
 namespace cas {
 
-extern template int launch_rows_partial<true, false>(cas_ctx*, const RowsArgs&, int);
-extern template int launch_rows_partial<false, false>(cas_ctx*, const RowsArgs&, int);
-extern template int launch_rows_partial<true, true>(cas_ctx*, const RowsArgs&, int);
-extern template int launch_rows_partial<false, true>(cas_ctx*, const RowsArgs&, int);
-extern template int launch_prefix_partial<true, false>(cas_ctx*, const RowsArgs&, int, int);
-extern template int launch_prefix_partial<false, false>(cas_ctx*, const RowsArgs&, int, int);
-extern template int launch_prefix_partial<true, true>(cas_ctx*, const RowsArgs&, int, int);
-extern template int launch_prefix_partial<false, true>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_rows_partial<true, false>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_rows_partial<false, false>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_rows_partial<true, true>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_rows_partial<false, true>(cas_ctx*, const RowsArgs&, int, int);
 
 // Joins the partial results of a row: PARTS waves per row (4 or 1) take every PARTS-th split each, lane two channels, and
 // add them in order; then the parts in order.  Bound by latency: the pairs and kMergeAhead outputs are requested at once, the
@@ -36,12 +32,12 @@ __device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head
   const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int rr = block * (4 / PARTS) + wv / PARTS, part = wv % PARTS;
   if (rr >= a.rows) return;  // with four parts no wave of the workgroup is left
-  const int si = which_of(a.row0, rr);
-  struct {
-    uint16_t* O;
-    int ncols, row0, splits;
+  const SeqTable t_row0(a.row0), t_cols(a.ncols), t_splits(a.splits), t_len(a.len), t_new(a.n_new), t_part0(a.part0);
+  const int si = t_row0.which(rr);
+  const struct {
+    int ncols, row0, splits, len, n_new;
     uint32_t part0;
-  } const me = {a.O[si], a.ncols[si], a.row0[si], a.splits[si], a.part0[si]};
+  } me = {t_cols[si], t_row0[si], t_splits[si], t_len[si], t_new[si], (uint32_t)t_part0[si]};
   const int r = rr - me.row0, rows = me.ncols * a.grp, ps = a.prefix_splits, n = ps + me.splits;
   const float2* mlp = a.ml_prefix + ((size_t)head * a.rows + rr) * ps;
   const float2* mlt = a.ml_tail + me.part0 + ((size_t)head * rows + r) * me.splits;
@@ -61,6 +57,10 @@ __device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head
       o[q] = make_float2(__uint_as_float(two[0]), __uint_as_float(two[1]));
     }
   };
+  // words of the in-flight V that hold infinities or NaN: of one or two pages
+  const int page0 = me.len >> 6, flags = 4 * ((me.len + me.n_new + 63) / 64 - page0);
+  uint64_t odd = 0;
+  if (lane < flags) odd = a.odd[((size_t)si * a.g.n_kv_heads + head) * 8 + lane];
   float2 own = make_float2(kLowest, 0.f), all = make_float2(kLowest, 0.f);  // pairs of split `lane` of the part, of the row
   if (lane < cnt) own = pair(part + PARTS * lane);
   if (lane < n) all = pair(lane);
@@ -99,7 +99,21 @@ __device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head
     }
   }
   const int c = r / a.grp, gi = r - c * a.grp;
-  uint32_t* out = reinterpret_cast<uint32_t*>(me.O + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128) + lane;
+  if (__builtin_amdgcn_ballot_w64(odd != 0)) {  // those that the row sees, which the partial results left out
+    const uint32_t q = reinterpret_cast<const uint32_t*>(a.Q[si] + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128)[lane];
+    for (int i = 0; i <= me.n_new - me.ncols + c; ++i) {
+      const int t = me.len + i;
+      if (!(__shfl(odd, (t >> 4) - 4 * page0) >> (4 * (t & 15)) & 0xF)) continue;
+      const uint32_t k = reinterpret_cast<const uint32_t*>(a.Knew[si] + ((size_t)i * a.g.n_kv_heads + head) * 128)[lane];
+      const uint32_t v = reinterpret_cast<const uint32_t*>(a.Vnew[si] + ((size_t)i * a.g.n_kv_heads + head) * 128)[lane];
+      auto lo = [](uint32_t x) { return __uint_as_float(x << 16); };
+      auto hi = [](uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); };
+      const float w = __builtin_amdgcn_exp2f(wave_sum(lo(q) * lo(k) + hi(q) * hi(k)) * a.scale2 - M);
+      if ((v & 0x7F80u) == 0x7F80u) num.x += w * lo(v);
+      if ((v & 0x7F800000u) == 0x7F800000u) num.y += w * hi(v);
+    }
+  }
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.O[si] + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128) + lane;
   *out = (uint32_t)f32_to_bf16(num.x / den) | ((uint32_t)f32_to_bf16(num.y / den) << 16);
 }
 
@@ -174,21 +188,29 @@ __global__ __launch_bounds__(256) void rows_merge_weights_kernel(RowsArgs a, int
 }
 
 // ---- host ---------------------------------------------------------------------------------------
-constexpr int kPrefixItems = 256;
-constexpr int kTailRun = 2;  // pages of a run behind the prefix: fixed, so that a sequence's values do not depend on its length
+// A workgroup takes a CU for itself, so there are 256 runs x kv heads at a time.  A prefix is cut into as many, of two pages a
+// step; behind it runs have a fixed length, so that a sequence's values do not depend on the others'.
+constexpr int kWorkgroups = 256;
+constexpr int kTailRun = 4;
 
 struct RowsPlan {
   RowsArgs a;
-  int tiles;          // of 16 query rows of a workgroup in the prefix's launch
-  int items, prefix_items;
+  int tiles;   // of 16 query rows of a workgroup
+  int items;
   size_t bytes;
 };
+
+// Pages of a run: an even number
+static int run_of(int64_t pages, int heads) {
+  const int64_t runs = std::max(1, kWorkgroups / heads);
+  return (int)(((pages + runs - 1) / runs + 1) / 2 * 2);
+}
 
 static int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 
 // What a call will launch and need; Q, Knew, Vnew and O are left to the caller.
 static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int prefix_len, const int32_t* ncols, int n_q_heads,
-                     const int32_t* n_new, bool weights, int num_cu, RowsPlan* out) {
+                     const int32_t* n_new, bool weights, RowsPlan* out) {
   if (!kv || n_seqs < 1 || n_seqs > kRowsSeqs || !seqs || !ncols || !n_new || prefix_len < 0) return CAS_EINVAL;
   const KvGeom& g = kv->geom;
   if (n_q_heads < g.n_kv_heads || n_q_heads % g.n_kv_heads != 0) return CAS_EINVAL;
@@ -201,10 +223,10 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   a.grp_inv = (65536u + (uint32_t)a.grp - 1u) / (uint32_t)a.grp;
   a.scale2 = (float)(1.4426950408889634 * 0.08838834764831845);
   a.n_seqs = n_seqs;
-  // a sequence on its own: its whole pages are the prefix
-  a.prefix_pages = (weights && seqs[0] >= 0 && seqs[0] < kv->desc.max_seqs ? kv->h_len[seqs[0]] : prefix_len) / 64;
+  a.prefix_pages = prefix_len / 64;
   a.tail_run = kTailRun;
   int64_t rows = 0, parts = 0, items = 0;
+  int most = 0;
   for (int i = 0; i < n_seqs; ++i) {
     if (seqs[i] < 0 || seqs[i] >= kv->desc.max_seqs) return CAS_EINVAL;
     for (int k = 0; k < i; ++k)
@@ -214,36 +236,40 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
     if (prefix_len > a.len[i]) return CAS_EINVAL;
     const int64_t pages = ((int64_t)a.len[i] + a.n_new[i] + 63) / 64;
     if (pages > g.max_pages_per_seq) return CAS_ENOMEM;
-    a.splits[i] = (int)(pages - a.prefix_pages + kTailRun - 1) / kTailRun;
+    if (weights) a.tail_run = run_of(pages, g.n_kv_heads);
+    a.splits[i] = (int)(pages - a.prefix_pages + a.tail_run - 1) / a.tail_run;
     a.row0[i] = (int)rows;
     rows += ncols[i] * a.grp;
+    most = std::max(most, ncols[i] * a.grp);
   }
   a.rows = (int)rows;
+  if (a.prefix_pages > 0) most = a.rows;
+  p.tiles = most <= 32 ? 2 : most <= 64 ? 4 : most <= 128 ? 8 : 16;
+  const int block = 16 * p.tiles;
   if (a.prefix_pages > 0) {
-    // one workgroup per CU takes the rows of a tile count; as many runs as that gives, of two pages a step
-    const int runs = std::max(1, kPrefixItems / g.n_kv_heads);
-    a.prefix_run = ((a.prefix_pages + runs - 1) / runs + 1) / 2 * 2;
+    a.prefix_run = run_of(a.prefix_pages, g.n_kv_heads);
     a.prefix_splits = (a.prefix_pages + a.prefix_run - 1) / a.prefix_run;
-    p.tiles = a.rows <= 32 ? 2 : a.rows <= 64 ? 4 : a.rows <= 128 ? 8 : 16;
-    p.prefix_items = a.prefix_splits * ((a.rows + 16 * p.tiles - 1) / (16 * p.tiles));
+    a.prefix_items = a.prefix_splits * ((a.rows + block - 1) / block);
   }
   for (int i = 0; i < n_seqs; ++i) {
     const int r = ncols[i] * a.grp;
     a.item0[i] = (int)items;
     a.part0[i] = (uint32_t)parts;
-    items += (int64_t)a.splits[i] * ((r + 15) / 16);
+    items += (int64_t)a.splits[i] * ((r + block - 1) / block);
     parts += (int64_t)a.splits[i] * g.n_kv_heads * r;
     if (items > 0x7FFFFFFF || parts > 0xFFFFFFFFll) return CAS_ENOTSUP;
   }
   for (int i = n_seqs; i < kRowsSeqs; ++i) a.row0[i] = a.item0[i] = 0x7FFFFFFF;
   const int64_t first = (int64_t)a.prefix_splits * g.n_kv_heads * a.rows;
-  if (items * g.n_kv_heads > 0x7FFFFFFF ||
-      (int64_t)p.prefix_items * g.n_kv_heads > 0x7FFFFFFF) return CAS_ENOTSUP;
+  items += a.prefix_items;
+  if (items * g.n_kv_heads > 0x7FFFFFFF) return CAS_ENOTSUP;
   p.items = (int)items;
   // workspace: outputs, pairs, and the exponents of the rows
   int64_t off = up256((first + parts) * 512);
   const int64_t off_ml = off;
   off += up256((first + parts) * 8);
+  const int64_t off_odd = off;
+  off += up256((int64_t)n_seqs * g.n_kv_heads * 64);
   const int64_t off_score = off;
   if (weights) {
     a.score_ld = ((int64_t)a.len[0] + a.n_new[0] + 63) / 64 * 64;
@@ -254,6 +280,7 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   a.out_tail = (float*)(uintptr_t)(first * 512);
   a.ml_prefix = (float2*)(uintptr_t)off_ml;
   a.ml_tail = (float2*)(uintptr_t)(off_ml + first * 8);
+  a.odd = (uint64_t*)(uintptr_t)off_odd;
   a.score = weights ? (float*)(uintptr_t)off_score : nullptr;
   *out = p;
   return CAS_OK;
@@ -262,7 +289,7 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
 static void place(RowsArgs& a, void* ws) {  // offsets into the workspace become addresses
   char* b = (char*)ws;
   auto at = [&](auto*& p) { p = (std::remove_reference_t<decltype(p)>)(b + (uintptr_t)p); };
-  at(a.out_prefix); at(a.out_tail); at(a.ml_prefix); at(a.ml_tail);
+  at(a.out_prefix); at(a.out_tail); at(a.ml_prefix); at(a.ml_tail); at(a.odd);
   if (a.score) at(a.score);
 }
 
@@ -280,13 +307,8 @@ static int launch_rows(cas_ctx* ctx, cas_kv* kv, RowsPlan& p, int layer, int ful
   a.verif_pool = (const uint32_t*)kv->d_verif;
   a.table = kv->d_page_table;
   a.layer = layer;
-  int rc = CAS_OK;
-  if (p.prefix_items > 0)
-    rc = a.g.mx ? (full ? launch_prefix_partial<true, true>(ctx, a, p.tiles, p.prefix_items) : launch_prefix_partial<false, true>(ctx, a, p.tiles, p.prefix_items))
-                : (full ? launch_prefix_partial<true, false>(ctx, a, p.tiles, p.prefix_items) : launch_prefix_partial<false, false>(ctx, a, p.tiles, p.prefix_items));
-  if (rc == CAS_OK)
-    rc = a.g.mx ? (full ? launch_rows_partial<true, true>(ctx, a, p.items) : launch_rows_partial<false, true>(ctx, a, p.items))
-                : (full ? launch_rows_partial<true, false>(ctx, a, p.items) : launch_rows_partial<false, false>(ctx, a, p.items));
+  const int rc = a.g.mx ? (full ? launch_rows_partial<true, true>(ctx, a, p.tiles, p.items) : launch_rows_partial<false, true>(ctx, a, p.tiles, p.items))
+                        : (full ? launch_rows_partial<true, false>(ctx, a, p.tiles, p.items) : launch_rows_partial<false, false>(ctx, a, p.tiles, p.items));
   if (rc != CAS_OK) return rc;
   int most = 0;  // splits of a row: one wave can have 16 outputs in flight, so longer rows are shared by four
   for (int i = 0; i < a.n_seqs; ++i) most = std::max(most, a.prefix_splits + a.splits[i]);
@@ -312,7 +334,7 @@ int cas_attention_shared(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const 
                          uint16_t* const* h_d_O) {
   if (!ctx || !kv || layer < 0 || layer >= kv->desc.n_layers || !h_d_Q || !h_d_Knew || !h_d_Vnew || !h_d_O) return CAS_EINVAL;
   cas::RowsPlan p;
-  const int rc = cas::plan_rows(kv, n_seqs, h_seqs, prefix_len, h_ncols, n_q_heads, h_n_new, false, ctx->num_cu, &p);
+  const int rc = cas::plan_rows(kv, n_seqs, h_seqs, prefix_len, h_ncols, n_q_heads, h_n_new, false, &p);
   if (rc != CAS_OK) return rc;
   for (int i = 0; i < n_seqs; ++i) {
     p.a.Q[i] = h_d_Q[i]; p.a.Knew[i] = h_d_Knew[i]; p.a.Vnew[i] = h_d_Vnew[i]; p.a.O[i] = h_d_O[i];
@@ -326,7 +348,7 @@ int cas_attention_shared(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const 
 size_t cas_attention_shared_bytes(const cas_kv* kv, int n_seqs, const int32_t* h_seqs, int prefix_len, const int32_t* h_ncols,
                                   int n_q_heads, const int32_t* h_n_new) {
   cas::RowsPlan p;
-  return cas::plan_rows(kv, n_seqs, h_seqs, prefix_len, h_ncols, n_q_heads, h_n_new, false, 256, &p) == CAS_OK ? p.bytes : 0;
+  return cas::plan_rows(kv, n_seqs, h_seqs, prefix_len, h_ncols, n_q_heads, h_n_new, false, &p) == CAS_OK ? p.bytes : 0;
 }
 
 int cas_attention_weights(cas_ctx* ctx, cas_kv* kv, int layer, int seq, int full, const uint16_t* d_Q, int ncols, int n_q_heads,
@@ -334,7 +356,7 @@ int cas_attention_weights(cas_ctx* ctx, cas_kv* kv, int layer, int seq, int full
                           float* d_score_out, int64_t ld) {
   if (!ctx || !kv || layer < 0 || layer >= kv->desc.n_layers || !d_Q || !d_Knew || !d_Vnew || !d_O || !d_score_out) return CAS_EINVAL;
   cas::RowsPlan p;
-  const int rc = cas::plan_rows(kv, 1, &seq, 0, &ncols, n_q_heads, &n_new, true, ctx->num_cu, &p);
+  const int rc = cas::plan_rows(kv, 1, &seq, 0, &ncols, n_q_heads, &n_new, true, &p);
   if (rc != CAS_OK) return rc;
   const int total = p.a.len[0] + n_new;
   if (ld < total) return CAS_EINVAL;
@@ -347,7 +369,7 @@ int cas_attention_weights(cas_ctx* ctx, cas_kv* kv, int layer, int seq, int full
 
 size_t cas_attention_weights_bytes(const cas_kv* kv, int seq, int ncols, int n_q_heads, int n_new) {
   cas::RowsPlan p;
-  return cas::plan_rows(kv, 1, &seq, 0, &ncols, n_q_heads, &n_new, true, 256, &p) == CAS_OK ? p.bytes : 0;
+  return cas::plan_rows(kv, 1, &seq, 0, &ncols, n_q_heads, &n_new, true, &p) == CAS_OK ? p.bytes : 0;
 }
 
 }  // extern "C"
