@@ -714,31 +714,28 @@ def cas_attention_shared(ctx: Context, kv: KVCache, layer, seqs, prefix_len, ful
     cas_attention."""
     torch = ctx._torch
     n = len(seqs)
-    outs = [torch.empty_like(q) for q in Qs] if outs is None else list(outs)
-    assert n == len(Qs) == len(Knews) == len(Vnews) == len(outs) and n > 0
-    heads, ints, ptrs = Qs[0].shape[1], [[], []], [[], [], [], []]
-    for q, k, v, o in zip(Qs, Knews, Vnews, outs):
-        cols, new = _check_attention(kv, heads, q, k, v, o)
-        ints[0].append(cols)
-        ints[1].append(new)
-        for p, t in zip(ptrs, (q, k, v, o)):
-            p.append(t.data_ptr())
-    i32, u64 = C.c_int32 * n, C.c_void_p * n
-    q, k, v, o = (u64(*p) for p in ptrs)
-    ctx._check(_lib().cas_attention_shared(ctx.h, kv.h, layer, n, i32(*seqs), prefix_len, 1 if full else 0, q, i32(*ints[0]), heads, k, v,
-                                           i32(*ints[1]), o), "cas_attention_shared")
+    outs = [torch.empty_like(q) for q in Qs] if outs is None else outs
+    heads = Qs[0].shape[1]
+    cols, new, ptrs = _check_attention(kv, heads, Qs, Knews, Vnews, outs)
+    assert n == len(cols)
+    i32, ptr = C.c_int32 * n, C.c_void_p * n
+    q, k, v, o = (ptr(*p) for p in ptrs)
+    ctx._check(_lib().cas_attention_shared(ctx.h, kv.h, layer, n, i32(*seqs), prefix_len, 1 if full else 0, q, i32(*cols), heads, k, v,
+                                           i32(*new), o), "cas_attention_shared")
     return outs
 
 
-def _check_attention(kv: KVCache, heads, q, k, v, o):
-    """Shapes, types and layout of one sequence's tensors; its columns and in-flight vectors."""
-    cols, qh, d = q.shape
-    new, kh, kd = k.shape
-    assert qh == heads and kh == kv.desc.n_kv_heads and d == kd == kv.desc.head_dim
-    assert v.numel() == k.numel() and o.numel() == q.numel()
-    for t in (q, k, v, o):
-        assert t.is_contiguous() and t.is_cuda and t.element_size() == 2
-    return cols, new
+def _check_attention(kv: KVCache, heads, Qs, Knews, Vnews, outs):
+    """Shapes, types and layout of the sequences' tensors: their columns, in-flight vectors, and addresses."""
+    d = kv.desc.head_dim
+    qs, ks = [t.shape for t in Qs], [t.shape for t in Knews]
+    cols, new = [s[0] for s in qs], [s[0] for s in ks]
+    qt, kt = (heads, d), (kv.desc.n_kv_heads, d)
+    assert all([s[1:] == qt for s in qs]) and all([s[1:] == kt for s in ks]) and len(cols) == len(new) == len(Vnews) == len(outs)
+    qb, kb = [2 * c * heads * d for c in cols], [2 * c * kt[0] * d for c in new]
+    for ts, nbytes in ((Qs, qb), (Knews, kb), (Vnews, kb), (outs, qb)):
+        assert all([t.is_contiguous() and t.is_cuda for t in ts]) and [t.nbytes for t in ts] == nbytes
+    return cols, new, [[t.data_ptr() for t in ts] for ts in (Qs, Knews, Vnews, outs)]
 
 
 def cas_attention_shared_bytes(kv: KVCache, seqs, prefix_len, ncols, n_q_heads, n_new) -> int:
@@ -754,9 +751,11 @@ def cas_attention_weights(ctx: Context, kv: KVCache, layer, seq, full, Q, Knew, 
     torch = ctx._torch
     if out is None:
         out = torch.empty_like(Q)
-    heads = Q.shape[1]
-    cols, new = _check_attention(kv, heads, Q, Knew, Vnew, out)
-    total, rows = cas_kv_len(kv, seq) + new, kv.desc.n_kv_heads
+    (cols, heads, d), (new, rows, kd) = Q.shape, Knew.shape
+    assert rows == kv.desc.n_kv_heads and d == kd == kv.desc.head_dim
+    for t, n in ((Q, cols * heads), (out, cols * heads), (Knew, new * rows), (Vnew, new * rows)):
+        assert t.is_contiguous() and t.is_cuda and t.nbytes == 2 * n * d
+    total = cas_kv_len(kv, seq) + new
     if score_out is None:
         ld = total if score_in is None else score_in.stride(0)
         score_out = torch.empty((rows, ld), dtype=torch.float32, device=Q.device)

@@ -120,64 +120,104 @@ __device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head
 template <int PARTS>
 __global__ __launch_bounds__(256) void rows_merge_kernel(RowsArgs a) { merge_row<PARTS>(a, blockIdx.x, blockIdx.y); }
 
-// Weights of 256 positions of a kv head: every row's maximum and sum first (four rows of a wave at a time), then a thread
-// per position, eight rows requested at once.
+// Weights of 256 positions of a kv head.  Every row's maximum and sum first, 16 lanes to a row; then the waves take every
+// fourth row each, four positions a lane and eight rows requested at once, and are added in order.
 constexpr int kWeightsRows = 16 * 48;  // most query rows of a kv head
+constexpr int kWeightsPos = 256;
+
+template <int CTRL>
+__device__ __forceinline__ float rotated(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float max_of_16(float v) {
+  v = fmaxf(v, rotated<0x121>(v));
+  v = fmaxf(v, rotated<0x122>(v));
+  v = fmaxf(v, rotated<0x124>(v));
+  return fmaxf(v, rotated<0x128>(v));
+}
+__device__ __forceinline__ float sum_of_16(float v) {
+  v += rotated<0x121>(v);
+  v += rotated<0x122>(v);
+  v += rotated<0x124>(v);
+  return v + rotated<0x128>(v);
+}
+
 __device__ __forceinline__ void add_weights(const RowsArgs& a, int block, int head, const float* in, float* out, int64_t ld) {
   __shared__ float2 row_ml[kWeightsRows];
-  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), rows = a.rows, ps = a.prefix_splits, n = ps + a.splits[0];
-  const int pos = block * 256 + tid;
-  const bool there = pos < a.len[0] + a.n_new[0];
+  __shared__ rows_f32x4 joined[4][64];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), rows = a.rows;
+  const int ps = a.prefix_splits, own = a.splits[0], n = ps + own, len = a.len[0], total = len + a.n_new[0];
+  const int pos = block * kWeightsPos + 4 * lane;
+  const float* x = a.score + (size_t)head * rows * a.score_ld + pos;  // rows are padded to whole pages
+  const bool there = pos < total;
+  rows_f32x4 before = {0.f, 0.f, 0.f, 0.f};
   const int64_t at = (int64_t)head * ld + pos;
-  const float before = there && in && pos < a.len[0] ? in[at] : 0.f;
-  for (int r0 = 4 * wv; r0 < rows; r0 += 16) {
-    float2 p[4];
-    float M[4], L[4];
-    auto pair = [&](int k, int i) {  // split i of row r0 + k, those of the prefix first
-      const size_t row = (size_t)head * rows + min(r0 + k, rows - 1);
-      return i < ps ? a.ml_prefix[row * ps + i] : a.ml_tail[row * a.splits[0] + i - ps];
-    };
+  if (wv == 0 && in) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) p[k] = lane < n ? pair(k, lane) : make_float2(kLowest, 0.f);
+    for (int e = 0; e < 4; ++e)
+      if (pos + e < len) before[e] = in[at + e];
+  }
+  // four pairs of a lane at once: of one row, or of four where 16 lanes hold all splits of a row
+  const bool wide = n > 16;
+  for (int r0 = tid >> 4; r0 < rows; r0 += wide ? 16 : 64) {
+    float M[4], L[4];
+    float2 p[4];
+    auto pair = [&](int r, int i) {  // split i of row r, those of the prefix first
+      const size_t row = (size_t)head * rows + min(r, rows - 1);
+      return i >= n ? make_float2(kLowest, 0.f) : i < ps ? a.ml_prefix[row * ps + i] : a.ml_tail[row * own + i - ps];
+    };
+    const int i0 = lane & 15;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) p[k] = wide ? pair(r0, i0 + 16 * k) : pair(r0 + 16 * k, i0);
 #pragma unroll
     for (int k = 0; k < 4; ++k) M[k] = p[k].x;
-    for (int i = lane + 64; i < n; i += 64) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) M[k] = fmaxf(M[k], pair(k, i).x);
+    if (wide) {
+      M[0] = fmaxf(fmaxf(M[0], M[1]), fmaxf(M[2], M[3]));
+      for (int i = i0 + 64; i < n; i += 16) M[0] = fmaxf(M[0], pair(r0, i).x);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      M[k] = wave_max(M[k]);
-      L[k] = __builtin_amdgcn_exp2f(p[k].x - M[k]) * p[k].y;
+      if (k == 0 || !wide) M[k] = max_of_16(M[k]);
+      L[k] = __builtin_amdgcn_exp2f(p[k].x - M[wide ? 0 : k]) * p[k].y;
     }
-    for (int i = lane + 64; i < n; i += 64) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 q = pair(k, i);
-        L[k] += __builtin_amdgcn_exp2f(q.x - M[k]) * q.y;
+    if (wide) {
+      L[0] = (L[0] + L[1]) + (L[2] + L[3]);
+      for (int i = i0 + 64; i < n; i += 16) {
+        const float2 q = pair(r0, i);
+        L[0] += __builtin_amdgcn_exp2f(q.x - M[0]) * q.y;
       }
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      L[k] = wave_sum(L[k]);
-      if (lane == 0 && r0 + k < rows) row_ml[r0 + k] = make_float2(M[k], 1.f / L[k]);
+      if (k > 0 && wide) break;
+      L[k] = sum_of_16(L[k]);
+      if (i0 == 0 && r0 + 16 * k < rows) row_ml[r0 + 16 * k] = make_float2(M[k], 1.f / L[k]);
     }
   }
   __syncthreads();
-  if (!there) return;
-  const float* x = a.score + (size_t)head * rows * a.score_ld + pos;
-  float w = 0.f;
-  for (int r0 = 0; r0 < rows; r0 += 8) {
-    float v[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = x[(size_t)min(r0 + k, rows - 1) * a.score_ld];
+  rows_f32x4 w = {0.f, 0.f, 0.f, 0.f};
+  for (int r0 = wv; r0 < rows; r0 += 32) {
+    rows_f32x4 v[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float2 ml = row_ml[min(r0 + k, rows - 1)];
-      w += r0 + k < rows ? __builtin_amdgcn_exp2f(v[k] - ml.x) * ml.y : 0.f;
+      v[k] = rows_f32x4{0.f, 0.f, 0.f, 0.f};
+      if (there && r0 + 4 * k < rows) v[k] = *reinterpret_cast<const rows_f32x4*>(x + (size_t)(r0 + 4 * k) * a.score_ld);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (r0 + 4 * k >= rows) break;
+      const float2 ml = row_ml[r0 + 4 * k];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] += __builtin_amdgcn_exp2f(v[k][e] - ml.x) * ml.y;
     }
   }
-  out[at] = before + w;
+  joined[wv][lane] = w;
+  __syncthreads();
+  if (wv != 0 || !there) return;
+  w = ((w + joined[1][lane]) + joined[2][lane]) + joined[3][lane];
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (pos + e < total) out[at + e] = before[e] + w[e];
 }
 
 // both in one launch: neither needs the other
@@ -188,10 +228,10 @@ __global__ __launch_bounds__(256) void rows_merge_weights_kernel(RowsArgs a, int
 }
 
 // ---- host ---------------------------------------------------------------------------------------
-// A workgroup takes a CU for itself, so there are 256 runs x kv heads at a time.  A prefix is cut into as many, of two pages a
-// step; behind it runs have a fixed length, so that a sequence's values do not depend on the others'.
-constexpr int kWorkgroups = 256;
-constexpr int kTailRun = 4;
+// A prefix (or a sequence on its own) is cut into as many runs as there are workgroups at a time, two of eight waves or one of
+// sixteen a CU; behind a prefix runs have a fixed length, so that a sequence's values do not depend on the others' lengths.
+constexpr int kCus = 256;
+constexpr int kTailRun = 2;
 
 struct RowsPlan {
   RowsArgs a;
@@ -200,10 +240,22 @@ struct RowsPlan {
   size_t bytes;
 };
 
-// Pages of a run: an even number
-static int run_of(int64_t pages, int heads) {
-  const int64_t runs = std::max(1, kWorkgroups / heads);
-  return (int)(((pages + runs - 1) / runs + 1) / 2 * 2);
+// Pages of a run, whole steps of it, for `columns` workgroups side by side (kv heads x blocks of rows) and `others`
+// workgroups behind them.  As many runs as there are workgroups at a time; or fewer, so that the others start with them,
+// where that lengthens the runs by less than the others would take afterwards (some five steps: three before the first
+// products and behind the last, two of their own).  us with all / room for a workgroup a sequence and head: 16 sequences over
+// 8192 positions, draft 33.1 / 30.0, 8 sequences of 5 columns 45.5 / 40.1; 4 sequences of 64 query heads over 32768 positions
+// the same run either way.
+static int run_of(int64_t pages, int64_t columns, int64_t others, int tiles) {
+  const int step = tiles == 16 ? 2 : 1;
+  const int64_t slots = 2 / step * kCus;
+  auto run = [&](int64_t places) {
+    const int64_t runs = std::max<int64_t>(1, places / columns);
+    return ((pages + runs - 1) / runs + step - 1) / step * step;
+  };
+  const int64_t all = run(slots);
+  if (2 * others <= slots && all / step * others < 5 * (slots - others)) return (int)run(slots - others);
+  return (int)all;
 }
 
 static int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
@@ -226,7 +278,7 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   a.prefix_pages = prefix_len / 64;
   a.tail_run = kTailRun;
   int64_t rows = 0, parts = 0, items = 0;
-  int most = 0;
+  int most = 0, pages[kRowsSeqs];
   for (int i = 0; i < n_seqs; ++i) {
     if (seqs[i] < 0 || seqs[i] >= kv->desc.max_seqs) return CAS_EINVAL;
     for (int k = 0; k < i; ++k)
@@ -234,10 +286,9 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
     if (ncols[i] < 1 || ncols[i] > 16 || n_new[i] < ncols[i] || n_new[i] > 64) return CAS_EINVAL;
     a.seq[i] = seqs[i]; a.len[i] = kv->h_len[seqs[i]]; a.ncols[i] = ncols[i]; a.n_new[i] = n_new[i];
     if (prefix_len > a.len[i]) return CAS_EINVAL;
-    const int64_t pages = ((int64_t)a.len[i] + a.n_new[i] + 63) / 64;
-    if (pages > g.max_pages_per_seq) return CAS_ENOMEM;
-    if (weights) a.tail_run = run_of(pages, g.n_kv_heads);
-    a.splits[i] = (int)(pages - a.prefix_pages + a.tail_run - 1) / a.tail_run;
+    const int64_t pages_i = ((int64_t)a.len[i] + a.n_new[i] + 63) / 64;
+    if (pages_i > g.max_pages_per_seq) return CAS_ENOMEM;
+    pages[i] = (int)pages_i;
     a.row0[i] = (int)rows;
     rows += ncols[i] * a.grp;
     most = std::max(most, ncols[i] * a.grp);
@@ -247,12 +298,17 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   p.tiles = most <= 32 ? 2 : most <= 64 ? 4 : most <= 128 ? 8 : 16;
   const int block = 16 * p.tiles;
   if (a.prefix_pages > 0) {
-    a.prefix_run = run_of(a.prefix_pages, g.n_kv_heads);
+    const int blocks = (a.rows + block - 1) / block;
+    int64_t others = 0;
+    for (int i = 0; i < n_seqs; ++i) others += (int64_t)g.n_kv_heads * ((ncols[i] * a.grp + block - 1) / block);
+    a.prefix_run = run_of(a.prefix_pages, (int64_t)g.n_kv_heads * blocks, others, p.tiles);
     a.prefix_splits = (a.prefix_pages + a.prefix_run - 1) / a.prefix_run;
-    a.prefix_items = a.prefix_splits * ((a.rows + block - 1) / block);
+    a.prefix_items = a.prefix_splits * blocks;
   }
+  if (weights) a.tail_run = run_of(pages[0], (int64_t)g.n_kv_heads * ((a.rows + block - 1) / block), 0, p.tiles);
   for (int i = 0; i < n_seqs; ++i) {
     const int r = ncols[i] * a.grp;
+    a.splits[i] = (pages[i] - a.prefix_pages + a.tail_run - 1) / a.tail_run;
     a.item0[i] = (int)items;
     a.part0[i] = (uint32_t)parts;
     items += (int64_t)a.splits[i] * ((r + block - 1) / block);
@@ -314,7 +370,7 @@ static int launch_rows(cas_ctx* ctx, cas_kv* kv, RowsPlan& p, int layer, int ful
   for (int i = 0; i < a.n_seqs; ++i) most = std::max(most, a.prefix_splits + a.splits[i]);
   const int parts = most <= kMergeAhead ? 1 : 4, blocks = (a.rows * parts + 3) / 4;
   if (weights) {
-    const dim3 grid(blocks + (a.len[0] + a.n_new[0] + 255) / 256, a.g.n_kv_heads);
+    const dim3 grid(blocks + (a.len[0] + a.n_new[0] + kWeightsPos - 1) / kWeightsPos, a.g.n_kv_heads);
     hipLaunchKernelGGL(parts == 1 ? rows_merge_weights_kernel<1> : rows_merge_weights_kernel<4>, grid, dim3(256), 0, ctx->stream, a, blocks,
                        weights->in, weights->out, weights->ld);
   } else {

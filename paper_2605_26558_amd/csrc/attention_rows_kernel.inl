@@ -58,16 +58,24 @@ struct SeqTable {
   __device__ __forceinline__ int operator[](int s) const { return __builtin_amdgcn_readlane(v, s); }
 };
 
-constexpr int kRowsWaves = 16;
+// Waves of a workgroup and pages of a step.  256 query rows need sixteen waves and both pages; with fewer, two workgroups of
+// eight share a CU, and one decodes while the other waits for its streams.
+template <int RT>
+struct RowsShape {
+  static constexpr int kWaves = RT == 16 ? 16 : 8, kPages = kWaves / 8;
+};
 // A page's K and V in LDS, slab by slab of 16 tokens: [1 + 32 positions][values], for K the four words of a token at one
 // position side by side, for V the tokens of a word; row 0 takes what lanes without a value left write.
 constexpr int kKPos = 64, kVPos = 72;                       // values from a position to the next
 constexpr int kKSlab = 33 * kKPos + 16, kVSlab = 33 * kVPos;
 constexpr int kRowsPage = 4 * (kKSlab + kVSlab);
-constexpr int kRowsSet = 2 * kRowsPage;
 constexpr int kStageRun = 65;                               // groups of four values of 64 lanes, padded
-constexpr size_t kRowsLds = sizeof(uint16_t) * 2 * kRowsSet;    // 141 KB; the joining of 16 waves needs 130
-static_assert(sizeof(float) * 4 * kStageRun * 8 * kRowsWaves <= kRowsLds, "");
+template <int RT>
+struct RowsLds {  // two sets of tiles (72 KB a workgroup, 144 for sixteen waves), in which the waves' results are joined as well
+  static constexpr int kSet = RowsShape<RT>::kPages * kRowsPage;
+  static constexpr size_t kBytes = sizeof(uint16_t) * 2 * kSet;
+  static_assert(sizeof(float) * 4 * kStageRun * 8 * RowsShape<RT>::kWaves <= kBytes && 16 * RT * 136 <= kSet, "");
+};
 
 // Maximum / sum over the four lanes that hold one query row (lanes 16 apart)
 __device__ __forceinline__ float over_groups_max(float v) {
@@ -146,15 +154,16 @@ __device__ __forceinline__ void load_window(__amdgpu_buffer_rsrc_t rs, int off, 
 // that a CU was busy with 256 rows over 32768 positions, now 31 of 189.)  The walks' writes meet more often for it (some 4 lanes in
 // place of 2), which is less.
 template <int T, bool FULL, bool MX, int RT>
-__global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) {
+__global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kernel(RowsArgs a) {
+  constexpr int kWaves = RowsShape<RT>::kWaves, kPages = RowsShape<RT>::kPages, kSet = RowsLds<RT>::kSet;
   extern __shared__ __align__(16) uint16_t tiles[];
-  __shared__ float red[2][kRowsWaves][16];
+  __shared__ float red[2][kWaves][16];
   constexpr int NS = RT >= 8 ? 4 : RT / 2;  // slabs of 16 tokens that a wave's products take of a page
   const KvGeom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = (int)blockIdx.x % g.n_kv_heads;  // heads next to each other: workgroups that share pages share an XCD's L2
   int item = (int)blockIdx.x / g.n_kv_heads;
-  const int slot = wv >> 3, u = wv & 7;                // page of the step, place among its waves
+  const int slot = kPages == 1 ? 0 : wv >> 3, u = wv & 7;  // page of the step, place among its waves
   const int kv = u >> 2, r = (u & 3) * 16 + (lane >> 2), j = lane & 3;  // decode role: K or V, token, word
   const int mi = lane & 15, mq = lane >> 4;            // role in the products: query row (token, channel) mi, group mq
   const int tile = RT == 16 ? wv : u % RT, slab0 = RT >= 8 ? 0 : (u / RT) * NS;   // and the wave's: tile of rows, first slab
@@ -172,7 +181,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
   const int split = item / blocks, row_base = (item - split * blocks) * 16 * RT;
   const int len = prefix ? a.prefix_pages * 64 : t_len[si], total = prefix ? len : len + t_new[si];
   const int run = prefix ? a.prefix_run : a.tail_run;
-  const int pg0 = (prefix ? 0 : a.prefix_pages) + split * run, pg1 = min(pg0 + run, (total + 63) / 64), steps = (pg1 - pg0 + 1) / 2;
+  const int pg0 = (prefix ? 0 : a.prefix_pages) + split * run, pg1 = min(pg0 + run, (total + 63) / 64), steps = (pg1 - pg0 + kPages - 1) / kPages;
   const int32_t* page_row = a.table + (size_t)t_seq[si] * g.max_pages_per_seq;
   const uint32_t first = prefix ? 0 : (uint32_t)t_part0[si];  // of the partial results
   const int splits = prefix ? a.prefix_splits : t_splits[si];
@@ -187,7 +196,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
   const int pitch = 2 * (kv ? kVPos : kKPos);  // bytes
   constexpr int kNone = -1, kFresh = -2;       // no page; one without committed positions
   auto page_of = [&](int step) {
-    const int pg = pg0 + 2 * step + slot;
+    const int pg = pg0 + kPages * step + slot;
     return pg >= pg1 ? kNone : pg * 64 >= len ? kFresh : min(max(page_row[pg], 0), g.n_pages - 1);
   };
   auto tile_of = [&](int page) { return (((size_t)a.layer * g.n_pages + page) * 2 + kv) * g.n_kv_heads + head; };
@@ -196,7 +205,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
     next_mask = next_exp = 0;
     if (page < 0) return;
     const uint32_t* sp = a.spec_pool + tile_of(page) * g.tile_spec_words;
-    if ((pg0 + 2 * step + slot) * 64 + r < len) {
+    if ((pg0 + kPages * step + slot) * 64 + r < len) {
       next_mask = sp[r * 4 + j];
       if constexpr (MX) next_exp = sp[64 * 4 + r];
     }
@@ -238,11 +247,11 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
   };
   auto decode = [&](int step, int page) {
     if (page == kNone) return;
-    const int set = step & 1, tok0 = (pg0 + 2 * step + slot) * 64;
+    const int set = step & 1, tok0 = (pg0 + kPages * step + slot) * 64;
     const bool whole = tok0 + 64 <= len;  // of committed positions
-    const uint32_t to = lds_address(tiles + set * kRowsSet + col);
+    const uint32_t to = lds_address(tiles + set * kSet + col);
     if (!FULL || !whole) {  // what is not written has to read as 0: 512 or 576 groups of eight values
-      uint16_t* const slab = tiles + set * kRowsSet + slot * kRowsPage + (kv ? 4 * kKSlab + (u & 3) * kVSlab + kVPos : (u & 3) * kKSlab + kKPos);
+      uint16_t* const slab = tiles + set * kSet + slot * kRowsPage + (kv ? 4 * kKSlab + (u & 3) * kVSlab + kVPos : (u & 3) * kKSlab + kKPos);
 #pragma unroll
       for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(slab)[lane + 64 * k] = make_uint4(0, 0, 0, 0);
       if (kv && lane < 32) reinterpret_cast<uint4*>(slab)[lane + 256] = make_uint4(0, 0, 0, 0);
@@ -287,13 +296,12 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
   // ---- queries, through the second set of tiles, which the decode of the second step is the first to write
   rows_bf16x8 q[4];
   {
-    static_assert(16 * RT * kQueryPitch <= kRowsSet, "");
-    constexpr int kParts = (RT * 256 + 64 * kRowsWaves - 1) / (64 * kRowsWaves);
-    uint16_t* const stage = tiles + kRowsSet;
+    constexpr int kParts = (RT * 256 + 64 * kWaves - 1) / (64 * kWaves);
+    uint16_t* const stage = tiles + kSet;
     QueryPart part[kParts];
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
-      const int i = tid + k * 64 * kRowsWaves;
+      const int i = tid + k * 64 * kWaves;
       int rr = row_base + (i >> 4), first = 0;
       const bool there = rr < rows && i < RT * 256;
       const uint16_t* src = a.Q[si];
@@ -311,7 +319,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
     }
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
-      const int i = tid + k * 64 * kRowsWaves;
+      const int i = tid + k * 64 * kWaves;
       if (i < RT * 256) part[k].store(stage + (i >> 4) * kQueryPitch, i & 15);
     }
     __syncthreads();
@@ -332,9 +340,9 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
   // token of a page that the lane holds as element e of product tt: four of the slab (NS = 1), or of every eight of two
   auto token = [&](int tt) { return NS == 1 ? slab0 * 16 + 4 * mq : slab0 * 16 + 32 * (tt >> 1) + 8 * mq + 4 * (tt & 1); };
   auto products = [&](int step, int page) {
-    const int pg = pg0 + 2 * step + page, set = step & 1;
+    const int pg = pg0 + kPages * step + page, set = step & 1;
     if (idle || pg >= pg1) return;
-    const uint16_t* const at = tiles + set * kRowsSet + page * kRowsPage;
+    const uint16_t* const at = tiles + set * kSet + page * kRowsPage;
     rows_f32x4 x[NS];
 #pragma unroll
     for (int tt = 0; tt < NS; ++tt) {
@@ -437,7 +445,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
 #pragma unroll
     for (int i = 0; i < 8; ++i) eight[2 * e + (i >> 2)][i & 3] = mq & 1 ? o[i ^ 1][e] : o[i][e];
   }
-  if constexpr (RT == 16) {
+  if constexpr (RT == kWaves) {  // each wave has rows of its own
     const int rr = tile * 16 + mi;
     if (rr >= left) return;
     rows_f32x4* const dst = reinterpret_cast<rows_f32x4*>(out + (size_t)rr * 128 + 8 * mq);
@@ -453,9 +461,9 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
     __syncthreads();
     float top = kLowest, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kRowsWaves / RT; ++w) top = fmaxf(top, red[0][w * RT + tile][mi]);
+    for (int w = 0; w < kWaves / RT; ++w) top = fmaxf(top, red[0][w * RT + tile][mi]);
 #pragma unroll
-    for (int w = 0; w < kRowsWaves / RT; ++w) sum += red[1][w * RT + tile][mi] * __builtin_amdgcn_exp2f(red[0][w * RT + tile][mi] - top);
+    for (int w = 0; w < kWaves / RT; ++w) sum += red[1][w * RT + tile][mi] * __builtin_amdgcn_exp2f(red[0][w * RT + tile][mi] - top);
     const float f = __builtin_amdgcn_exp2f(m - top);
     rows_f32x4* const stage = reinterpret_cast<rows_f32x4*>(tiles);
     if (!idle) {
@@ -464,13 +472,13 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
       if (wv < RT && mq == 0 && tile * 16 + mi < left) ml[(size_t)(tile * 16 + mi) * splits] = make_float2(top, sum);
     }
     __syncthreads();
-    for (int e = tid; e < RT * 16 * 32; e += 64 * kRowsWaves) {  // four channels c4 of row rr
+    for (int e = tid; e < RT * 16 * 32; e += 64 * kWaves) {  // four channels c4 of row rr
       const int rr = e >> 5, c4 = e & 31;
       if (rr >= left) break;
       const rows_f32x4* const from = stage + ((rr >> 4) * 8 + (c4 >> 3) * 2 + (c4 & 1)) * kStageRun + ((c4 >> 1) & 3) * 16 + (rr & 15);
       rows_f32x4 sum4 = from[0];
 #pragma unroll
-      for (int w = 1; w < kRowsWaves / RT; ++w) sum4 += from[w * RT * 8 * kStageRun];
+      for (int w = 1; w < kWaves / RT; ++w) sum4 += from[w * RT * 8 * kStageRun];
       *reinterpret_cast<rows_f32x4*>(out + (size_t)rr * 128 + 4 * c4) = sum4;
     }
   }
@@ -479,9 +487,9 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(RowsArgs a) 
 template <int T, bool FULL, bool MX, int RT>
 int launch_rows_tiles(cas_ctx* ctx, const RowsArgs& a, dim3 grid) {
   static LdsLimit lim;
-  const int rc = allow_lds(ctx, (const void*)attn_rows_kernel<T, FULL, MX, RT>, kRowsLds, lim);
+  const int rc = allow_lds(ctx, (const void*)attn_rows_kernel<T, FULL, MX, RT>, RowsLds<RT>::kBytes, lim);
   if (rc != CAS_OK) return rc;
-  hipLaunchKernelGGL((attn_rows_kernel<T, FULL, MX, RT>), grid, dim3(64 * kRowsWaves), kRowsLds, ctx->stream, a);
+  hipLaunchKernelGGL((attn_rows_kernel<T, FULL, MX, RT>), grid, dim3(64 * RowsShape<RT>::kWaves), RowsLds<RT>::kBytes, ctx->stream, a);
   CAS_HIP(ctx, hipGetLastError());
   return CAS_OK;
 }

@@ -78,11 +78,13 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
       }
     }
   };
-  // The largest T that at least `want` keys reach, two bits a turn; a last turn counts the keys above it.
+  // The largest T that at least `want` keys reach, two bits a turn; found early where exactly
+  // `want` keys reach it, otherwise a last turn counts the keys above it.
   uint32_t T = 0, above = 0;
   if (want > 0) {
     int set = 0;
-    for (int bit = 30; bit >= -2; bit -= 2) {
+    bool exact = false;
+    for (int bit = 30; bit >= -2 && !exact; bit -= 2) {
       uint32_t n[3] = {0, 0, 0};
       const uint32_t t1 = bit >= 0 ? T | 1u << bit : T + 1u, t2 = bit >= 0 ? T | 2u << bit : 0u, t3 = bit >= 0 ? T | 3u << bit : 0u;
       each([&](uint32_t k) {
@@ -93,11 +95,21 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
       if (lane < 3) atomicAdd(&cnt[set][lane], lane == 0 ? n[0] : lane == 1 ? n[1] : n[2]);
       const int next = set == 2 ? 0 : set + 1;
       __syncthreads();
-      const uint32_t s0 = cnt[set][0], s1 = cnt[set][1], s2 = cnt[set][2];
+      // one value for all lanes, and known to be
+      const uint32_t s0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)cnt[set][0]), s1 = (uint32_t)__builtin_amdgcn_readfirstlane((int)cnt[set][1]),
+                     s2 = (uint32_t)__builtin_amdgcn_readfirstlane((int)cnt[set][2]);
       if (tid < 4) cnt[next == 2 ? 0 : next + 1][tid] = 0;
       set = next;
-      if (bit >= 0) T = s2 >= want ? t3 : s1 >= want ? t2 : s0 >= want ? t1 : T;
-      else above = T == 0xFFFFFFFFu ? 0u : s0;
+      if (bit >= 0) {
+        T = s2 >= want ? t3 : s1 >= want ? t2 : s0 >= want ? t1 : T;
+        exact = s2 == want || (s2 < want && s1 == want) || (s1 < want && s0 == want);
+      } else {
+        above = T == 0xFFFFFFFFu ? 0u : s0;
+      }
+    }
+    if (exact) {  // those that reach T are those that stay: none is equal to one below it
+      T -= 1u;
+      above = want;
     }
   }
   const uint32_t ties = want - above;  // equals of the threshold that stay
