@@ -64,17 +64,19 @@ def _reference(torch, B, ctx, kv, layer, s, full, q, kn, vn):
     seen = torch.arange(n + N, device="cuda") <= (torch.arange(C, device="cuda") + n + N - C).repeat_interleave(G)[:, None]
     sc = sc.masked_fill(~seen, -math.inf)
     p = torch.softmax(sc, 2)
-    # row by row, so that what a row does not see is no factor of it
-    rows = [torch.where(seen[i][:, None], v, 0.0) for i in range(C * G)]
-    o = torch.stack([(p[:, i, :, None] * rows[i]).sum(1) for i in range(C * G)], 1)
-    mean = torch.stack([(p[:, i, :, None] * rows[i].abs()).sum(1) for i in range(C * G)], 1)
+    o, mean = torch.empty_like(p[..., :1]).expand(-1, -1, 128).clone(), torch.empty_like(p[..., :1]).expand(-1, -1, 128).clone()
+    for i in range(C * G):  # row by row, so that what a row does not see is no factor of it
+        row = torch.where(seen[i][:, None], v, 0.0)
+        o[:, i] = (p[:, i, :, None] * row).sum(1)
+        mean[:, i] = (p[:, i, :, None] * row.abs()).sum(1)
     # a weight's relative error: its score as 128 fp32 additions of exact products and a scaling, in the exponent, and the
     # rounding of the exponential (2^-23 each of these); the same once more through the sum it is divided by
     rel = 2.0 ** -23 * (70 * big.masked_fill(~seen, 0.0) + 8)
     rel = rel + (p * rel).sum(2, keepdim=True) + 2.0 ** -24 * (64 + (n + N) / 16)
     w, wt = p.sum(1), (p * rel).sum(1) + 2.0 ** -23 * p.sum(1) * C * G
-    # an output: weights rounded to bf16 for the product (2^-8), its own rounding (2^-8), fp32 additions
-    tol = 2.0 ** -8 * o.abs() + (2.0 ** -8 + 2.0 ** -24 * (64 + (n + N) / 4) + rel.amax(2, keepdim=True)) * mean
+    # an output: weights as a bf16 head and the bf16 rounding of the rest (2^-7 cut off, 2^-8 of that), its own rounding (2^-8),
+    # fp32 additions
+    tol = 2.0 ** -8 * o.abs() + (2.0 ** -15 + 2.0 ** -24 * (64 + (n + N) / 4) + rel.amax(2, keepdim=True)) * mean
     shape = lambda x: x.view(H, C, G, 128).transpose(0, 1).reshape(C, nq, 128)  # noqa: E731
     return shape(o), shape(tol), w, wt
 
@@ -105,6 +107,14 @@ SHARED = [  # n_kv, group, prefix, tails, columns, in flight, full, keep, t, mod
     (2, 4, 192, [40, 2], [2, 2], [2, 2], False, 1000, 1, 2),
     (2, 3, 320, [129, 2, 3], [6, 5, 4], [6, 5, 4], True, 333, 2, 0),
     (8, 8, 640, [50, 20, 0, 64], [5, 5, 5, 5], [5, 5, 5, 5], True, 600, 6, 0),
+    (2, 8, 704, [9] * 9, [2] * 9, [2] * 9, False, 600, 4, 0),
+    # runs of several pages: of three, of five with a page left over, and of ten for the sixteen waves of many rows
+    (8, 4, 14117, [70, 3], [1, 1], [1, 2], False, 600, 4, 0),
+    (8, 2, 19205, [1], [7], [7], True, 400, 2, 2),
+    (8, 8, 19205, [70, 3, 130], [3, 2, 1], [3, 2, 4], True, 600, 4, 0),
+    (8, 8, 12900, [5, 3, 0, 1], [5, 5, 5, 5], [5, 5, 5, 5], True, 600, 4, 2),
+    (4, 8, 20000, [0, 100, 7], [6, 6, 6], [6, 6, 6], False, 500, 1, 0),
+    (8, 4, 0, [9000, 100], [5, 1], [5, 1], True, 600, 4, 0),
 ]
 
 
@@ -176,7 +186,8 @@ WEIGHTS = [  # n_kv, group, len, columns, in flight, full, keep, t, mode
     (2, 2, 0, 1, 1, False, 600, 4, 0), (2, 2, 0, 3, 5, True, 600, 4, 0), (1, 1, 1, 1, 1, True, 600, 4, 0),
     (2, 4, 63, 1, 1, False, 600, 4, 0), (2, 4, 64, 5, 5, True, 600, 4, 0), (8, 4, 1000, 1, 3, False, 600, 4, 2),
     (4, 8, 2049, 7, 7, True, 600, 4, 0), (1, 48, 130, 16, 20, True, 500, 3, 0), (2, 5, 4000, 3, 3, False, 250, 0, 0),
-    (8, 1, 515, 2, 64, True, 700, 5, 2), (2, 16, 300, 1, 1, False, 1000, 7, 0),
+    (8, 1, 515, 2, 64, True, 700, 5, 2), (2, 16, 300, 1, 1, False, 1000, 7, 0), (8, 4, 17001, 3, 3, True, 600, 4, 0),
+    (8, 8, 12300, 5, 6, False, 600, 4, 2), (1, 4, 9000, 1, 2, True, 600, 4, 0), (2, 9, 600, 16, 16, True, 600, 4, 0),
 ]
 
 
@@ -260,6 +271,29 @@ def test_captured_and_on_another_stream(env):
         with torch.cuda.stream(s):   # eager work on the same context between replays
             B.cas_attention(ctx, kv, 0, 1, True, Q[1], Kn[1], Vn[1])
         s.synchronize()
+
+
+def test_two_streams_at_once(env):
+    """Two contexts with workspaces of their own, on streams of their own, over the same cache."""
+    torch, B, ctx = env
+    kv = _cache(torch, B, ctx, 4, 2000, [100, 7])
+    Q, Kn, Vn = _inputs(torch, 2, [3, 1], [3, 1], 16, 4)
+    want = B.cas_attention_shared(ctx, kv, 0, [0, 1], 2000, True, Q, Kn, Vn)
+    want_w = B.cas_attention_weights(ctx, kv, 0, 0, True, Q[0], Kn[0], Vn[0])
+    torch.cuda.synchronize()
+    streams, runs = [torch.cuda.Stream() for _ in range(2)], []
+    for s in streams:
+        with torch.cuda.stream(s):
+            runs.append((B.Context(workspace=torch.empty(32 << 20, dtype=torch.uint8, device="cuda")), [], []))
+    for _ in range(10):
+        for s, (c, outs, ws) in zip(streams, runs):
+            with torch.cuda.stream(s):
+                outs.append(B.cas_attention_shared(c, kv, 0, [0, 1], 2000, True, Q, Kn, Vn))
+                ws.append(B.cas_attention_weights(c, kv, 0, 0, True, Q[0], Kn[0], Vn[0]))
+    torch.cuda.synchronize()
+    for _, outs, ws in runs:
+        for o, w in zip(outs, ws):
+            assert all(torch.equal(x, y) for x, y in zip(o, want)) and all(torch.equal(x, y) for x, y in zip(w, want_w))
 
 
 def test_refusals(env):
