@@ -192,11 +192,14 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
 
 // ---- moving ---------------------------------------------------------------------------------------
 // A tile (64 vectors of one head) is two runs of words, its parts of the two pools, each made of streams of w words per
-// vector in vector order.  A thread moves four words of the destination that follow one another and were, where they do
-// not reach into the next vector, four words that followed one another in the source: 16 bytes either way.
+// vector in vector order.  A thread moves four words of a vector, the last four of a stream where fewer are left (two threads then
+// write the same words): one load and one store of 16 bytes each, on multiples of 4 bytes, for every stream of four words
+// or more.  With 16 bytes of the destination to a thread, which may reach into the next vector, a quarter of the threads needs
+// four loads, and their waves five: what a CU's address unit then takes was most of 32 layers' 175 us.
 struct MoveStream {
   int begin, w;       // first word in the pool's part of a tile, words of a vector
-  uint32_t inv;       // ceil(2^18 / w): word e < 4096 of the stream belongs to vector e * inv >> 18
+  int first, groups;  // threads before, and to a vector
+  uint32_t inv;       // ceil(2^18 / groups): thread e < 4096 of the stream takes vector e * inv >> 18
 };
 struct MoveArgs {
   KvGeom g;
@@ -204,7 +207,7 @@ struct MoveArgs {
   int tile_words[2];
   int n_streams[2];
   MoveStream s[2][3];
-  int words[2];       // words of a tile that hold vectors
+  int threads[2];     // of a tile
   const int32_t* src_row;
   const int32_t* dst_row;
   const int32_t* index;
@@ -212,61 +215,48 @@ struct MoveArgs {
 };
 
 constexpr int kMoveThreads = 256;
-constexpr int kMoveGroups = 5;  // groups of four words of a thread and pool: 64 x 68 words and fewer in 4 x 256 + 64 groups
+constexpr int kMoveEach = 5;  // places of a thread: 64 vectors of at most 17 groups, 1088, in 5 x 256
 
-struct MoveGroup {
-  uint32_t v[4];
+typedef unsigned int words4 __attribute__((ext_vector_type(4), aligned(4)));
+struct MovePlace {
+  int row = 64, at = 0, w = 0, begin = 0;  // vector of the tile, first word of the four in it, the stream
+  __device__ __forceinline__ MovePlace(const MoveArgs& a, int pool, int e) {
+    if (e >= a.threads[pool]) return;
+    MoveStream s = a.s[pool][0];
+#pragma unroll
+    for (int i = 1; i < 3; ++i)
+      if (i < a.n_streams[pool] && e >= a.s[pool][i].first) s = a.s[pool][i];
+    e -= s.first;
+    row = (int)((uint32_t)e * s.inv >> 18);
+    at = max(min(4 * (e - row * s.groups), s.w - 4), 0);
+    w = s.w;
+    begin = s.begin;
+  }
+  __device__ __forceinline__ void load(const uint32_t* from, words4& v) const {
+    if (w >= 4) {
+      v = __builtin_nontemporal_load(reinterpret_cast<const words4*>(from + at));  // read once: 164 -> 155 us for 32 layers
+    } else {
+      v.x = from[0];
+      v.y = w > 1 ? from[1] : 0u;
+      v.z = w > 2 ? from[2] : 0u;
+    }
+  }
+  __device__ __forceinline__ void store(uint32_t* to, words4 v) const {
+    if (w >= 4) {
+      *reinterpret_cast<words4*>(to + at) = v;
+    } else {
+      to[0] = v.x;
+      if (w > 1) to[1] = v.y;
+      if (w > 2) to[2] = v.z;
+    }
+  }
 };
-
-// The words of group q of one pool's part: gathered from the vectors that stay.  src: first word of the pool's part of the
-// tile that vector r of the destination comes from; row: its place there.
-__device__ __forceinline__ MoveGroup move_load(const MoveArgs& a, int pool, int q, const uint32_t* const* src, const int* row,
-                                               int rows) {
-  MoveGroup m;
-  const int word = 4 * q;
-  MoveStream s = a.s[pool][0];
-#pragma unroll
-  for (int i = 1; i < 3; ++i)
-    if (i < a.n_streams[pool] && word >= a.s[pool][i].begin) s = a.s[pool][i];
-  const uint32_t e = (uint32_t)(word - s.begin);
-  int r = (int)(e * s.inv >> 18), c = (int)e - r * s.w;
-  if (c + 4 <= s.w && r < rows) {
-    typedef unsigned int words4 __attribute__((ext_vector_type(4), aligned(4)));
-    const words4 v = *reinterpret_cast<const words4*>(src[r] + s.begin + row[r] * s.w + c);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m.v[i] = v[i];
-    return m;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    m.v[i] = 0;
-    if (r < rows) m.v[i] = src[r][s.begin + row[r] * s.w + c];
-    if (++c == s.w) { c = 0; ++r; }
-  }
-  return m;
-}
-
-__device__ __forceinline__ void move_store(const MoveArgs& a, int pool, int q, uint32_t* dst, const MoveGroup& m, int rows) {
-  const int word = 4 * q;
-  MoveStream s = a.s[pool][0];
-#pragma unroll
-  for (int i = 1; i < 3; ++i)
-    if (i < a.n_streams[pool] && word >= a.s[pool][i].begin) s = a.s[pool][i];
-  const int left = s.begin + rows * s.w - word;  // words of the stream from here on that belong to the vectors moved
-  if (left >= 4) {
-    *reinterpret_cast<uint4*>(dst + word) = make_uint4(m.v[0], m.v[1], m.v[2], m.v[3]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-      if (i < left) dst[word + i] = m.v[i];
-  }
-}
 
 // blockIdx.y: K heads, then V heads; blockIdx.z: 2 * layer + pool.  IN_PLACE: one workgroup takes all tiles of a head in
 // order, tile i being read whole before it is written.  Position i moves to or before the place it comes from (the
 // indices ascend), so a tile is never written before a later one has been read from it.
 template <bool IN_PLACE>
-__global__ __launch_bounds__(kMoveThreads) void move_kernel(MoveArgs a) {
+__global__ __launch_bounds__(kMoveThreads, 8) void move_kernel(MoveArgs a) {
   __shared__ const uint32_t* src[64];
   __shared__ int row[64];
   const KvGeom& g = a.g;
@@ -277,7 +267,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_kernel(MoveArgs a) {
     const size_t tile = (((size_t)(a.layer0 + layer) * g.n_pages + page) * 2 + kv) * g.n_kv_heads + head;
     return a.pool[pool] + tile * a.tile_words[pool];
   };
-  const int tiles = (a.n_keep + 63) / 64, groups = a.words[pool] / 4;
+  const int tiles = (a.n_keep + 63) / 64;
   for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
     const int rows = min(64, a.n_keep - 64 * t);
     if (tid < 64) {
@@ -286,20 +276,20 @@ __global__ __launch_bounds__(kMoveThreads) void move_kernel(MoveArgs a) {
       row[tid] = p & 63;
     }
     __syncthreads();
-    MoveGroup m[kMoveGroups];
+    words4 v[kMoveEach];
 #pragma unroll
-    for (int i = 0; i < kMoveGroups; ++i) {
-      const int q = tid + i * kMoveThreads;
-      if (q < groups) m[i] = move_load(a, pool, q, src, row, rows);
+    for (int i = 0; i < kMoveEach; ++i) {
+      const MovePlace m(a, pool, tid + i * kMoveThreads);
+      if (m.row < rows) m.load(src[m.row] + m.begin + row[m.row] * m.w, v[i]);
     }
     if (IN_PLACE) __syncthreads();  // the whole tile is in registers
     const int page = a.dst_row[t];
     if (page >= 0 && page < g.n_pages) {
-      uint32_t* dst = part(page);
+      uint32_t* const dst = part(page);
 #pragma unroll
-      for (int i = 0; i < kMoveGroups; ++i) {
-        const int q = tid + i * kMoveThreads;
-        if (q < groups) move_store(a, pool, q, dst, m[i], rows);
+      for (int i = 0; i < kMoveEach; ++i) {
+        const MovePlace m(a, pool, tid + i * kMoveThreads);
+        if (m.row < rows) m.store(dst + m.begin + m.row * m.w, v[i]);
       }
     }
     __syncthreads();  // the table of this tile is done with, and its words are written
@@ -317,8 +307,9 @@ static int launch_select(cas_ctx* ctx, const SelectArgs& a, int n_rows) {
 
 static void add_stream(MoveArgs& a, int pool, int begin, int w) {
   if (w == 0) return;
-  a.s[pool][a.n_streams[pool]++] = MoveStream{begin, w, ((1u << 18) + (uint32_t)w - 1u) / (uint32_t)w};
-  a.words[pool] = begin + 64 * w;
+  const int groups = (w + 3) / 4;
+  a.s[pool][a.n_streams[pool]++] = MoveStream{begin, w, a.threads[pool], groups, ((1u << 18) + (uint32_t)groups - 1u) / (uint32_t)groups};
+  a.threads[pool] += 64 * groups;
 }
 
 static int launch_evict(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, int seq, int dst_seq, const int32_t* d_index, int n_keep) {
