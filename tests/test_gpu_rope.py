@@ -164,6 +164,24 @@ def test_in_place_padding_and_positions_outside(env):
     assert B.cas_rope(ctx, table, [x[:0]])[0].shape == (0, 4, 128)
 
 
+@pytest.mark.parametrize("pad", [0, 1])
+def test_tokens_far_apart(env, pad):
+    """Two tokens more than 2^32 bytes apart, on the aligned and on the other path."""
+    torch, B, ctx = env
+    table = B.cas_rope_table(ctx, B.cas_rope_cfg(128, 0, 10000.0, 1.0, 0, 0.0, 0.0, 1.0), 0, 20)
+    ld = (1 << 31) + 8 + pad
+    far = torch.empty(ld + 256, dtype=torch.bfloat16, device="cuda")
+    x = far.as_strided((2, 2, 128), (ld, 128, 1))
+    x.copy_(torch.randn(2, 2, 128, device="cuda"))
+    near = x.contiguous()
+    want = B.cas_rope(ctx, table, [near], pos0=5)[0]
+    B.cas_rope(ctx, table, [x], pos0=5, outs=[x])
+    torch.cuda.synchronize()
+    assert torch.equal(x.contiguous(), want)
+    del far, x
+    torch.cuda.empty_cache()
+
+
 def test_infinities_and_nan_stay_in_their_pair(env):
     torch, B, ctx = env
     table = B.cas_rope_table(ctx, B.cas_rope_cfg(128, 0, 10000.0, 1.0, 0, 0.0, 0.0, 1.0), 0, 20)

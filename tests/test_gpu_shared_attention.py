@@ -115,6 +115,10 @@ SHARED = [  # n_kv, group, prefix, tails, columns, in flight, full, keep, t, mod
     (8, 8, 12900, [5, 3, 0, 1], [5, 5, 5, 5], [5, 5, 5, 5], True, 600, 4, 2),
     (4, 8, 20000, [0, 100, 7], [6, 6, 6], [6, 6, 6], False, 500, 1, 0),
     (8, 4, 0, [9000, 100], [5, 1], [5, 1], True, 600, 4, 0),
+    # 4096 query rows of a kv head; shared exponents at the other truncations
+    (2, 8, 130, [1] * 31 + [40], [16] * 32, [16] * 32, False, 600, 4, 0),
+    (2, 4, 128, [30, 7], [2, 3], [2, 3], True, 600, 0, 2), (2, 4, 128, [30, 7], [2, 3], [2, 3], False, 600, 3, 2),
+    (2, 4, 128, [30, 7], [2, 3], [2, 3], True, 700, 6, 2), (2, 4, 128, [30, 7], [2, 3], [2, 3], True, 500, 7, 2),
 ]
 
 
@@ -167,6 +171,79 @@ def test_infinities_a_column_does_not_see(env):
         ref, tol, _, _ = _reference(torch, B, ctx, kv, 0, s, True, Q[s], Kn[s], Vn[s])
         _check(torch, outs[s], ref, tol, s)
     assert torch.equal(outs[0][:2], clean[0][:2]) and torch.equal(outs[1][:2], clean[1][:2])
+
+
+def test_infinities_of_keys(env):
+    """In-flight keys with infinities: NaN for the rows that see them (or weight 0), the other columns as without."""
+    torch, B, ctx = env
+    kv = _cache(torch, B, ctx, 2, 64, [61, 5])
+    Q, Kn, Vn = _inputs(torch, 2, [4, 4], [5, 4], 8, 2)
+    Q[0], Q[1] = Q[0].abs(), Q[1].abs()
+    clean = B.cas_attention_shared(ctx, kv, 0, [0, 1], 64, True, Q, Kn, Vn)
+    Kn[0][3, 0, 17], Kn[1][2, 1, 64] = math.inf, -math.inf      # scores of +inf and of -inf
+    outs = B.cas_attention_shared(ctx, kv, 0, [0, 1], 64, True, Q, Kn, Vn)
+    torch.cuda.synchronize()
+    for s in (0, 1):
+        ref, tol, _, _ = _reference(torch, B, ctx, kv, 0, s, True, Q[s], Kn[s], Vn[s])
+        _check(torch, outs[s], ref, torch.where(torch.isfinite(tol), tol, 2.0 ** -6 * ref.abs() + 1e-2), s)
+        assert torch.equal(outs[s][:2], clean[s][:2])
+    assert bool(torch.isnan(outs[0][2:, :4].float()).all()) and bool(torch.isfinite(outs[1].float()).all())
+
+
+def test_order_of_sequences_and_copies_of_the_prefix(env):
+    """The prefix is read through the first sequence's pages: the others may have copies of it, or pages of nothing."""
+    torch, B, ctx = env
+    n_kv, P, tails = 2, 200, [40, 3, 100]
+    kv = B.KVCache(ctx, 1, n_kv, 24, 3, 8, page_table=torch.randperm(24, dtype=torch.int32).view(3, 8))
+    K, V = synth.kv_tensor(P, n_kv, 128, seed=1), synth.kv_tensor(P, n_kv, 128, seed=2, outlier_channels=0)
+    for s, n in enumerate(tails):
+        k = np.concatenate([K, synth.kv_tensor(n, n_kv, 128, seed=20 + s)])
+        v = np.concatenate([V, synth.kv_tensor(n, n_kv, 128, seed=60 + s, outlier_channels=0)])
+        B.cas_kv_append(ctx, kv, 0, s, _bits(torch, k), _bits(torch, v))
+        B.cas_kv_set_len(kv, s, P + n)
+    Q, Kn, Vn = _inputs(torch, 3, [2, 1, 3], [2, 1, 4], 8, n_kv)
+    for order in ([0, 1, 2], [2, 0, 1], [1, 2], [2]):
+        outs = B.cas_attention_shared(ctx, kv, 0, order, P, True, [Q[s] for s in order], [Kn[s] for s in order], [Vn[s] for s in order])
+        torch.cuda.synchronize()
+        for s, o in zip(order, outs):
+            ref, tol, _, _ = _reference(torch, B, ctx, kv, 0, s, True, Q[s], Kn[s], Vn[s])
+            _check(torch, o, ref, tol, (order, s))
+
+
+def test_a_cache_beyond_32_bits(env):
+    """Pools of more than 2^32 words: shared attention, weights and an eviction in the last layer, on the last pages."""
+    torch, B, ctx = env
+    layers, n_kv, pages = 190, 8, 1100
+    kv = B.KVCache(ctx, layers, n_kv, pages, 3, 4, keep_permille=600, trunc_bits=4,
+                   page_table=torch.tensor([[1099, 1090, 1098, 1], [1099, 1090, 1097, 2], [1095, 1094, 0, 3]], dtype=torch.int32))
+    assert min(kv.desc.spec_pool_bytes, kv.desc.verif_pool_bytes) > 4 << 32
+    layer, P, tails = layers - 1, 128, [30, 9]
+    K, V = synth.kv_tensor(P, n_kv, 128, seed=1), synth.kv_tensor(P, n_kv, 128, seed=2, outlier_channels=0)
+    for s, n in enumerate(tails):
+        k = np.concatenate([K, synth.kv_tensor(n, n_kv, 128, seed=20 + s)])
+        v = np.concatenate([V, synth.kv_tensor(n, n_kv, 128, seed=60 + s, outlier_channels=0)])
+        B.cas_kv_append(ctx, kv, layer, s, _bits(torch, k), _bits(torch, v))
+        B.cas_kv_set_len(kv, s, P + n)
+    Q, Kn, Vn = _inputs(torch, 2, [2, 1], [2, 1], 16, n_kv)
+    outs = B.cas_attention_shared(ctx, kv, layer, [0, 1], P, True, Q, Kn, Vn)
+    o, w = B.cas_attention_weights(ctx, kv, layer, 0, False, Q[0], Kn[0], Vn[0])
+    torch.cuda.synchronize()
+    for s in (0, 1):
+        ref, tol, _, _ = _reference(torch, B, ctx, kv, layer, s, True, Q[s], Kn[s], Vn[s])
+        _check(torch, outs[s], ref, tol, s)
+    ref, tol, want, wt = _reference(torch, B, ctx, kv, layer, 0, False, Q[0], Kn[0], Vn[0])
+    _check(torch, o, ref, tol, "weights")
+    assert bool(((w.double() - want).abs() <= wt).all())
+    index = B.cas_kv_select(ctx, w, P + 30, 70, 4, 10).view(1, n_kv, 70)
+    B.cas_kv_evict(ctx, kv, layer, 1, 0, 2, index)
+    B.cas_kv_set_len(kv, 2, 70)
+    a, b = B.cas_kv_read(ctx, kv, layer, 0, 0, P + 30, True), B.cas_kv_read(ctx, kv, layer, 2, 0, 70, True)
+    torch.cuda.synchronize()
+    for x, y in zip(a, b):
+        for h in range(n_kv):
+            assert torch.equal(y[:, h], x[index[0, h].long(), h])
+    del kv
+    torch.cuda.empty_cache()
 
 
 def test_shared_agrees_with_attention_per_sequence(env):
