@@ -8,9 +8,13 @@ namespace cas {
 
 // ---- selection ----------------------------------------------------------------------------------
 // One workgroup per row.  The scores between the first and the last positions are mapped to integers of the same order;
-// the threshold (the highest value that enough of them reach) is found two bits at a time by counting, and of its equals
+// the threshold (the highest value that enough of them reach) is found kSelBits at a time by counting, and of its equals
 // the lower positions are taken.  Kept positions are dealt their places by counting those before them: ballots within a
 // wave, one table of counts per wave and step for the workgroup.
+// Bound by latency: 16 turns of ballots, an addition in LDS and a barrier.  8 rows of 2049 scores take 11 us, 256 rows of 8192
+// 20 (8 MB read and 4 written: 3 at the rate of a copy).  Of a selection and the move of a layer behind it, with 1 / 2 / 4 bits a turn:
+// 23.3 / 21.1 / 24.0 us; four are half the turns and 2.5 times the ballots.
+constexpr int kSelBits = 2;
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 
 __device__ __forceinline__ uint32_t score_key(float v) {  // NaN on top, -0 as +0; 0 is below every key
@@ -35,7 +39,8 @@ template <int PER>
 __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
   constexpr int N = PER > 0 ? PER : 1;
   constexpr int kAhead = 8;  // scores requested at once where they are read again
-  __shared__ uint32_t cnt[3][4];
+  constexpr int kCounts = (1 << kSelBits) - 1;
+  __shared__ uint32_t cnt[3][kCounts + 1];
   __shared__ uint32_t place[PER > 0 ? PER * kSelWaves : 2 * kSelWaves];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float* row = a.score + (int64_t)blockIdx.x * a.ld;
@@ -60,7 +65,7 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) key[i] = key_of(i, v[i]);
   }
-  if (tid < 12) (&cnt[0][0])[tid] = 0;
+  if (tid < 3 * (kCounts + 1)) (&cnt[0][0])[tid] = 0;
   __syncthreads();
   // f(key) of every position, the workgroup's waves together
   auto each = [&](auto&& f) {
@@ -84,27 +89,28 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
   if (want > 0) {
     int set = 0;
     bool exact = false;
-    for (int bit = 30; bit >= -2 && !exact; bit -= 2) {
-      uint32_t n[3] = {0, 0, 0};
-      const uint32_t t1 = bit >= 0 ? T | 1u << bit : T + 1u, t2 = bit >= 0 ? T | 2u << bit : 0u, t3 = bit >= 0 ? T | 3u << bit : 0u;
+    for (int bit = 32 - kSelBits; bit >= -kSelBits && !exact; bit -= kSelBits) {
+      uint32_t n = 0;  // lane c: keys of the wave's that reach T with c + 1 as the next bits; behind the last bit, those above T
       each([&](uint32_t k) {
-        n[0] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t1));
-        n[1] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t2));
-        n[2] += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t3));
+#pragma unroll
+        for (int c = 0; c < kCounts; ++c) {
+          const uint32_t t = bit >= 0 ? T | (uint32_t)(c + 1) << bit : T + 1u;
+          const uint32_t reach = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t));  // of all lanes, not in a branch
+          n += lane == c ? reach : 0u;
+        }
       });
-      if (lane < 3) atomicAdd(&cnt[set][lane], lane == 0 ? n[0] : lane == 1 ? n[1] : n[2]);
+      if (lane < kCounts) atomicAdd(&cnt[set][lane], n);
       const int next = set == 2 ? 0 : set + 1;
       __syncthreads();
-      // one value for all lanes, and known to be
-      const uint32_t s0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)cnt[set][0]), s1 = (uint32_t)__builtin_amdgcn_readfirstlane((int)cnt[set][1]),
-                     s2 = (uint32_t)__builtin_amdgcn_readfirstlane((int)cnt[set][2]);
-      if (tid < 4) cnt[next == 2 ? 0 : next + 1][tid] = 0;
+      const uint32_t mine = cnt[set][lane & kCounts];  // lane kCounts: 0
+      if (tid <= kCounts) cnt[next == 2 ? 0 : next + 1][tid] = 0;
       set = next;
       if (bit >= 0) {
-        T = s2 >= want ? t3 : s1 >= want ? t2 : s0 >= want ? t1 : T;
-        exact = s2 == want || (s2 < want && s1 == want) || (s1 < want && s0 == want);
+        const int c = __popcll(__builtin_amdgcn_ballot_w64(lane < kCounts && mine >= want));
+        T |= (uint32_t)c << bit;
+        exact = c > 0 && (uint32_t)__builtin_amdgcn_readlane((int)mine, c - 1) == want;
       } else {
-        above = T == 0xFFFFFFFFu ? 0u : s0;
+        above = T == 0xFFFFFFFFu ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)mine);
       }
     }
     if (exact) {  // those that reach T are those that stay: none is equal to one below it
@@ -124,8 +130,10 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     const uint32_t t_rank = t_before + (uint32_t)__popcll(mt & below);
     if (sure || (tie && t_rank < ties)) {
       const uint32_t at = s_before + (uint32_t)__popcll(ms & below) + min(t_rank, ties);
-      index[at] = i * kSelThreads + tid;
-      if (kept) kept[at] = x;
+      if (at < (uint32_t)a.n_keep) {  // also where scores change meanwhile
+        index[at] = i * kSelThreads + tid;
+        if (kept) kept[at] = x;
+      }
     }
   };
   if constexpr (PER > 0) {
@@ -194,8 +202,9 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
 // A tile (64 vectors of one head) is two runs of words, its parts of the two pools, each made of streams of w words per
 // vector in vector order.  A thread moves four words of a vector, the last four of a stream where fewer are left (two threads then
 // write the same words): one load and one store of 16 bytes each, on multiples of 4 bytes, for every stream of four words
-// or more.  With 16 bytes of the destination to a thread, which may reach into the next vector, a quarter of the threads needs
-// four loads, and their waves five: what a CU's address unit then takes was most of 32 layers' 175 us.
+// or more.  Bound by latency and address units.  With 16 bytes of the destination to a thread, which may reach into the next
+// vector, a quarter of the threads needs four loads, and their waves five: 175 us for 32 layers of 2048 of 8192 positions
+// (549 MB read and written: 115 at the rate of a copy), now 142.
 struct MoveStream {
   int begin, w;       // first word in the pool's part of a tile, words of a vector
   int first, groups;  // threads before, and to a vector
@@ -234,7 +243,7 @@ struct MovePlace {
   }
   __device__ __forceinline__ void load(const uint32_t* from, words4& v) const {
     if (w >= 4) {
-      v = __builtin_nontemporal_load(reinterpret_cast<const words4*>(from + at));  // read once: 164 -> 155 us for 32 layers
+      v = __builtin_nontemporal_load(reinterpret_cast<const words4*>(from + at));  // read once: 148 -> 143 us for those
     } else {
       v.x = from[0];
       v.y = w > 1 ? from[1] : 0u;
