@@ -457,10 +457,12 @@ int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout,
  * for the vectors being the same.  Arguments as for cas_attention_multi, except that a sequence may bring up to
  * 16 columns, and a kv head have up to 48 query heads, in both forms.
  * Outputs are those of cas_attention within its tolerance, not bit for bit: pages are added in runs whose length
- * depends on prefix_len, the heads, and the numbers of sequences and columns.  A sequence's values do not depend on what the other sequences hold behind the prefix, nor on how long they are.
+ * depends on prefix_len, the heads, and the numbers of sequences and columns.  A sequence's values do not depend
+ * on what the other sequences hold behind the prefix, nor on how long they are.
  * Workspace: cas_attention_shared_bytes (host only; 0 for arguments that cas_attention_shared refuses).  Like
  * every call that uses the context's workspace, two of them that may overlap (two streams, two captured
- * graphs replayed side by side) need contexts with workspaces of their own.  CAS_EINVAL unless the context's device is current.
+ * graphs replayed side by side) need contexts with workspaces of their own.  CAS_EINVAL unless the context's
+ * device is current.
  */
 int cas_attention_shared(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const int32_t* h_seqs, int prefix_len,
                          int full, const uint16_t* const* h_d_Q, const int32_t* h_ncols, int n_q_heads,
@@ -480,8 +482,9 @@ size_t cas_attention_shared_bytes(const cas_kv* kv, int n_seqs, const int32_t* h
  * = NULL stands for zeros.  What stands behind the committed length in d_score_in is not read: the sums of
  * in-flight positions that were not accepted are gone with them, those of accepted ones are kept.  Every
  * column of the call counts, also one that is rejected later.  Entries from len + n_new on stay as they were.
- * Other arguments, outputs and workspace rules as for cas_attention_shared (workspace: cas_attention_weights_bytes, host only;
- * 0 for arguments that cas_attention_weights refuses).  Sums are fp32 in a fixed order.
+ * Other arguments, outputs and workspace rules as for cas_attention_shared (workspace:
+ * cas_attention_weights_bytes, host only; 0 for arguments that cas_attention_weights refuses).  Sums are fp32 in a
+ * fixed order.
  */
 int cas_attention_weights(cas_ctx* ctx, cas_kv* kv, int layer, int seq, int full, const uint16_t* d_Q, int ncols,
                           int n_q_heads, const uint16_t* d_Knew, const uint16_t* d_Vnew, int n_new, uint16_t* d_O,
@@ -494,17 +497,18 @@ size_t cas_attention_weights_bytes(const cas_kv* kv, int seq, int ncols, int n_q
  * d_index: int32 [n_rows][n_keep], positions in ascending order.  d_kept: NULL or float [n_rows][ld_kept],
  * receives the scores of the kept positions (ld_kept >= n_keep); it may be d_score itself with ld_kept = ld,
  * whose entries from n_keep on then stay as they were.  0 <= n_first, n_last; n_first + n_last <= n_keep <= len.
- * CAS_EINVAL unless the context's device is current. */
+ * len <= 2^30 (CAS_ENOTSUP above).  CAS_EINVAL unless the context's device is current. */
 int cas_kv_select(cas_ctx* ctx, const float* d_score, int64_t ld, int n_rows, int len, int n_keep, int n_first,
                   int n_last, int32_t* d_index, float* d_kept, int64_t ld_kept);
 
 /* Moves the vectors that stay: in n_layers layers from layer0 on, position i of kv head g of dst_seq
  * becomes position d_index[layer - layer0][g][i] of seq, K and V, still encoded as they are; i < n_keep,
  * d_index: int32 [n_layers][n_kv_heads][n_keep], clamped into 0 .. len(seq)-1.  dst_seq = seq moves in
- * place, for which the indices of a head have to ascend strictly, as cas_kv_select writes them; otherwise the pages of the
- * two sequences must not be the same, and indices may be in any order and repeat.  Page table entries outside the pool are
- * clamped for reading and not written to.  Nothing behind position n_keep of dst_seq changes, and no length does: cas_kv_set_len(dst_seq,
- * n_keep) once all layers are done.  Pages that other sequences name too (a shared prefix) must not be evicted in place.
+ * place, for which the indices of a head have to ascend strictly, as cas_kv_select writes them; otherwise the
+ * pages of the two sequences must not be the same, and indices may be in any order and repeat.  Page table entries
+ * outside the pool are clamped for reading and not written to.  Nothing behind position n_keep of dst_seq changes,
+ * and no length does: cas_kv_set_len(dst_seq, n_keep) once all layers are done.  Pages that other sequences name too
+ * (a shared prefix) must not be evicted in place.
  * The model passes place a token at the position that the cache's length gives; after an eviction use the
  * stand-alone calls, with cas_rope at the positions that the tokens have.  CAS_EINVAL unless the context's device is current. */
 int cas_kv_evict(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, int seq, int dst_seq, const int32_t* d_index,

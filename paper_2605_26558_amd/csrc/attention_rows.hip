@@ -12,6 +12,12 @@
 // Attention weights: the partial kernel also writes the exponents of its scores, and the second launch, beside joining the
 // rows, forms the weights of all rows of a kv head from them and adds them up.  Exponents are 4 bytes per row and position,
 // a vector of K 131 in the draft form: cheaper than decoding K again.
+//
+// Measured (8 kv heads, 60 % kept, t = 4; both launches; in brackets the bytes of the streams at the rate of a copy): 16 sequences
+// of 4 query heads a kv head over a shared 8192 and 500 of their own, draft 30 us (5.5); 8 of 5 columns, exact, 300 of
+// their own 43 (8.9); 32 of 8 query heads over 32768, exact, shared exponents 130 (29).  One sequence with weights: 8192 positions,
+// exact 22 us (7.7), 30011 and 7 columns 55 (28).  Bound by the vector operations of the decode: 63 to 71 % of a
+// SIMD's cycles, the matrix products and the LDS beside them (LDS busy 49 % of the time with 256 rows).
 #include <algorithm>
 #include "attention_rows_kernel.inl"
 
@@ -229,7 +235,10 @@ __global__ __launch_bounds__(256) void rows_merge_weights_kernel(RowsArgs a, int
 
 // ---- host ---------------------------------------------------------------------------------------
 // A prefix (or a sequence on its own) is cut into as many runs as there are workgroups at a time, two of eight waves or one of
-// sixteen a CU; behind a prefix runs have a fixed length, so that a sequence's values do not depend on the others' lengths.
+// sixteen a CU (slots for 128 / 192 / 256 / 512 CUs: 32 sequences over 32768 positions 164 / 122 / 120 / 141 us, 8 over 8192
+// 44.7 / 40.1 / 45.5 / 64); behind a prefix runs have a fixed length, so that a sequence's values do not depend on the others'
+// lengths: two pages, a step of sixteen waves (longer ones: 2 short sequences 11.8 -> 13.3 us, 8 over 8192 positions 45.8
+// -> 48.9, 32 over 32768 119 -> 114).
 constexpr int kCus = 256;
 constexpr int kTailRun = 2;
 
@@ -244,8 +253,8 @@ struct RowsPlan {
 // workgroups behind them.  As many runs as there are workgroups at a time; or fewer, so that the others start with them,
 // where that lengthens the runs by less than the others would take afterwards (some five steps: three before the first
 // products and behind the last, two of their own).  us with all / room for a workgroup a sequence and head: 16 sequences over
-// 8192 positions, draft 33.1 / 30.0, 8 sequences of 5 columns 45.5 / 40.1; 4 sequences of 64 query heads over 32768 positions
-// the same run either way.
+// 8192 positions, draft 33.1 / 30.0, 8 sequences of 5 columns 45.5 / 40.1; 32 sequences of 64 query heads over 32768 positions
+// take the same run either way.
 static int run_of(int64_t pages, int64_t columns, int64_t others, int tiles) {
   const int step = tiles == 16 ? 2 : 1;
   const int64_t slots = 2 / step * kCus;
@@ -295,6 +304,8 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   }
   a.rows = (int)rows;
   if (a.prefix_pages > 0) most = a.rows;
+  // Room for all rows of a decoded page, up to 256.  Smaller workgroups at the limits, us: 8 tiles above 128 rows 45 -> 62 (160
+  // rows), 119 -> 147 (256); larger ones: 4 tiles above 16 rows 56 -> 62 (28 rows), 8 above 48 33 -> 36 (64).
   p.tiles = most <= 32 ? 2 : most <= 64 ? 4 : most <= 128 ? 8 : 16;
   const int block = 16 * p.tiles;
   if (a.prefix_pages > 0) {
@@ -318,7 +329,7 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   for (int i = n_seqs; i < kRowsSeqs; ++i) a.row0[i] = a.item0[i] = 0x7FFFFFFF;
   const int64_t first = (int64_t)a.prefix_splits * g.n_kv_heads * a.rows;
   items += a.prefix_items;
-  if (items * g.n_kv_heads > 0x7FFFFFFF) return CAS_ENOTSUP;
+  if (items * g.n_kv_heads > 0x3FFFFF) return CAS_ENOTSUP;  // a launch has fewer than 2^32 threads
   p.items = (int)items;
   // workspace: outputs, pairs, and the exponents of the rows
   int64_t off = up256((first + parts) * 512);
