@@ -8,6 +8,8 @@ namespace cas {
 
 typedef short rows_s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 rows_bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 rows_bf16x2 __attribute__((ext_vector_type(2)));
+typedef float rows_f32x2 __attribute__((ext_vector_type(2)));
 typedef float rows_f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int rows_u32x4 __attribute__((ext_vector_type(4)));
 
@@ -124,6 +126,17 @@ __device__ __forceinline__ void lds_write(uint32_t base, int i, int pitch, uint1
   uint32_t at;
   asm("v_mad_i32_i24 %0, %1, %2, %3" : "=v"(at) : "v"(i), "s"(pitch), "v"(base));
   *(lds_u16*)(uintptr_t)at = v;
+}
+
+// What the heads of two numbers leave of them, rounded to bf16: a product of two elements subtracts a head in one operation
+// where it lies (its other element times 0), one conversion takes both.
+__device__ __forceinline__ uint32_t bf16_rests(uint32_t heads, float lo, float hi) {
+  uint32_t minus_lo = 0x0000BF80u, minus_hi = 0xBF800000u;
+  asm("" : "+s"(minus_lo), "+s"(minus_hi));  // in registers: as constants of the instruction both came out as the upper one
+  const rows_bf16x2 h = __builtin_bit_cast(rows_bf16x2, heads);
+  const rows_f32x2 d = {__builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(rows_bf16x2, minus_lo), lo, false),
+                        __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(rows_bf16x2, minus_hi), hi, false)};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(d, rows_bf16x2));
 }
 
 // The N words of a window, the last ones only if a lane of the wave has fields there.  A scattered load takes a CU's address
@@ -387,17 +400,16 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
     uint32_t h[2 * NS], rest[2 * NS];
 #pragma unroll
     for (int tt = 0; tt < NS; ++tt) {
-      float w[4], d[4];
+      float w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         w[e] = __builtin_amdgcn_exp2f(fmaf(x[tt][e], a.scale2, -top));
         l += w[e];
-        d[e] = w[e] - __uint_as_float(__float_as_uint(w[e]) & 0xFFFF0000u);
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         h[2 * tt + i] = __builtin_amdgcn_perm(__float_as_uint(w[2 * i + 1]), __float_as_uint(w[2 * i]), 0x07060302u);
-        rest[2 * tt + i] = (uint32_t)f32_to_bf16(d[2 * i]) | ((uint32_t)f32_to_bf16(d[2 * i + 1]) << 16);
+        rest[2 * tt + i] = bf16_rests(h[2 * tt + i], w[2 * i], w[2 * i + 1]);
       }
     }
     // outputs: value e of o[ct] is channel 32 e + 8 mq + (ct ^ (mq & 1))
