@@ -685,7 +685,7 @@ def cas_rope(ctx: Context, table, xs, pos=None, pos0=0, layout=CAS_ROPE_HALF, tr
         shape, (ldx, head, one), fp32 = x.shape, x.stride(), x.dtype == torch.float32
         heads = shape[1]
         if outs is None:
-            y = torch.empty(shape, dtype=torch.int16 if fp32 else x.dtype, device=x.device)
+            y = torch.empty_like(x, dtype=torch.int16 if fp32 else None, memory_format=torch.contiguous_format)
             ldy = heads * dim
         else:
             y = outs[i]
