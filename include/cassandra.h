@@ -459,6 +459,8 @@ int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout,
  * Outputs are those of cas_attention within its tolerance, not bit for bit: pages are added in runs whose length
  * depends on prefix_len, the heads, and the numbers of sequences and columns.  A sequence's values do not depend
  * on what the other sequences hold behind the prefix, nor on how long they are.
+ * Infinities and NaN of in-flight vectors reach the columns that see them only; an infinity among the committed V
+ * of a sequence makes its channel infinite or NaN, as in cas_attention.
  * Workspace: cas_attention_shared_bytes (host only; 0 for arguments that cas_attention_shared refuses).  Like
  * every call that uses the context's workspace, two of them that may overlap (two streams, two captured
  * graphs replayed side by side) need contexts with workspaces of their own.  CAS_EINVAL unless the context's
