@@ -457,7 +457,7 @@ int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout,
  * for the vectors being the same.  Arguments as for cas_attention_multi, except that a sequence may bring up to
  * 16 columns, and a kv head have up to 48 query heads, in both forms.
  * Outputs are those of cas_attention within its tolerance, not bit for bit: pages are added in runs whose length
- * depends on prefix_len, the heads, and the numbers of sequences and columns.  A sequence's values do not depend
+ * depends on prefix_len, the sequence's own length, the heads, and the numbers of sequences and columns.  A sequence's values do not depend
  * on what the other sequences hold behind the prefix, nor on how long they are.
  * Infinities and NaN of in-flight vectors reach the columns that see them only; an infinity among the committed V
  * of a sequence makes its channel infinite or NaN, as in cas_attention.

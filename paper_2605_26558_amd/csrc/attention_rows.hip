@@ -236,11 +236,9 @@ __global__ __launch_bounds__(256) void rows_merge_weights_kernel(RowsArgs a, int
 // ---- host ---------------------------------------------------------------------------------------
 // A prefix (or a sequence on its own) is cut into as many runs as there are workgroups at a time, two of eight waves or one of
 // sixteen a CU (slots for 128 / 192 / 256 / 512 CUs: 32 sequences over 32768 positions 164 / 122 / 120 / 141 us, 8 over 8192
-// 44.7 / 40.1 / 45.5 / 64); behind a prefix runs have a fixed length, so that a sequence's values do not depend on the others'
-// lengths: two pages, a step of sixteen waves (longer ones: 2 short sequences 11.8 -> 13.3 us, 8 over 8192 positions 45.8
-// -> 48.9, 32 over 32768 119 -> 114).
+// 44.7 / 40.1 / 45.5 / 64); the length of the runs behind a prefix does not depend on the other sequences' lengths, so that a
+// sequence's values do not either.
 constexpr int kCus = 256;
-constexpr int kTailRun = 2;
 
 struct RowsPlan {
   RowsArgs a;
@@ -267,6 +265,18 @@ static int run_of(int64_t pages, int64_t columns, int64_t others, int tiles) {
   return (int)all;
 }
 
+// Pages of a run of a sequence's own positions, behind the prefix; `columns` as above, of all sequences.  It depends on this
+// sequence's length and on the numbers of the others.  A step where that leaves workgroups free, otherwise two, which share a start
+// and an end; more where there are so many that all places are taken twice, up to four (or 32 runs); and no more than 64
+// runs, a table of the merge's.  us, runs of two pages throughout / this: 2 sequences of 90 behind 703 positions 11.8 / 10.3; 32 of
+// 1000 behind 2000 45.2 / 43.8; 8 of 16000 behind 1000 94 / 73; one of 9000 21.3 / 18.0, of 60000 98 / 65.
+static int tail_run_of(int64_t pages, int64_t columns, int tiles) {
+  const int step = tiles == 16 ? 2 : 1;
+  const int64_t slots = 2 / step * kCus, steps = (pages + step - 1) / step;
+  const int64_t least = std::max(steps, (int64_t)2) * columns >= slots ? 2 : 1, most = std::max<int64_t>(4, (steps + 31) / 32);
+  return (int)std::max({least, std::min(most, steps * columns / (2 * slots)), (steps + 63) / 64}) * step;
+}
+
 static int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 
 // What a call will launch and need; Q, Knew, Vnew and O are left to the caller.
@@ -285,7 +295,6 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   a.scale2 = (float)(1.4426950408889634 * 0.08838834764831845);
   a.n_seqs = n_seqs;
   a.prefix_pages = prefix_len / 64;
-  a.tail_run = kTailRun;
   int64_t rows = 0, parts = 0, items = 0;
   int most = 0, pages[kRowsSeqs];
   for (int i = 0; i < n_seqs; ++i) {
@@ -316,13 +325,14 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
     a.prefix_splits = (a.prefix_pages + a.prefix_run - 1) / a.prefix_run;
     a.prefix_items = a.prefix_splits * blocks;
   }
-  if (weights) a.tail_run = run_of(pages[0], (int64_t)g.n_kv_heads * ((a.rows + block - 1) / block), 0, p.tiles);
   for (int i = 0; i < n_seqs; ++i) {
     const int r = ncols[i] * a.grp;
-    a.splits[i] = (pages[i] - a.prefix_pages + a.tail_run - 1) / a.tail_run;
+    const int64_t tail = pages[i] - a.prefix_pages, blocks = (r + block - 1) / block;
+    a.run[i] = weights ? run_of(tail, g.n_kv_heads * blocks, 0, p.tiles) : tail_run_of(tail, (int64_t)n_seqs * g.n_kv_heads * blocks, p.tiles);
+    a.splits[i] = (int)((tail + a.run[i] - 1) / a.run[i]);
     a.item0[i] = (int)items;
     a.part0[i] = (uint32_t)parts;
-    items += (int64_t)a.splits[i] * ((r + block - 1) / block);
+    items += a.splits[i] * blocks;
     parts += (int64_t)a.splits[i] * g.n_kv_heads * r;
     if (items > 0x7FFFFFFF || parts > 0xFFFFFFFFll) return CAS_ENOTSUP;
   }

@@ -27,7 +27,7 @@ struct RowsArgs {
   uint32_t grp_inv;          // row / grp = row * grp_inv >> 16
   float scale2;              // log2(e) / sqrt(128): scores are kept as exponents of two
   int n_seqs, rows;          // rows: of all sequences
-  int prefix_pages, prefix_run, prefix_splits, prefix_items, tail_run;
+  int prefix_pages, prefix_run, prefix_splits, prefix_items;
   // partial results: 128 outputs each, [split][kv head][row] of the prefix, then the same sequence by sequence; and the
   // pairs (maximum, sum) in the same two regions as [kv head][row][split]
   float* out_prefix;
@@ -46,7 +46,8 @@ struct RowsArgs {
   const uint16_t* Vnew[kRowsSeqs];
   uint16_t* O[kRowsSeqs];
   int seq[kRowsSeqs], len[kRowsSeqs], n_new[kRowsSeqs], ncols[kRowsSeqs];
-  int splits[kRowsSeqs];     // runs of pages behind the prefix
+  int run[kRowsSeqs];        // pages of a run behind the prefix
+  int splits[kRowsSeqs];     // runs
   uint32_t part0[kRowsSeqs]; // partial results (row, run, kv head) behind the prefix, of the sequences before
 };
 
@@ -182,7 +183,7 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
   const int tile = RT == 16 ? wv : u % RT, slab0 = RT >= 8 ? 0 : (u / RT) * NS;   // and the wave's: tile of rows, first slab
 
   // ---- what this workgroup works on (uniform)
-  const SeqTable t_item0(a.item0), t_len(a.len), t_new(a.n_new), t_cols(a.ncols), t_seq(a.seq), t_splits(a.splits), t_part0(a.part0);
+  const SeqTable t_item0(a.item0), t_len(a.len), t_new(a.n_new), t_cols(a.ncols), t_seq(a.seq), t_splits(a.splits), t_part0(a.part0), t_run(a.run);
   const bool prefix = item < a.prefix_items;
   int si = 0;
   if (!prefix) {
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
   const int rows = prefix ? a.rows : t_cols[si] * a.grp, blocks = (rows + 16 * RT - 1) / (16 * RT);
   const int split = item / blocks, row_base = (item - split * blocks) * 16 * RT;
   const int len = prefix ? a.prefix_pages * 64 : t_len[si], total = prefix ? len : len + t_new[si];
-  const int run = prefix ? a.prefix_run : a.tail_run;
+  const int run = prefix ? a.prefix_run : t_run[si];
   const int pg0 = (prefix ? 0 : a.prefix_pages) + split * run, pg1 = min(pg0 + run, (total + 63) / 64), steps = (pg1 - pg0 + kPages - 1) / kPages;
   const int32_t* page_row = a.table + (size_t)t_seq[si] * g.max_pages_per_seq;
   const uint32_t first = prefix ? 0 : (uint32_t)t_part0[si];  // of the partial results

@@ -115,6 +115,10 @@ SHARED = [  # n_kv, group, prefix, tails, columns, in flight, full, keep, t, mod
     (8, 8, 12900, [5, 3, 0, 1], [5, 5, 5, 5], [5, 5, 5, 5], True, 600, 4, 2),
     (4, 8, 20000, [0, 100, 7], [6, 6, 6], [6, 6, 6], False, 500, 1, 0),
     (8, 4, 0, [9000, 100], [5, 1], [5, 1], True, 600, 4, 0),
+    # behind the prefix: runs of two steps, of sixteen waves and of eight; more than 64 steps
+    (8, 4, 100, [130, 300, 5] + [70] * 13, [5] * 16, [5] * 16, True, 600, 4, 0),
+    (8, 2, 70, [500, 300, 5, 129] + [70] * 28, [1] * 32, [1] * 32, False, 600, 4, 0),
+    (1, 2, 64, [8300, 10], [1, 2], [1, 2], False, 600, 4, 0),
     # 4096 query rows of a kv head; shared exponents at the other truncations
     (2, 8, 130, [1] * 31 + [40], [16] * 32, [16] * 32, False, 600, 4, 0),
     (2, 4, 128, [30, 7], [2, 3], [2, 3], True, 600, 0, 2), (2, 4, 128, [30, 7], [2, 3], [2, 3], False, 600, 3, 2),
