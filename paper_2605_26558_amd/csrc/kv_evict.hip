@@ -8,13 +8,14 @@ namespace cas {
 
 // ---- selection ----------------------------------------------------------------------------------
 // One workgroup per row.  The scores between the first and the last positions are mapped to integers of the same order;
-// the threshold (the highest value that enough of them reach) is found kSelBits at a time by counting, and of its equals
-// the lower positions are taken.  Kept positions are dealt their places by counting those before them: ballots within a
-// wave, one table of counts per wave and step for the workgroup.
-// Bound by latency: 16 turns of ballots, an addition in LDS and a barrier.  8 rows of 2049 scores take 11 us, 256 rows of 8192
-// 20 (8 MB read and 4 written: 3 at the rate of a copy).  Of a selection and the move of a layer behind it, with 1 / 2 / 4 bits a turn:
-// 23.3 / 21.1 / 24.0 us; four are half the turns and 2.5 times the ballots.
-constexpr int kSelBits = 2;
+// the threshold (the highest value that enough of them reach) is found kSelBits at a time: counts per digit in LDS, then the
+// digit with which enough are reached by a sum over the counts; and of its equals the lower positions are taken.  Kept positions
+// are dealt their places by counting those before them: ballots within a wave, one table of counts per wave and step for the workgroup.
+// Bound by latency (three passes of five barriers), for long rows by vector issue.  us, also where all scores are equal, and with two
+// bits a turn by ballots instead of digits in LDS: 8 rows of 2049 7.1 / 8.5 / 9.9, of 8192 12.3 / 14.7 / 17, of 21647 27 / 32 / 42;
+// 256 of 8192 14.5 / 15.6 / 19.7 (8 MB read and 4 written: 3 at the rate of a copy).
+constexpr int kSelBits = 11, kSelBins = 1 << kSelBits;
+constexpr int kGroup = 4;  // steps between two looks at the row's end
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 
 __device__ __forceinline__ uint32_t score_key(float v) {  // NaN on top, -0 as +0; 0 is below every key
@@ -31,16 +32,13 @@ struct SelectArgs {
   float* kept;
 };
 
-// Counts of the 16 waves meet in one LDS counter each (integer additions: no order in the result); three sets take turns, so
-// that one barrier a turn is enough: a set is cleared in the turn before it is added to, behind the barrier after which all have read it.
-// PER: scores of a thread kept in registers (as scores and as keys); 0: read again wherever they are needed, rows too
-// long for registers.
+// PER: scores of a thread kept in registers; 0: read again wherever they are needed, rows too long for registers.
 template <int PER>
 __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
   constexpr int N = PER > 0 ? PER : 1;
   constexpr int kAhead = 8;  // scores requested at once where they are read again
-  constexpr int kCounts = (1 << kSelBits) - 1;
-  __shared__ uint32_t cnt[3][kCounts + 1];
+  __shared__ __align__(8) uint32_t bins[kSelBins];
+  __shared__ uint32_t wave_total[kSelWaves], found[3];
   __shared__ uint32_t place[PER > 0 ? PER * kSelWaves : 2 * kSelWaves];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float* row = a.score + (int64_t)blockIdx.x * a.ld;
@@ -54,25 +52,27 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     return p < a.len ? row[p] : 0.f;
   };
   auto key_of = [&](int i, float x) {  // 0 outside the middle
-    const int p = i * kSelThreads + tid;
+    int p = tid;
+    asm volatile("" : "+v"(p));  // worked out anew each time: the places and answers of all steps do not fit the registers
+    p += i * kSelThreads;
     return p >= lo && p < hi ? score_key(x) : 0u;
   };
   float v[N];
-  uint32_t key[N];
-  if constexpr (PER > 0) {
+  if constexpr (PER > 0) {  // 0 behind the row
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(row), 0, 4 * a.len, kRawBufferFlags);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) v[i] = value(i);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) key[i] = key_of(i, v[i]);
+    for (int i = 0; i < PER; ++i) v[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, 4 * tid, 4 * i * kSelThreads, 0));
   }
-  if (tid < 3 * (kCounts + 1)) (&cnt[0][0])[tid] = 0;
-  __syncthreads();
   // f(key) of every position, the workgroup's waves together
   auto each = [&](auto&& f) {
     if constexpr (PER > 0) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (i < steps) f(key[i]);
+      for (int i = 0; i < PER; i += kGroup) {
+        if (i > 0 && i * kSelThreads >= a.len) break;
+#pragma unroll
+        for (int q = 0; q < kGroup; ++q) f(key_of(i + q, v[i + q]));
+        asm volatile("" ::: "memory");
+      }
     } else {
       for (int i = 0; i < steps; i += kAhead) {
         float x[kAhead];
@@ -83,35 +83,45 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
       }
     }
   };
-  // The largest T that at least `want` keys reach, two bits a turn; found early where exactly
-  // `want` keys reach it, otherwise a last turn counts the keys above it.
+  // The largest T that at least `want` keys reach, some bits a pass; found early where exactly `want` keys reach it with the
+  // bits behind as zeros.
   uint32_t T = 0, above = 0;
   if (want > 0) {
-    int set = 0;
     bool exact = false;
-    for (int bit = 32 - kSelBits; bit >= -kSelBits && !exact; bit -= kSelBits) {
-      uint32_t n = 0;  // lane c: keys of the wave's that reach T with c + 1 as the next bits; behind the last bit, those above T
-      each([&](uint32_t k) {
-#pragma unroll
-        for (int c = 0; c < kCounts; ++c) {
-          const uint32_t t = bit >= 0 ? T | (uint32_t)(c + 1) << bit : T + 1u;
-          const uint32_t reach = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= t));  // of all lanes, not in a branch
-          n += lane == c ? reach : 0u;
-        }
-      });
-      if (lane < kCounts) atomicAdd(&cnt[set][lane], n);
-      const int next = set == 2 ? 0 : set + 1;
+    for (int left = 32; left > 0 && !exact;) {  // bits of T that are not known
+      const int next = max(left - kSelBits, 0);
+      const uint32_t mask = (1u << (left - next)) - 1u;
+      for (int i = tid; i < kSelBins; i += kSelThreads) bins[i] = 0;
       __syncthreads();
-      const uint32_t mine = cnt[set][lane & kCounts];  // lane kCounts: 0
-      if (tid <= kCounts) cnt[next == 2 ? 0 : next + 1][tid] = 0;
-      set = next;
-      if (bit >= 0) {
-        const int c = __popcll(__builtin_amdgcn_ballot_w64(lane < kCounts && mine >= want));
-        T |= (uint32_t)c << bit;
-        exact = c > 0 && (uint32_t)__builtin_amdgcn_readlane((int)mine, c - 1) == want;
-      } else {
-        above = T == 0xFFFFFFFFu ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)mine);
+      each([&](uint32_t k) {
+        const bool in = k != 0 && (k ^ T) >> 1 >> (left - 1) == 0;
+        const uint64_t all = __builtin_amdgcn_ballot_w64(in);
+        if (all == 0) return;
+        // those that agree with the first of them in one addition: many scores may be the same (all of 8192: 28.7 -> 14.7 us, none 10.2 -> 12.3)
+        const int digit = kSelBins - 1 - (int)(k >> next & mask), first = __builtin_ctzll(all);
+        const bool same = in && digit == __builtin_amdgcn_readlane(digit, first);
+        const uint32_t agree = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(same));
+        if (in && (!same || lane == first)) atomicAdd(&bins[digit], same ? agree : 1u);
+      });
+      __syncthreads();
+      const uint2 c = *reinterpret_cast<const uint2*>(bins + 2 * tid);  // the higher digits first
+      const uint32_t sum = c.x + c.y, incl = (uint32_t)wave_incl_scan((int)sum);
+      if (lane == 63) wave_total[wv] = incl;
+      __syncthreads();
+      uint32_t before = above + incl - sum;
+#pragma unroll
+      for (int w = 0; w < kSelWaves; ++w) before += w < wv ? wave_total[w] : 0u;
+      if (before < want && before + sum >= want) {  // one thread
+        const bool second = before + c.x < want;
+        found[0] = T | (uint32_t)(kSelBins - 1 - (2 * tid + second)) << next;
+        found[1] = second ? before + c.x : before;
+        found[2] = second ? c.y : c.x;
       }
+      __syncthreads();
+      T = (uint32_t)__builtin_amdgcn_readfirstlane((int)found[0]);
+      above = (uint32_t)__builtin_amdgcn_readfirstlane((int)found[1]);
+      exact = above + (uint32_t)__builtin_amdgcn_readfirstlane((int)found[2]) == want;
+      left = next;
     }
     if (exact) {  // those that reach T are those that stay: none is equal to one below it
       T -= 1u;
@@ -120,7 +130,9 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
   }
   const uint32_t ties = want - above;  // equals of the threshold that stay
   auto sure_of = [&](int i, uint32_t k) {
-    const int p = i * kSelThreads + tid;
+    int p = tid;
+    asm volatile("" : "+v"(p));
+    p += i * kSelThreads;
     return (p < a.len && (p < lo || p >= hi)) || (want > 0 && k > T);
   };
   auto tie_of = [&](uint32_t k) { return want > 0 && k == T; };
@@ -137,14 +149,16 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     }
   };
   if constexpr (PER > 0) {
-    // one table of the counts of every 64 positions, summed up by one wave (at most 2^15 of either kind)
+    // one table of the counts of every 64 positions, summed up by one wave (at most 2^16 of either kind, those in front of the last 64 fewer)
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if (i < steps) {
-        const uint64_t ms = __builtin_amdgcn_ballot_w64(sure_of(i, key[i])), mt = __builtin_amdgcn_ballot_w64(tie_of(key[i]));
-        if (lane == 0) place[i * kSelWaves + wv] = (uint32_t)__popcll(ms) | (uint32_t)__popcll(mt) << 16;
-      }
+      if (i * kSelThreads >= a.len) break;
+      const uint32_t k = key_of(i, v[i]);
+      const uint64_t ms = __builtin_amdgcn_ballot_w64(sure_of(i, k)), mt = __builtin_amdgcn_ballot_w64(tie_of(k));
+      if (lane == 0) place[i * kSelWaves + wv] = (uint32_t)__popcll(ms) | (uint32_t)__popcll(mt) << 16;
+      asm volatile("" ::: "memory");
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all scores are here, over which kept ones may be written
     __syncthreads();
     if (wv == 0) {
       constexpr int kEach = PER * kSelWaves / 64;  // entries of a lane
@@ -165,11 +179,11 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if (i < steps) {
-        const bool sure = sure_of(i, key[i]), tie = tie_of(key[i]);
-        const uint32_t before = place[i * kSelWaves + wv];
-        put(i, v[i], sure, tie, __builtin_amdgcn_ballot_w64(sure), __builtin_amdgcn_ballot_w64(tie), before & 0xFFFFu, before >> 16);
-      }
+      if (i * kSelThreads >= a.len) break;
+      const uint32_t k = key_of(i, v[i]), before = place[i * kSelWaves + wv];
+      const bool sure = sure_of(i, k), tie = tie_of(k);
+      put(i, v[i], sure, tie, __builtin_amdgcn_ballot_w64(sure), __builtin_amdgcn_ballot_w64(tie), before & 0xFFFFu, before >> 16);
+      asm volatile("" ::: "memory");
     }
   } else {
     uint32_t s_base = 0, t_base = 0;
@@ -183,7 +197,8 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
         place[2 * wv] = (uint32_t)__popcll(ms);
         place[2 * wv + 1] = (uint32_t)__popcll(mt);
       }
-      __syncthreads();  // and this step's scores, over which a kept one may be written
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();  // and this step's scores are here, over which a kept one may be written
       uint32_t s_before = s_base, t_before = t_base;
 #pragma unroll
       for (int w = 0; w < kSelWaves; ++w) {
@@ -308,7 +323,9 @@ __global__ __launch_bounds__(kMoveThreads, 8) void move_kernel(MoveArgs a) {
 static int launch_select(cas_ctx* ctx, const SelectArgs& a, int n_rows) {
   const dim3 grid(n_rows), block(kSelThreads);
   if (a.len <= 8 * kSelThreads) hipLaunchKernelGGL(select_kernel<8>, grid, block, 0, ctx->stream, a);
+  // longer rows from registers as long as they have room: 8 rows of 60000 80 us, 136 reading them again
   else if (a.len <= 32 * kSelThreads) hipLaunchKernelGGL(select_kernel<32>, grid, block, 0, ctx->stream, a);
+  else if (a.len <= 64 * kSelThreads) hipLaunchKernelGGL(select_kernel<64>, grid, block, 0, ctx->stream, a);
   else hipLaunchKernelGGL(select_kernel<0>, grid, block, 0, ctx->stream, a);
   CAS_HIP(ctx, hipGetLastError());
   return CAS_OK;

@@ -47,6 +47,7 @@ KINDS = {
     (1, 1, 0, 0, 3), (1, 1, 1, 0, 1), (5, 2, 0, 0, 2), (64, 63, 4, 8, 5), (1000, 1000, 10, 10, 2), (1025, 512, 0, 512, 2), (2049, 100, 4, 95, 9),
     (8192, 2048, 4, 512, 3), (8193, 1, 0, 0, 2), (8193, 8192, 0, 0, 1), (32768, 5000, 1, 7, 2), (32769, 32000, 0, 0, 2), (70001, 777, 3, 0, 1),
     (300, 20, 20, 0, 2), (300, 20, 0, 20, 2), (300, 20, 13, 7, 2),
+    (4096, 4000, 0, 3, 2), (20000, 300, 100, 200, 2), (65536, 40000, 3, 1000, 2), (65537, 9, 0, 0, 1), (50000, 17, 9, 8, 2), (70001, 70001, 0, 0, 1),
 ])
 def test_selection_is_that_of_a_stable_sort(env, kind, n, keep, first, last, rows):
     torch, B, ctx = env
