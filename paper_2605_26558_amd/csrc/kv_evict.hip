@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
 struct MoveStream {
   int begin, w;       // first word in the pool's part of a tile, words of a vector
   int first, groups;  // threads before, and to a vector
-  uint32_t inv;       // ceil(2^18 / groups): thread e < 4096 of the stream takes vector e * inv >> 18
+  uint32_t inv;       // ceil(2^18 / groups): place e < 2^14 of the stream takes vector e * inv >> 18
 };
 struct MoveArgs {
   KvGeom g;
@@ -243,18 +243,17 @@ constexpr int kMoveEach = 5;  // places of a thread: 64 vectors of at most 17 gr
 
 typedef unsigned int words4 __attribute__((ext_vector_type(4), aligned(4)));
 struct MovePlace {
-  int row = 64, at = 0, w = 0, begin = 0;  // vector of the tile, first word of the four in it, the stream
-  __device__ __forceinline__ MovePlace(const MoveArgs& a, int pool, int e) {
-    if (e >= a.threads[pool]) return;
-    MoveStream s = a.s[pool][0];
+  int row = 64, at = 0, w = 0, begin = 0;  // vector of the tile (of a step), first word of the four in it, the stream
+  __device__ __forceinline__ MovePlace(const MoveStream& s, int e) : row((int)((uint32_t)e * s.inv >> 18)), w(s.w), begin(s.begin) {
+    at = max(min(4 * (e - row * s.groups), s.w - 4), 0);
+  }
+  __device__ __forceinline__ MovePlace(const MoveStream (&t)[3], int n_streams, int threads, int e) {
+    if (e >= threads) return;
+    MoveStream s = t[0];
 #pragma unroll
     for (int i = 1; i < 3; ++i)
-      if (i < a.n_streams[pool] && e >= a.s[pool][i].first) s = a.s[pool][i];
-    e -= s.first;
-    row = (int)((uint32_t)e * s.inv >> 18);
-    at = max(min(4 * (e - row * s.groups), s.w - 4), 0);
-    w = s.w;
-    begin = s.begin;
+      if (i < n_streams && e >= t[i].first) s = t[i];
+    *this = MovePlace(s, e - s.first);
   }
   __device__ __forceinline__ void load(const uint32_t* from, words4& v) const {
     if (w >= 4) {
@@ -276,10 +275,7 @@ struct MovePlace {
   }
 };
 
-// blockIdx.y: K heads, then V heads; blockIdx.z: 2 * layer + pool.  IN_PLACE: one workgroup takes all tiles of a head in
-// order, tile i being read whole before it is written.  Position i moves to or before the place it comes from (the
-// indices ascend), so a tile is never written before a later one has been read from it.
-template <bool IN_PLACE>
+// blockIdx.y: K heads, then V heads; blockIdx.z: 2 * layer + pool.
 __global__ __launch_bounds__(kMoveThreads, 8) void move_kernel(MoveArgs a) {
   __shared__ const uint32_t* src[64];
   __shared__ int row[64];
@@ -291,32 +287,96 @@ __global__ __launch_bounds__(kMoveThreads, 8) void move_kernel(MoveArgs a) {
     const size_t tile = (((size_t)(a.layer0 + layer) * g.n_pages + page) * 2 + kv) * g.n_kv_heads + head;
     return a.pool[pool] + tile * a.tile_words[pool];
   };
-  const int tiles = (a.n_keep + 63) / 64;
-  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int rows = min(64, a.n_keep - 64 * t);
-    if (tid < 64) {
-      const int p = min(max(index[64 * t + min(tid, rows - 1)], 0), a.len - 1);
-      src[tid] = part(min(max(a.src_row[p >> 6], 0), g.n_pages - 1));
-      row[tid] = p & 63;
-    }
-    __syncthreads();
-    words4 v[kMoveEach];
+  MoveStream streams[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {  // in scalar registers: a choice among them must not become a load per lane
+    streams[i] = a.s[pool][i];
+    asm("" : "+s"(streams[i].begin), "+s"(streams[i].w), "+s"(streams[i].first), "+s"(streams[i].groups), "+s"(streams[i].inv));
+  }
+  const int n_streams = a.n_streams[pool], threads = a.threads[pool], t = blockIdx.x;
+  const int rows = min(64, a.n_keep - 64 * t);
+  if (tid < 64) {
+    const int p = min(max(index[64 * t + min(tid, rows - 1)], 0), a.len - 1);
+    src[tid] = part(min(max(a.src_row[p >> 6], 0), g.n_pages - 1));
+    row[tid] = p & 63;
+  }
+  __syncthreads();
+  words4 v[kMoveEach];
+#pragma unroll
+  for (int i = 0; i < kMoveEach; ++i) {
+    const MovePlace m(streams, n_streams, threads, tid + i * kMoveThreads);
+    if (m.row < rows) m.load(src[m.row] + m.begin + row[m.row] * m.w, v[i]);
+  }
+  const int page = a.dst_row[t];
+  if (page >= 0 && page < g.n_pages) {
+    uint32_t* const dst = part(page);
 #pragma unroll
     for (int i = 0; i < kMoveEach; ++i) {
-      const MovePlace m(a, pool, tid + i * kMoveThreads);
-      if (m.row < rows) m.load(src[m.row] + m.begin + row[m.row] * m.w, v[i]);
+      const MovePlace m(streams, n_streams, threads, tid + i * kMoveThreads);
+      if (m.row < rows) m.store(dst + m.begin + m.row * m.w, v[i]);
     }
-    if (IN_PLACE) __syncthreads();  // the whole tile is in registers
-    const int page = a.dst_row[t];
-    if (page >= 0 && page < g.n_pages) {
-      uint32_t* const dst = part(page);
+  }
+}
+
+// In place: a workgroup takes one stream (blockIdx.x) of a head (blockIdx.y: K heads, then V heads) of layer blockIdx.z, as many
+// vectors a step as its places hold; all are read before one is written.  Position i moves to or before the place it comes from (the indices
+// ascend), so that no step writes what a later one reads.  The places of the next step's vectors are looked up under the
+// loads of this one.  Bound by the latency of a step; us, with a tile of 64 vectors and all streams of a pool a step / this: one layer, 1024
+// of 2049 positions 35 / 8.8, 2048 of 8192 75 / 19, 16384 of 32768 663 / 126; 32 layers, 2048 of 8192 176 / 178.
+constexpr int kInPlaceThreads = 1024, kInPlaceEach = 4;
+__global__ __launch_bounds__(kInPlaceThreads, 8) void move_in_place_kernel(MoveArgs a) {
+  const KvGeom& g = a.g;
+  const int pool = (int)blockIdx.x >= a.n_streams[0], kvh = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x;
+  const int head = kvh % g.n_kv_heads, kv = kvh / g.n_kv_heads;
+  const MoveStream s = a.s[pool][blockIdx.x - (pool ? a.n_streams[0] : 0)];
+  const int32_t* index = a.index + ((int64_t)layer * g.n_kv_heads + head) * a.n_keep;
+  auto part = [&](int page) {
+    const size_t tile = (((size_t)(a.layer0 + layer) * g.n_pages + page) * 2 + kv) * g.n_kv_heads + head;
+    return a.pool[pool] + tile * a.tile_words[pool];
+  };
+  constexpr int kPlaces = kInPlaceEach * kInPlaceThreads;
+  __shared__ const uint32_t* src[kPlaces];     // of a step's vectors
+  __shared__ uint32_t* dst[2][kPlaces / 64 + 1];  // of its tiles; two sets in turn, the stores of a step use one while the next is written
+  const int step = (int)((uint32_t)kPlaces * s.inv >> 18);  // vectors
+  const uint32_t* from[kInPlaceEach];
+  auto look_up = [&](int r0) {
 #pragma unroll
-      for (int i = 0; i < kMoveEach; ++i) {
-        const MovePlace m(a, pool, tid + i * kMoveThreads);
-        if (m.row < rows) m.store(dst + m.begin + m.row * m.w, v[i]);
+    for (int i = 0; i < kInPlaceEach; ++i) {
+      if (i * kInPlaceThreads >= step) break;
+      const int p = min(max(index[min(r0 + tid + i * kInPlaceThreads, a.n_keep - 1)], 0), a.len - 1);
+      from[i] = part(min(max(a.src_row[p >> 6], 0), g.n_pages - 1)) + s.begin + (p & 63) * s.w;
+    }
+  };
+  look_up(0);
+  int set = 0;
+#pragma unroll 1
+  for (int r0 = 0; r0 < a.n_keep; r0 += step, set ^= 1) {
+    const int rows = min(step, a.n_keep - r0), tile0 = r0 >> 6;
+#pragma unroll
+    for (int i = 0; i < kInPlaceEach; ++i)
+      if (tid + i * kInPlaceThreads < rows) src[tid + i * kInPlaceThreads] = from[i];
+    if (tid <= (r0 + rows - 1) / 64 - tile0) {
+      const int page = a.dst_row[tile0 + tid];
+      dst[set][tid] = page >= 0 && page < g.n_pages ? part(page) + s.begin : nullptr;
+    }
+    __syncthreads();
+    words4 v[kInPlaceEach];
+#pragma unroll
+    for (int i = 0; i < kInPlaceEach; ++i) {
+      const MovePlace m(s, tid + i * kInPlaceThreads);
+      m.load(src[min(m.row, rows - 1)], v[i]);
+    }
+    if (r0 + step < a.n_keep) look_up(r0 + step);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // all vectors of the step are in registers
+#pragma unroll
+    for (int i = 0; i < kInPlaceEach; ++i) {
+      const MovePlace m(s, tid + i * kInPlaceThreads);
+      if (m.row < rows) {
+        uint32_t* const to = dst[set][((r0 + m.row) >> 6) - tile0];
+        if (to) m.store(to + ((r0 + m.row) & 63) * s.w, v[i]);
       }
     }
-    __syncthreads();  // the table of this tile is done with, and its words are written
   }
 }
 
@@ -354,8 +414,8 @@ static int launch_evict(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, int 
   a.index = d_index;
   a.layer0 = layer0; a.n_keep = n_keep; a.len = kv->h_len[seq];
   const int tiles = (n_keep + 63) / 64;
-  if (seq == dst_seq) hipLaunchKernelGGL(move_kernel<true>, dim3(1, 2 * g.n_kv_heads, 2 * n_layers), dim3(kMoveThreads), 0, ctx->stream, a);
-  else hipLaunchKernelGGL(move_kernel<false>, dim3(tiles, 2 * g.n_kv_heads, 2 * n_layers), dim3(kMoveThreads), 0, ctx->stream, a);
+  if (seq == dst_seq) hipLaunchKernelGGL(move_in_place_kernel, dim3(a.n_streams[0] + a.n_streams[1], 2 * g.n_kv_heads, n_layers), dim3(kInPlaceThreads), 0, ctx->stream, a);
+  else hipLaunchKernelGGL(move_kernel, dim3(tiles, 2 * g.n_kv_heads, 2 * n_layers), dim3(kMoveThreads), 0, ctx->stream, a);
   CAS_HIP(ctx, hipGetLastError());
   return CAS_OK;
 }
