@@ -13,11 +13,11 @@
 // rows, forms the weights of all rows of a kv head from them and adds them up.  Exponents are 4 bytes per row and position,
 // a vector of K 131 in the draft form: cheaper than decoding K again.
 //
-// Measured (8 kv heads, 60 % kept, t = 4; both launches; in brackets the bytes of the streams at the rate of a copy): 16 sequences
-// of 4 query heads a kv head over a shared 8192 and 500 of their own, draft 30 us (5.5); 8 of 5 columns, exact, 300 of
-// their own 42 (8.9); 32 of 8 query heads over 32768, exact, shared exponents 125 (29).  One sequence with weights: 8192 positions,
-// exact 22 us (7.7), 30011 and 7 columns 55 (28).  Bound by the vector operations of the decode: 63 to 71 % of a
-// SIMD's cycles, the matrix products and the LDS beside them (LDS busy 49 % of the time with 256 rows).
+// Measured (8 kv heads, 60 % kept, t = 4; us, both launches; in brackets the bytes of the streams at the rate of a copy): 16 sequences
+// of 4 query heads a kv head over a shared 8192 and 500 of their own, draft 29 (5.5); 8 of 5 columns, exact, 300 of
+// their own 41 (8.9); 32 of 8 query heads over 32768, exact, shared exponents 124 (29).  One sequence with weights: 8192 positions,
+// exact 21 (7.7), 30011 and 7 columns 55 (28).  Bound by the vector operations of the decode: 60 to 71 % of a
+// SIMD's cycles, the matrix products and the LDS beside them (busy 20 and 39 % of the time with 256 rows).
 #include <algorithm>
 #include "attention_rows_kernel.inl"
 

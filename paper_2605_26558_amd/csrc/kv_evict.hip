@@ -11,7 +11,7 @@ namespace cas {
 // the threshold (the highest value that enough of them reach) is found kSelBits at a time: counts per digit in LDS, then the
 // digit with which enough are reached by a sum over the counts; and of its equals the lower positions are taken.  Kept positions
 // are dealt their places by counting those before them: ballots within a wave, one table of counts per wave and step for the workgroup.
-// Bound by latency (three passes of five barriers), for long rows by vector issue.  us, also where all scores are equal, and with two
+// Bound by latency (three passes of four barriers), for long rows by vector issue.  us, also where all scores are equal, and with two
 // bits a turn by ballots instead of digits in LDS: 8 rows of 2049 7.1 / 8.5 / 9.9, of 8192 12.3 / 14.7 / 17, of 21647 27 / 32 / 42;
 // 256 of 8192 14.5 / 15.6 / 19.7 (8 MB read and 4 written: 3 at the rate of a copy).
 constexpr int kSelBits = 11, kSelBins = 1 << kSelBits;
