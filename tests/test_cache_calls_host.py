@@ -1,0 +1,52 @@
+"""Host parts of the calls around the cache: frequencies of rotary positions, and refusals that need no device."""
+import ctypes as C
+import math
+
+import pytest
+
+
+def close(got, want):
+    return len(got) == len(want) and all(math.isclose(a, b, rel_tol=1e-13) for a, b in zip(got, want))
+
+
+def _cfg(B, rot=128, scaling=0, base=10000.0, factor=1.0, trained=0, low=0.0, high=0.0, magnitude=1.0):
+    return B.cas_rope_cfg(rot, scaling, base, factor, trained, low, high, magnitude)
+
+
+def test_frequencies_of_every_scaling():
+    from paper_2605_26558_amd import binding as B
+    for rot in (2, 6, 64, 128, 256):
+        plain = [500000.0 ** (-2.0 * i / rot) for i in range(rot // 2)]
+        assert close(B.cas_rope_freqs(_cfg(B, rot, base=500000.0, factor=7.0)), plain)
+        assert close(B.cas_rope_freqs(_cfg(B, rot, 1, 500000.0, 8.0)), [f / 8 for f in plain])
+        if rot > 2:  # the slowest pair ends up as far as with squeezed positions, the fastest stays
+            got = B.cas_rope_freqs(_cfg(B, rot, 2, 500000.0, 8.0))
+            assert got[0] == 1.0 and math.isclose(got[-1], plain[-1] / 8, rel_tol=1e-12)
+        got = B.cas_rope_freqs(_cfg(B, rot, 3, 500000.0, 8.0, 8192, 1.0, 32.0))
+        for f, g in zip(plain, got):
+            turns = 8192 * f / (2 * math.pi)
+            assert f / 8 * (1 - 1e-12) <= g <= f * (1 + 1e-12)
+            if turns >= 32:
+                assert math.isclose(g, f, rel_tol=1e-13)
+            if turns <= 1:
+                assert math.isclose(g, f / 8, rel_tol=1e-13)
+
+
+def test_refusals_without_a_device():
+    from paper_2605_26558_amd import binding as B
+    lib = B._lib()
+    for bad in (dict(rot=0), dict(rot=5), dict(rot=258), dict(scaling=4), dict(base=0.0), dict(base=math.nan), dict(scaling=1, factor=0.5),
+                dict(rot=2, scaling=2), dict(scaling=3, trained=0, high=1.0), dict(scaling=3, trained=9, low=1.0, high=1.0), dict(magnitude=0.0)):
+        with pytest.raises(B.CasError) as e:
+            B.cas_rope_freqs(_cfg(B, **bad))
+        assert e.value.code == B.CAS_EINVAL, bad
+    cfg, one = _cfg(B), (C.c_int32 * 1)(1)
+    assert lib.cas_rope_freqs(C.byref(cfg), None) == B.CAS_EINVAL and lib.cas_rope_freqs(None, None) == B.CAS_EINVAL
+    assert lib.cas_rope_table(None, C.byref(cfg), 0, 4, None) == B.CAS_EINVAL
+    assert lib.cas_rope(None, None, 4, 64, 0, 0, None, 0, 1, 128, 1, None) == B.CAS_EINVAL
+    assert lib.cas_attention_shared(None, None, 0, 1, one, 0, 1, None, one, 8, None, None, one, None) == B.CAS_EINVAL
+    assert lib.cas_attention_weights(None, None, 0, 0, 1, None, 1, 8, None, None, 1, None, None, None, 0) == B.CAS_EINVAL
+    assert lib.cas_kv_select(None, None, 1, 1, 1, 1, 0, 0, None, None, 0) == B.CAS_EINVAL
+    assert lib.cas_kv_evict(None, None, 0, 1, 0, 0, None, 1) == B.CAS_EINVAL
+    assert lib.cas_attention_shared_bytes(None, 1, one, 0, one, 8, one) == 0
+    assert lib.cas_attention_weights_bytes(None, 0, 1, 8, 1) == 0
