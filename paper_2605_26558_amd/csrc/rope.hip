@@ -58,42 +58,49 @@ __global__ __launch_bounds__(256) void rope_table_kernel(RopeFreqs f, int units,
 }
 
 constexpr int kRopeParts = 4;
+struct RopePart {
+  uint64_t x, y;      // where head 0 of the first token would be if all heads were the part's
+  int64_t ldx, ldy;   // bytes
+  int head0;          // heads of a token before the part; all heads for one that is not there
+  int kind;           // bit 0: floats, bit 1: turns
+};
 struct RopeArgs {
-  cas_rope_part part[kRopeParts];
-  int head0[kRopeParts + 1];  // heads of a token before each part
+  RopePart part[kRopeParts];
   const float* table;
   const int32_t* pos;
-  int pos0, n_pos, n_tok, half, dim, parts, blocks;  // half: pairs of a head; blocks: workgroups of a token
+  int pos0, n_pos, n_tok, half, dim, heads, blocks;  // half: pairs of a head; heads: of all parts; blocks: workgroups of a token
   float sign;
 };
 
-// V consecutive values as floats: bf16 (exact) or floats rounded to bf16, as every tensor that passes from one operation to
-// the next is
+// V consecutive values: requested as words (eight bf16 are four words, eight floats eight), and taken as floats: bf16 (exact) or floats
+// rounded to bf16, as every tensor that passes from one operation to the next is
 template <int V>
-__device__ __forceinline__ void rope_load(const cas_rope_part& p, size_t at, float (&v)[V]) {
-  if (p.x_fp32) {
-    const float* x = static_cast<const float*>(p.d_x) + at;
-#pragma unroll
-    for (int i = 0; i < V; i += 4) {
-      if constexpr (V == 1) v[i] = x[i];
-      else {
-        const float4 q = *reinterpret_cast<const float4*>(x + i);
-        v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = round_bf16(v[i]);
+__device__ __forceinline__ void rope_request(uint64_t x, int at, bool fp32, uint32_t (&w)[V]) {
+  const uint64_t src = x + (uint32_t)at * (fp32 ? 4u : 2u);
+  if constexpr (V == 1) {
+    if (fp32) w[0] = *reinterpret_cast<const uint32_t*>(src);
+    else w[0] = *reinterpret_cast<const uint16_t*>(src);
   } else {
-    const uint16_t* x = static_cast<const uint16_t*>(p.d_x) + at;
-    if constexpr (V == 1) v[0] = bf16_to_f32(x[0]);
-    else {
-      const uint4 q = *reinterpret_cast<const uint4*>(x);
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    const uint4 q = reinterpret_cast<const uint4*>(src)[0];
+    w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    if (fp32) {
+      const uint4 r = reinterpret_cast<const uint4*>(src)[1];
+      w[4] = r.x; w[5] = r.y; w[6] = r.z; w[7] = r.w;
+    }
+  }
+}
+template <int V>
+__device__ __forceinline__ void rope_take(const uint32_t (&w)[V], bool fp32, float (&v)[V]) {
+  if (fp32) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-      }
+    for (int i = 0; i < V; ++i) v[i] = round_bf16(__uint_as_float(w[i]));
+  } else if constexpr (V == 1) {
+    v[0] = bf16_to_f32((uint16_t)w[0]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
   }
 }
@@ -119,17 +126,17 @@ struct RopeUnits {
 
 // Bound by memory: every value is read and written once, a token's row of the table comes from a cache for all heads but
 // the first.  A workgroup takes some heads of one token: `units` threads to a head, each with its part of the table's row in
-// registers for all heads that it goes through.  4099 tokens of 40 heads of 256 values, 168 MB: 33 us, 5.0 TB/s; 5 tokens of 48
-// heads of 128 values: 4 us, a launch.
+// registers for all heads that it goes through.  4099 tokens of 40 heads of 256 values, 168 MB: 31 us, 5.4 TB/s (a
+// copy of as much 33); 5 tokens of 48 heads of 128 values: 3.3 us, a launch.  Two, three or five heads of a thread requested at once: 30.6,
+// 30.6, 31.0, and 512 tokens of fp32 heads 6.1 -> 6.4, 6.8, 8.7.
 template <int V, bool INTER>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   using U = RopeUnits<V, INTER>;
   const int units = U::of_head(a.half, a.dim), turning = U::turning(a.half);
   const int slots = 256 / units, slot = (int)threadIdx.x / units, u = (int)threadIdx.x - slot * units;
-  const int tok = (int)blockIdx.x / a.blocks, block = (int)blockIdx.x - tok * a.blocks;
+  const int tok = __builtin_amdgcn_readfirstlane((int)blockIdx.x / a.blocks), block = (int)blockIdx.x - tok * a.blocks;
   const int p = a.pos ? a.pos[tok] : a.pos0 + tok;
   if (p < 0 || p >= a.n_pos || slot >= slots) return;  // padding, or a thread without a place
-  const int heads = a.head0[a.parts];
   const bool turns = u < turning;
   float c[U::kPairs], s[U::kPairs];
   if (turns) {
@@ -141,49 +148,60 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
       s[i] = a.sign * cs.y;
     }
   }
-  for (int h = block * slots + slot; h < heads; h += a.blocks * slots) {
-    int k = 0;
+  // The parts in scalars: the arguments lie in host memory, and a load from there by
+  // each lane, for its part, costs more than the head does: 44 us for the 4099 tokens from memory.
+  RopePart part[kRopeParts];
 #pragma unroll
-    for (int i = 1; i < kRopeParts; ++i) k += i < a.parts && h >= a.head0[i] ? 1 : 0;
-    const cas_rope_part& part = a.part[k];
-    const int at = (h - a.head0[k]) * a.dim;
-    const size_t x0 = (size_t)tok * part.ldx + at;
-    uint16_t* y = part.d_y + (size_t)tok * part.ldy + at;
-    if (!turns) {
-      const int e = 2 * a.half + (u - turning) * V;
-      float v[V];
-      rope_load<V>(part, x0 + e, v);
-      rope_store<V>(y + e, v);
-      continue;
+  for (int i = 0; i < kRopeParts; ++i) {
+    part[i] = a.part[i];
+    part[i].x += (uint64_t)(tok * part[i].ldx);
+    part[i].y += (uint64_t)(tok * part[i].ldy);
+    asm("" : "+s"(part[i].x), "+s"(part[i].y), "+s"(part[i].head0), "+s"(part[i].kind));
+  }
+  // the thread's places in a head: V values, and as many in the other half
+  const int e0 = !turns ? 2 * a.half + (u - turning) * V : INTER && V == 1 ? 2 * u : u * V;
+  const int e1 = INTER ? 2 * u + 1 : a.half + u * V;
+  const bool two = turns && !(INTER && V > 1);
+  for (int h = block * slots + slot; h < a.heads; h += a.blocks * slots) {
+    uint64_t x = part[0].x, y = part[0].y;
+    int kind = part[0].kind;
+#pragma unroll
+    for (int i = 1; i < kRopeParts; ++i) {
+      const bool in = h >= part[i].head0;
+      x = in ? part[i].x : x;
+      y = in ? part[i].y : y;
+      kind = in ? part[i].kind : kind;
     }
-    if constexpr (INTER && V > 1) {
-      float v[V];
-      rope_load<V>(part, x0 + u * V, v);
-      if (part.turn) {
+    const bool fp32 = kind & 1, turn = turns && (kind & 2);
+    uint16_t* const to = reinterpret_cast<uint16_t*>(y) + h * a.dim;
+    uint32_t w0[V], w1[V];
+    rope_request<V>(x, h * a.dim + e0, fp32, w0);
+    if (two) rope_request<V>(x, h * a.dim + e1, fp32, w1);
+    float v0[V];
+    rope_take<V>(w0, fp32, v0);
+    if constexpr (!INTER || V == 1) {
+      if (two) {
+        float v1[V];
+        rope_take<V>(w1, fp32, v1);
+        if (turn) {
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-          const float p0 = v[2 * i], p1 = v[2 * i + 1];
-          v[2 * i] = p0 * c[i] - p1 * s[i];
-          v[2 * i + 1] = p1 * c[i] + p0 * s[i];
+          for (int i = 0; i < V; ++i) {
+            const float p0 = v0[i], p1 = v1[i];
+            v0[i] = p0 * c[i] - p1 * s[i];
+            v1[i] = p1 * c[i] + p0 * s[i];
+          }
         }
+        rope_store<V>(to + e1, v1);
       }
-      rope_store<V>(y + u * V, v);
-    } else {
-      const int e0 = INTER ? 2 * u : u * V, e1 = INTER ? 2 * u + 1 : a.half + u * V;
-      float v0[V], v1[V];
-      rope_load<V>(part, x0 + e0, v0);
-      rope_load<V>(part, x0 + e1, v1);
-      if (part.turn) {
+    } else if (turn) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float p0 = v0[i], p1 = v1[i];
-          v0[i] = p0 * c[i] - p1 * s[i];
-          v1[i] = p1 * c[i] + p0 * s[i];
-        }
+      for (int i = 0; i < V / 2; ++i) {
+        const float p0 = v0[2 * i], p1 = v0[2 * i + 1];
+        v0[2 * i] = p0 * c[i] - p1 * s[i];
+        v0[2 * i + 1] = p1 * c[i] + p0 * s[i];
       }
-      rope_store<V>(y + e0, v0);
-      rope_store<V>(y + e1, v1);
     }
+    rope_store<V>(to + e0, v0);
   }
 }
 
@@ -191,7 +209,7 @@ template <int V, bool INTER>
 static int launch_rope(cas_ctx* ctx, RopeArgs& a) {
   const int units = RopeUnits<V, INTER>::of_head(a.half, a.dim), slots = 256 / units;
   // few tokens: a workgroup for every 256/units heads; many: one for all heads of a token, whose table row is then read once
-  const int most = (a.head0[a.parts] + slots - 1) / slots;
+  const int most = (a.heads + slots - 1) / slots;
   a.blocks = std::max(1, std::min(most, 1024 / a.n_tok));
   const int64_t grid = (int64_t)a.n_tok * a.blocks;
   if (grid > 0xFFFFFF) return CAS_ENOTSUP;  // a launch has fewer than 2^32 threads
@@ -264,18 +282,21 @@ int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout,
     if (p.n_heads < 0 || p.n_heads > (1 << 16)) return CAS_EINVAL;
     const int64_t row = (int64_t)p.n_heads * head_dim;
     if (p.ldx < row || p.ldy < row) return CAS_EINVAL;
-    a.part[i] = p;
-    a.head0[i + 1] = a.head0[i] + p.n_heads;
+    const int64_t before = (int64_t)a.heads * head_dim, size = p.x_fp32 ? 4 : 2;
+    a.part[i] = {(uint64_t)p.d_x - (uint64_t)(before * size), (uint64_t)p.d_y - (uint64_t)(before * 2), p.ldx * size, p.ldy * 2, a.heads,
+                 (p.x_fp32 ? 1 : 0) | (p.turn ? 2 : 0)};
+    a.heads += p.n_heads;
     if (row == 0 || n_tok == 0) continue;
     const uintptr_t x = (uintptr_t)p.d_x, y = (uintptr_t)p.d_y;
     if (!x || !y || x % (p.x_fp32 ? 4 : 2) || y % 2) return CAS_EINVAL;
     if (x == y && (p.x_fp32 || p.ldx != p.ldy)) return CAS_EINVAL;
     wide = wide && x % 16 == 0 && y % 16 == 0 && p.ldx % 8 == 0 && p.ldy % 8 == 0;
   }
-  if (n_tok == 0 || n_pos == 0 || a.head0[n_parts] == 0) return CAS_OK;
+  if (n_tok == 0 || n_pos == 0 || a.heads == 0) return CAS_OK;
+  for (int i = n_parts; i < cas::kRopeParts; ++i) a.part[i].head0 = a.heads;
   if (!d_table || !cas::aligned256(d_table) || !cas::on_device(ctx)) return CAS_EINVAL;
   a.table = d_table; a.pos = d_pos; a.pos0 = pos0; a.n_pos = n_pos; a.n_tok = n_tok;
-  a.half = half; a.dim = head_dim; a.parts = n_parts; a.sign = transposed ? -1.f : 1.f;
+  a.half = half; a.dim = head_dim; a.sign = transposed ? -1.f : 1.f;
   if (layout == CAS_ROPE_HALF) return wide ? cas::launch_rope<8, false>(ctx, a) : cas::launch_rope<1, false>(ctx, a);
   return wide ? cas::launch_rope<8, true>(ctx, a) : cas::launch_rope<1, true>(ctx, a);
 }
