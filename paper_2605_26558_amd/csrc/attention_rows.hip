@@ -28,12 +28,16 @@ extern template int launch_rows_partial<false, false>(cas_ctx*, const RowsArgs&,
 extern template int launch_rows_partial<true, true>(cas_ctx*, const RowsArgs&, int, int);
 extern template int launch_rows_partial<false, true>(cas_ctx*, const RowsArgs&, int, int);
 
-// Joins the partial results of a row: PARTS waves per row (4 or 1) take every PARTS-th split each, lane two channels, and
-// add them in order; then the parts in order.  Bound by latency: the pairs and kMergeAhead outputs are requested at once, the
-// outputs through buffer descriptors, of no length past the end of the part: what lies there reads as 0 without a branch.
-constexpr int kMergeAhead = 16;
+// Joins the partial results of a row in kMergeSums sums, of every kMergeSums-th split each, in order; then these in order.  One
+// wave forms all four or four waves one each (PARTS), a lane two channels: how many waves there are goes by the row with the most
+// splits of the launch, so the order of a row's additions must not depend on it.  Bound by latency: the pairs and kMergeAhead outputs
+// are requested at once, the outputs through buffer descriptors, of no length past the end of the part: what lies there reads as 0
+// without a branch.
+constexpr int kMergeAhead = 16, kMergeSums = 4;
 template <int PARTS>
 __device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head) {
+  static_assert(PARTS == 1 || PARTS == kMergeSums, "");
+  constexpr int kOwn = kMergeSums / PARTS;  // sums of a wave
   __shared__ float2 joined[4][64];
   const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int rr = block * (4 / PARTS) + wv / PARTS, part = wv % PARTS;
@@ -80,7 +84,9 @@ __device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head
     den += __builtin_amdgcn_exp2f(p.x - M) * p.y;
   }
   den = wave_sum(den);
-  float2 num = make_float2(0.f, 0.f);
+  float2 sums[kOwn];
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) sums[k] = make_float2(0.f, 0.f);
   for (int q0 = 0; q0 < cnt; q0 += kMergeAhead) {
     if (q0 > 0) {
       if ((q0 & 63) == 0) own = q0 + lane < cnt ? pair(part + PARTS * (q0 + lane)) : make_float2(kLowest, 0.f);
@@ -90,19 +96,21 @@ __device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head
 #pragma unroll
     for (int q = 0; q < kMergeAhead; ++q) {
       const float ws = __int_as_float(__builtin_amdgcn_readlane(w, (q0 & 63) + q));
-      num.x += ws * o[q].x;
-      num.y += ws * o[q].y;
+      sums[q % kOwn].x += ws * o[q].x;
+      sums[q % kOwn].y += ws * o[q].y;
     }
   }
+  float2 num = sums[0];
   if constexpr (PARTS > 1) {
     joined[part][lane] = num;
     __syncthreads();
     if (part != 0) return;
+  }
 #pragma unroll
-    for (int p = 1; p < PARTS; ++p) {
-      num.x += joined[p][lane].x;
-      num.y += joined[p][lane].y;
-    }
+  for (int p = 1; p < kMergeSums; ++p) {
+    const float2 add = PARTS > 1 ? joined[p][lane] : sums[p % kOwn];
+    num.x += add.x;
+    num.y += add.y;
   }
   const int c = r / a.grp, gi = r - c * a.grp;
   if (__builtin_amdgcn_ballot_w64(odd != 0)) {  // those that the row sees, which the partial results left out

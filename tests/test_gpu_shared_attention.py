@@ -421,3 +421,20 @@ def test_refusals(env):
     assert weights(c=B.Context()) == B.CAS_ENOMEM
     assert weights(ld=111, o=p(torch.empty_like(many))) == B.CAS_OK
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("prefix,own,other", [(0, 790, (790, 3000, 200)), (703, 90, (90, 4000)), (130, 500, (64, 5000))])
+def test_lengths_of_the_others_leave_the_bits(env, prefix, own, other):
+    """The same call with another sequence that is short, or so long that a row of it has more partial results than the one looked at."""
+    torch, B, ctx = env
+    cols = [16, 1]
+    kv = _cache(torch, B, ctx, 8, prefix, [own, max(other)])
+    for seed in range(4):   # a sum in another order shows in some 6 of 100000 values, of which a call has 131072
+        Q, Kn, Vn = _inputs(torch, 2, cols, cols, 64, 8, seed=seed)
+        outs = []
+        for n in other:
+            B.cas_kv_set_len(kv, 1, prefix + n)
+            outs.append(B.cas_attention_shared(ctx, kv, 0, [0, 1], prefix, True, Q, Kn, Vn)[0])
+        torch.cuda.synchronize()
+        for n, o in zip(other, outs):
+            assert torch.equal(o, outs[0]), (seed, n, int((o != outs[0]).sum()))
