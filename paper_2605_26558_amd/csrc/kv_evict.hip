@@ -58,10 +58,10 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     return p >= lo && p < hi ? score_key(x) : 0u;
   };
   float v[N];
-  if constexpr (PER > 0) {  // 0 behind the row
+  if constexpr (PER > 0) {  // 0 behind the row: the whole distance in the offset that is checked, the scalar one is not
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(row), 0, 4 * a.len, kRawBufferFlags);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) v[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, 4 * tid, 4 * i * kSelThreads, 0));
+    for (int i = 0; i < PER; ++i) v[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, 4 * (tid + i * kSelThreads), 0, 0));
   }
   // f(key) of every position, the workgroup's waves together
   auto each = [&](auto&& f) {
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(kInPlaceThreads, 8) void move_in_place_kernel(MoveA
 static int launch_select(cas_ctx* ctx, const SelectArgs& a, int n_rows) {
   const dim3 grid(n_rows), block(kSelThreads);
   if (a.len <= 8 * kSelThreads) hipLaunchKernelGGL(select_kernel<8>, grid, block, 0, ctx->stream, a);
-  // longer rows from registers as long as they have room: 8 rows of 60000 80 us, 136 reading them again
+  // longer rows from registers as long as they have room: 8 rows of 60000 85 us, 136 reading them again
   else if (a.len <= 32 * kSelThreads) hipLaunchKernelGGL(select_kernel<32>, grid, block, 0, ctx->stream, a);
   else if (a.len <= 64 * kSelThreads) hipLaunchKernelGGL(select_kernel<64>, grid, block, 0, ctx->stream, a);
   else hipLaunchKernelGGL(select_kernel<0>, grid, block, 0, ctx->stream, a);

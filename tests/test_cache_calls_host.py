@@ -50,3 +50,27 @@ def test_refusals_without_a_device():
     assert lib.cas_kv_evict(None, None, 0, 1, 0, 0, None, 1) == B.CAS_EINVAL
     assert lib.cas_attention_shared_bytes(None, 1, one, 0, one, 8, one) == 0
     assert lib.cas_attention_weights_bytes(None, 0, 1, 8, 1) == 0
+
+
+def test_buffer_accesses_are_checked_over_their_whole_distance():
+    """Raw buffer accesses are held to the descriptor's length by their lane offset alone: nothing may be in the scalar offset."""
+    import glob
+    import os
+    import re
+    import paper_2605_26558_amd as P
+    seen = 0
+    for path in sorted(glob.glob(os.path.join(os.path.dirname(P.__file__), "csrc", "*"))):
+        text = open(path, encoding="utf-8").read() if os.path.isfile(path) else ""
+        for m in re.finditer(r"__builtin_amdgcn_raw_buffer_(load|store)_\w+\(", text):
+            args, depth, at = [""], 0, m.end()
+            while depth >= 0:
+                c = text[at]
+                depth += (c in "([{") - (c in ")]}")
+                if c == "," and depth == 0:
+                    args.append("")
+                elif depth >= 0:
+                    args[-1] += c
+                at += 1
+            seen += 1
+            assert args[-2].strip() == "0", (os.path.basename(path), m.group(0) + ",".join(args))
+    assert seen > 10
