@@ -499,7 +499,7 @@ size_t cas_attention_weights_bytes(const cas_kv* kv, int seq, int ncols, int n_q
  * d_index: int32 [n_rows][n_keep], positions in ascending order.  d_kept: NULL or float [n_rows][ld_kept],
  * receives the scores of the kept positions (ld_kept >= n_keep); it may be d_score itself with ld_kept = ld,
  * whose entries from n_keep on then stay as they were.  0 <= n_first, n_last; n_first + n_last <= n_keep <= len.
- * len <= 2^30 (CAS_ENOTSUP above).  CAS_EINVAL unless the context's device is current. */
+ * len <= 2^30 and n_rows < 2^22 (CAS_ENOTSUP above).  CAS_EINVAL unless the context's device is current. */
 int cas_kv_select(cas_ctx* ctx, const float* d_score, int64_t ld, int n_rows, int len, int n_keep, int n_first,
                   int n_last, int32_t* d_index, float* d_kept, int64_t ld_kept);
 

@@ -430,7 +430,7 @@ int cas_kv_select(cas_ctx* ctx, const float* d_score, int64_t ld, int n_rows, in
   if ((int64_t)n_first + n_last > n_keep || (d_kept && ld_kept < n_keep)) return CAS_EINVAL;
   if (d_kept && d_kept == d_score && ld_kept != ld) return CAS_EINVAL;
   if (n_rows == 0 || n_keep == 0) return CAS_OK;
-  if (len > 1 << 30) return CAS_ENOTSUP;
+  if (len > 1 << 30 || n_rows > 0x3FFFFF) return CAS_ENOTSUP;  // a launch has fewer than 2^32 threads
   if (!d_score || !d_index || !cas::on_device(ctx)) return CAS_EINVAL;
   cas::SelectArgs a{d_score, ld, ld_kept, len, n_keep, n_first, n_last, d_index, d_kept};
   return cas::launch_select(ctx, a, n_rows);

@@ -309,3 +309,19 @@ def test_operators_together(env):
     torch.cuda.synchronize()
     _check(torch, o, ref, tol, "after the eviction")
     assert bool(torch.isfinite(s2).all())
+
+
+def test_as_many_rows_as_a_launch_has(env):
+    torch, B, ctx = env
+    rows = 1 << 22
+    score = torch.arange(rows, dtype=torch.float32, device="cuda").view(rows, 1)
+    index = torch.full((rows, 1), 7, dtype=torch.int32, device="cuda")
+    with pytest.raises(B.CasError) as e:
+        B.cas_kv_select(ctx, score, 1, 1, index=index)
+    assert e.value.code == B.CAS_ENOTSUP
+    torch.cuda.synchronize()
+    assert bool((index == 7).all())
+    kept = torch.zeros(rows, 1, device="cuda")
+    B.cas_kv_select(ctx, score[1:], 1, 1, index=index[1:], kept=kept[1:])
+    torch.cuda.synchronize()
+    assert int(index[0]) == 7 and bool((index[1:] == 0).all()) and torch.equal(kept[1:], score[1:])
