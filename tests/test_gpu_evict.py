@@ -311,6 +311,34 @@ def test_operators_together(env):
     assert bool(torch.isfinite(s2).all())
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+def test_sums_go_on_behind_an_eviction(env, in_place):
+    """The sums of the positions that stay are carried on at their new places, those of new positions begin at nothing."""
+    torch, B, ctx = env
+    from tests.test_gpu_shared_attention import _cache, _inputs, _reference
+    n_kv, n, held = 2, 300, 117
+    kv = _cache(torch, B, ctx, n_kv, 0, [n, n])
+    dst = 0 if in_place else 1
+    (q,), (k,), (v,) = _inputs(torch, 1, [3], [3], 8, n_kv)
+    _, score = B.cas_attention_weights(ctx, kv, 0, 0, True, q, k, v)
+    before = score.clone()
+    index = B.cas_kv_select(ctx, score, n, held, 4, 16, kept=score)
+    B.cas_kv_evict(ctx, kv, 0, 1, 0, dst, index.view(1, n_kv, held))
+    B.cas_kv_set_len(kv, dst, held)
+    torch.cuda.synchronize()
+    assert torch.equal(score[:, :held], before.gather(1, index.long())) and torch.equal(score[:, held:], before[:, held:])
+    (q,), (k,), (v,) = _inputs(torch, 1, [2], [2], 8, n_kv, seed=6)
+    after = torch.full_like(score, 9.0)
+    B.cas_attention_weights(ctx, kv, 0, dst, True, q, k, v, score, score_out=after)
+    _, _, w, wt = _reference(torch, B, ctx, kv, 0, dst, True, q, k, v)
+    torch.cuda.synchronize()
+    want = w.clone()
+    want[:, :held] += score[:, :held].double()
+    err = (after[:, :held + 2].double() - want).abs()     # the sum's own rounding beside the weights' tolerance
+    assert bool((err <= wt + 2.0 ** -24 * want).all()), float((err / wt).max())
+    assert bool((after[:, held + 2:] == 9.0).all())
+
+
 def test_as_many_rows_as_a_launch_has(env):
     torch, B, ctx = env
     rows = 1 << 22

@@ -283,3 +283,22 @@ def test_refusals(env):
     assert call(dim=264, ldx=528, ldy=528) == B.CAS_ENOTSUP
     assert call(n_tok=0, xp=None, yp=None, tab=None) == B.CAS_OK
     assert call(heads=0, xp=None, yp=None, tab=None) == B.CAS_OK
+
+
+@pytest.mark.parametrize("rot,scaling,pos0,n,factor,mag", [
+    (128, 0, 0, 20000, 1.0, 1.0), (128, 3, 0, 4097, 16.0, 1.2772588722239782), (64, 3, (1 << 24) - 300, 300, 40.0, 0.5),
+    (128, 0, (1 << 24) - 5000, 5000, 1.0, 1.0), (256, 1, (1 << 24) - 2000, 2000, 3.0, 0.1), (80, 2, 1 << 20, 3000, 3.5, 1.7),
+])
+def test_table_within_its_bound_at_every_position(env, rot, scaling, pos0, n, factor, mag):
+    """The documented 2e-7 * magnitude and nothing beside it, against the frequencies that cas_rope_freqs gives."""
+    torch, B, ctx = env
+    print(f"case {rot=} {scaling=} {pos0=} {n=}", flush=True)
+    assert np.finfo(np.longdouble).nmant >= 63
+    cfg = B.cas_rope_cfg(rot, scaling, 10000.0, factor, 4096, 1.0, 32.0, mag)
+    f = np.array(B.cas_rope_freqs(cfg)).astype(np.longdouble)
+    a = np.arange(pos0, pos0 + n).astype(np.longdouble)[:, None] * f   # 24 and 53 bits into 64: off by 2^24 * 2^-64
+    ref = np.stack([np.cos(a), np.sin(a)], -1) * np.longdouble(mag)
+    got = B.cas_rope_table(ctx, cfg, pos0, n).cpu().numpy()
+    # relative to the magnitude: the reduced angle as fp32 2.6e-8, quarter turns per position in 64 bits 0.6e-8, the series 2.5e-8 and
+    # its last rounding 3e-8 (at pi / 4, where the value is 0.71; 3e-8 alone at 1), magnitude and product 2^-24 of the value each
+    assert float(np.abs(got - ref).max()) <= 2e-7 * mag
