@@ -413,7 +413,7 @@ typedef struct {
   double factor;    /* >= 1, finite */
   int32_t trained;  /* CAS_ROPE_BANDS: positions of the trained context, >= 1 */
   double low, high; /* CAS_ROPE_BANDS: turns below which a pair is squeezed whole and above which it is left; 0 <= low < high */
-  double magnitude; /* > 0, finite */
+  double magnitude; /* FLT_MIN .. FLT_MAX: a normal number of the fp32 table */
 } cas_rope_cfg;
 
 /* Host only: the rot/2 frequencies f_i after scaling. */

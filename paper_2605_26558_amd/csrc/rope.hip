@@ -2,6 +2,7 @@
 // positions, with the frequencies scaled for long contexts, and the rotation of the heads of a projection at positions
 // given one by one.  (The model passes rotate inside their own kernels, at the positions of the cache.)
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include "cas_device.hpp"
 #include "cas_internal.hpp"
@@ -223,7 +224,8 @@ static int launch_rope(cas_ctx* ctx, RopeArgs& a) {
 static bool rope_cfg_ok(const cas_rope_cfg* c) {
   if (!c || c->rot < 2 || c->rot > 2 * cas::kRopePairs || (c->rot & 1)) return false;
   if (c->scaling < CAS_ROPE_PLAIN || c->scaling > CAS_ROPE_BANDS) return false;
-  if (!(c->base >= 1.0) || !std::isfinite(c->base) || !(c->magnitude > 0.0) || !std::isfinite(c->magnitude)) return false;
+  if (!(c->base >= 1.0) || !std::isfinite(c->base)) return false;
+  if (!(c->magnitude >= (double)FLT_MIN) || !(c->magnitude <= (double)FLT_MAX)) return false;  // the table is fp32
   if (c->scaling != CAS_ROPE_PLAIN && (!(c->factor >= 1.0) || !std::isfinite(c->factor))) return false;
   if (c->scaling == CAS_ROPE_BASE && c->rot < 4) return false;
   if (c->scaling == CAS_ROPE_BANDS &&

@@ -74,3 +74,13 @@ def test_buffer_accesses_are_checked_over_their_whole_distance():
             seen += 1
             assert args[-2].strip() == "0", (os.path.basename(path), m.group(0) + ",".join(args))
     assert seen > 10
+
+
+def test_a_magnitude_that_fp32_does_not_hold_is_refused():
+    from paper_2605_26558_amd import binding as B
+    for magnitude in (2.0 ** -126, 3.4028234663852886e38):   # the smallest normal and the largest number of the table
+        assert len(B.cas_rope_freqs(_cfg(B, magnitude=magnitude))) == 64
+    for magnitude in (1e-39, 2.0 ** -150, 3.5e38, 1e300):
+        with pytest.raises(B.CasError) as e:
+            B.cas_rope_freqs(_cfg(B, magnitude=magnitude))
+        assert e.value.code == B.CAS_EINVAL, magnitude

@@ -302,3 +302,13 @@ def test_table_within_its_bound_at_every_position(env, rot, scaling, pos0, n, fa
     # relative to the magnitude: the reduced angle as fp32 2.6e-8, quarter turns per position in 64 bits 0.6e-8, the series 2.5e-8 and
     # its last rounding 3e-8 (at pi / 4, where the value is 0.71; 3e-8 alone at 1), magnitude and product 2^-24 of the value each
     assert float(np.abs(got - ref).max()) <= 2e-7 * mag
+
+
+@pytest.mark.parametrize("mag", [2.0 ** -126, 3.4028234663852886e38])
+def test_magnitudes_at_the_ends_of_fp32(env, mag):
+    torch, B, ctx = env
+    cfg = B.cas_rope_cfg(128, 0, 10000.0, 1.0, 0, 0.0, 0.0, mag)
+    a = np.arange(500, 1500, dtype=np.float64)[:, None] * np.array(B.cas_rope_freqs(cfg))
+    got = B.cas_rope_table(ctx, cfg, 500, 1000).cpu().numpy()
+    # the documented bound; below the normal numbers a product is off by 2^-150, 2^-24 of the smallest normal one
+    assert np.abs(got / mag - np.stack([np.cos(a), np.sin(a)], -1)).max() <= 2e-7
