@@ -216,6 +216,11 @@ def _lib():
     return _LIB
 
 
+def _bf16_bits(torch):
+    """Types that hold a bf16 number: other numbers of two bytes would be read as bits of one."""
+    return (torch.bfloat16, torch.int16, torch.uint16)
+
+
 def _ptr(t):
     if t is None:
         return None
@@ -669,7 +674,7 @@ def cas_rope_table(ctx: Context, cfg: cas_rope_cfg, pos0, n_pos, out=None):
 
 
 def cas_rope(ctx: Context, table, xs, pos=None, pos0=0, layout=CAS_ROPE_HALF, transposed=False, turn=None, outs=None):
-    """Rotates up to four tensors [n_tok, heads, head_dim] (float32, or two-byte bf16 bits) of the same tokens; the heads
+    """Rotates up to four tensors [n_tok, heads, head_dim] (float32, or bf16 as bfloat16, int16 or uint16) of the same tokens; the heads
     of a token side by side, tokens any stride apart.  table: float32 [n_pos, rot/2, 2] from position 0 on; pos: int32
     [n_tok] on the GPU, or None for pos0 + token.  turn: per tensor, False to take it over unrotated.  Returns bf16
     tensors (bits as int16 for float32 inputs, the input's type otherwise); outs may be given, xs[i] itself included
@@ -680,7 +685,7 @@ def cas_rope(ctx: Context, table, xs, pos=None, pos0=0, layout=CAS_ROPE_HALF, tr
     n_tok, _, dim = xs[0].shape
     assert pos is None or (pos.is_cuda and pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == n_tok)
     assert outs is None or len(outs) == len(xs)
-    ys, parts = [], []
+    ys, parts, bits = [], [], _bf16_bits(torch)
     for i, x in enumerate(xs):
         shape, (ldx, head, one), fp32 = x.shape, x.stride(), x.dtype == torch.float32
         heads = shape[1]
@@ -692,7 +697,7 @@ def cas_rope(ctx: Context, table, xs, pos=None, pos0=0, layout=CAS_ROPE_HALF, tr
             ldy, yhead, yone = y.stride()
             assert y.shape == shape and y.is_cuda and (yone == 1 or dim == 1) and (yhead == dim or heads <= 1)
         assert x.is_cuda and shape[0] == n_tok and shape[2] == dim and (one == 1 or dim == 1) and (head == dim or heads <= 1)
-        assert y.element_size() == 2 and (fp32 or x.element_size() == 2)
+        assert y.dtype in bits and (fp32 or x.dtype in bits)
         if n_tok == 1:  # no second token that a distance would lead to
             ldx, ldy = max(ldx, heads * dim), max(ldy, heads * dim)
         ys.append(y)
@@ -716,7 +721,7 @@ def cas_attention_shared(ctx: Context, kv: KVCache, layer, seqs, prefix_len, ful
     n = len(seqs)
     outs = [torch.empty_like(q) for q in Qs] if outs is None else outs
     heads = Qs[0].shape[1]
-    cols, new, ptrs = _check_attention(kv, heads, Qs, Knews, Vnews, outs)
+    cols, new, ptrs = _check_attention(kv, heads, Qs, Knews, Vnews, outs, _bf16_bits(torch))
     assert n == len(cols)
     i32, ptr = C.c_int32 * n, C.c_void_p * n
     q, k, v, o = (ptr(*p) for p in ptrs)
@@ -725,16 +730,16 @@ def cas_attention_shared(ctx: Context, kv: KVCache, layer, seqs, prefix_len, ful
     return outs
 
 
-def _check_attention(kv: KVCache, heads, Qs, Knews, Vnews, outs):
+def _check_attention(kv: KVCache, heads, Qs, Knews, Vnews, outs, bits):
     """Shapes, types and layout of the sequences' tensors: their columns, in-flight vectors, and addresses."""
     d = kv.desc.head_dim
     qs, ks = [t.shape for t in Qs], [t.shape for t in Knews]
     cols, new = [s[0] for s in qs], [s[0] for s in ks]
     qt, kt = (heads, d), (kv.desc.n_kv_heads, d)
     assert all([s[1:] == qt for s in qs]) and all([s[1:] == kt for s in ks]) and len(cols) == len(new) == len(Vnews) == len(outs)
-    qb, kb = [2 * c * heads * d for c in cols], [2 * c * kt[0] * d for c in new]
-    for ts, nbytes in ((Qs, qb), (Knews, kb), (Vnews, kb), (outs, qb)):
-        assert all([t.is_contiguous() and t.is_cuda for t in ts]) and [t.nbytes for t in ts] == nbytes
+    assert [t.nbytes for t in Vnews] == [2 * c * kt[0] * d for c in new] and [t.nbytes for t in outs] == [2 * c * heads * d for c in cols]
+    for ts in (Qs, Knews, Vnews, outs):
+        assert all([t.is_contiguous() and t.is_cuda and t.dtype in bits for t in ts])
     return cols, new, [[t.data_ptr() for t in ts] for ts in (Qs, Knews, Vnews, outs)]
 
 
@@ -751,10 +756,10 @@ def cas_attention_weights(ctx: Context, kv: KVCache, layer, seq, full, Q, Knew, 
     torch = ctx._torch
     if out is None:
         out = torch.empty_like(Q)
-    (cols, heads, d), (new, rows, kd) = Q.shape, Knew.shape
+    (cols, heads, d), (new, rows, kd), bits = Q.shape, Knew.shape, _bf16_bits(torch)
     assert rows == kv.desc.n_kv_heads and d == kd == kv.desc.head_dim
     for t, n in ((Q, cols * heads), (out, cols * heads), (Knew, new * rows), (Vnew, new * rows)):
-        assert t.is_contiguous() and t.is_cuda and t.nbytes == 2 * n * d
+        assert t.is_contiguous() and t.is_cuda and t.dtype in bits and t.nbytes == 2 * n * d
     total = cas_kv_len(kv, seq) + new
     if score_out is None:
         ld = total if score_in is None else score_in.stride(0)

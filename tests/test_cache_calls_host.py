@@ -84,3 +84,46 @@ def test_a_magnitude_that_fp32_does_not_hold_is_refused():
         with pytest.raises(B.CasError) as e:
             B.cas_rope_freqs(_cfg(B, magnitude=magnitude))
         assert e.value.code == B.CAS_EINVAL, magnitude
+
+
+@pytest.fixture
+def wrappers(monkeypatch):
+    """The binding with tensors that say they are on the GPU and a context that is none: a call whose arguments the wrapper
+    takes comes back from the library as CAS_EINVAL, one that it does not take raises AssertionError."""
+    import types
+    import torch
+    from paper_2605_26558_amd import binding as B
+
+    class OnGpu(torch.Tensor):
+        is_cuda = True
+
+    def check(rc, what):
+        if rc != B.CAS_OK:
+            raise B.CasError(rc, what)
+
+    ctx = types.SimpleNamespace(_torch=torch, h=None, _check=check)
+    kv = types.SimpleNamespace(h=None, desc=types.SimpleNamespace(n_kv_heads=2, head_dim=128))
+    monkeypatch.setattr(B, "cas_kv_len", lambda kv, seq: 10)
+    return torch, B, ctx, kv, lambda *shape, dtype=torch.bfloat16: torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+def _taken(B, call):
+    with pytest.raises((B.CasError, AssertionError)) as e:
+        call()
+    return isinstance(e.value, B.CasError) and e.value.code == B.CAS_EINVAL
+
+
+def test_wrappers_take_bf16_bits_and_no_other_two_byte_numbers(wrappers):
+    torch, B, ctx, kv, t = wrappers
+    table, bits = t(4, 64, 2, dtype=torch.float32), (torch.bfloat16, torch.int16, torch.uint16)
+    for dtype in (*bits, torch.float32, torch.float16, torch.float64, torch.int32):
+        x = t(3, 2, 128, dtype=dtype)
+        assert _taken(B, lambda: B.cas_rope(ctx, table, [x])) == (dtype in bits or dtype == torch.float32), dtype
+        y = t(3, 2, 128, dtype=dtype)
+        assert _taken(B, lambda: B.cas_rope(ctx, table, [t(3, 2, 128)], outs=[y])) == (dtype in bits), dtype
+        for i in range(4):
+            a = [t(1, 4, 128), t(1, 2, 128), t(1, 2, 128), t(1, 4, 128)]
+            a[i] = a[i].to(dtype).as_subclass(type(table))
+            q, k, v, o = a
+            assert _taken(B, lambda: B.cas_attention_shared(ctx, kv, 0, [0], 0, True, [q], [k], [v], outs=[o])) == (dtype in bits), (i, dtype)
+            assert _taken(B, lambda: B.cas_attention_weights(ctx, kv, 0, 0, True, q, k, v, score_out=t(2, 11, dtype=torch.float32), out=o)) == (dtype in bits), (i, dtype)
