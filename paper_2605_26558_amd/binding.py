@@ -762,15 +762,16 @@ def cas_attention_weights(ctx: Context, kv: KVCache, layer, seq, full, Q, Knew, 
         assert t.is_contiguous() and t.is_cuda and t.dtype in bits and t.nbytes == 2 * n * d
     total = cas_kv_len(kv, seq) + new
     if score_out is None:
-        ld = total if score_in is None else score_in.stride(0)
+        ld = total if score_in is None else max(score_in.stride(0), total)
         score_out = torch.empty((rows, ld), dtype=torch.float32, device=Q.device)
         if ld != total:
             score_out = score_out[:, :total]
-    ld = score_out.stride(0)
+    ld = total if rows == 1 else score_out.stride(0)  # a single row has no next one
     for s in (score_out, score_in):
         if s is not None:
-            assert s.is_cuda and s.dtype == torch.float32 and s.stride() == (ld, 1)
-            assert s.shape[0] == rows and s.shape[1] >= total
+            (r, w), (step, one) = s.shape, s.stride()
+            assert s.is_cuda and s.dtype == torch.float32 and r == rows and w >= total
+            assert (step == ld or rows == 1) and (one == 1 or w == 1)
     ctx._check(_lib().cas_attention_weights(ctx.h, kv.h, layer, seq, 1 if full else 0, Q.data_ptr(), cols, heads, Knew.data_ptr(),
                                             Vnew.data_ptr(), new, out.data_ptr(), None if score_in is None else score_in.data_ptr(),
                                             score_out.data_ptr(), ld), "cas_attention_weights")

@@ -127,3 +127,19 @@ def test_wrappers_take_bf16_bits_and_no_other_two_byte_numbers(wrappers):
             q, k, v, o = a
             assert _taken(B, lambda: B.cas_attention_shared(ctx, kv, 0, [0], 0, True, [q], [k], [v], outs=[o])) == (dtype in bits), (i, dtype)
             assert _taken(B, lambda: B.cas_attention_weights(ctx, kv, 0, 0, True, q, k, v, score_out=t(2, 11, dtype=torch.float32), out=o)) == (dtype in bits), (i, dtype)
+
+
+def test_scores_of_one_kv_head_lie_anywhere(wrappers):
+    """A single row has no next one, so its step does not matter; rows of several heads lie the same distance apart."""
+    torch, B, ctx, kv, t = wrappers
+    f = lambda *shape: t(*shape, dtype=torch.float32)  # noqa: E731
+    for heads in (1, 2):
+        kv.desc.n_kv_heads = heads
+        q, k, v = t(1, 4, 128), t(1, heads, 128), t(1, heads, 128)
+        forms = [f(heads, 11), f(heads, 40)[:, :11], f(40, heads, 20)[3, :, 5:16]] + [f(11).expand(1, 11)] * (heads == 1)
+        for a in forms + [None]:
+            for b in forms:
+                want = heads == 1 or a is None or a.stride() == b.stride()
+                assert _taken(B, lambda: B.cas_attention_weights(ctx, kv, 0, 0, True, q, k, v, a, score_out=b)) == want, (heads, a, b)
+        assert not _taken(B, lambda: B.cas_attention_weights(ctx, kv, 0, 0, True, q, k, v, f(heads, 22)[:, ::2], score_out=f(heads, 11)))
+        assert not _taken(B, lambda: B.cas_attention_weights(ctx, kv, 0, 0, True, q, k, v, f(heads, 10), score_out=f(heads, 11)))

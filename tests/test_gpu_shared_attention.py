@@ -438,3 +438,18 @@ def test_lengths_of_the_others_leave_the_bits(env, prefix, own, other):
         torch.cuda.synchronize()
         for n, o in zip(other, outs):
             assert torch.equal(o, outs[0]), (seed, n, int((o != outs[0]).sum()))
+
+
+def test_scores_of_one_kv_head_in_other_tensors(env):
+    """Sums of a single kv head read from and written to rows of tensors of different widths."""
+    torch, B, ctx = env
+    kv = _cache(torch, B, ctx, 1, 0, [300])
+    (q,), (kn,), (vn,) = _inputs(torch, 1, [2], [3], 4, 1)
+    before, after = torch.rand(5, 320, device="cuda"), torch.full((3, 400), 9.0, device="cuda")
+    _, want = B.cas_attention_weights(ctx, kv, 0, 0, True, q, kn, vn, before[2:3, :303].contiguous())
+    _, got = B.cas_attention_weights(ctx, kv, 0, 0, True, q, kn, vn, before[2:3, :303], score_out=after[1:2, 7:310])
+    _, third = B.cas_attention_weights(ctx, kv, 0, 0, True, q, kn, vn, before[2].expand(1, 320))
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(third[:, :303], want)
+    after[1, 7:310] = 9.0
+    assert bool((after == 9.0).all())
