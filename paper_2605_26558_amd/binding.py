@@ -546,6 +546,7 @@ class KVCache:
                  spec_pool=None, verif_pool=None):
         """spec_pool, verif_pool: device tensors to use as the pools (both or none), e.g. of a stored cache."""
         torch = ctx._torch
+        assert (spec_pool is None) == (verif_pool is None), "spec_pool and verif_pool: both or none"
         d = cas_kv_desc()
         d.n_layers, d.n_kv_heads, d.head_dim, d.page_tokens = n_layers, n_kv_heads, head_dim, page_tokens
         d.n_pages, d.max_seqs, d.max_pages_per_seq = n_pages, max_seqs, max_pages_per_seq

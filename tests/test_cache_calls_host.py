@@ -143,3 +143,10 @@ def test_scores_of_one_kv_head_lie_anywhere(wrappers):
                 assert _taken(B, lambda: B.cas_attention_weights(ctx, kv, 0, 0, True, q, k, v, a, score_out=b)) == want, (heads, a, b)
         assert not _taken(B, lambda: B.cas_attention_weights(ctx, kv, 0, 0, True, q, k, v, f(heads, 22)[:, ::2], score_out=f(heads, 11)))
         assert not _taken(B, lambda: B.cas_attention_weights(ctx, kv, 0, 0, True, q, k, v, f(heads, 10), score_out=f(heads, 11)))
+
+
+def test_pools_of_a_cache_are_given_both_or_not_at_all(wrappers):
+    torch, B, ctx, _, t = wrappers
+    for pools in (dict(spec_pool=t(1 << 20)), dict(verif_pool=t(1 << 20))):
+        with pytest.raises(AssertionError, match="both"):
+            B.KVCache(ctx, 1, 2, 4, 1, 4, **pools)
