@@ -121,28 +121,6 @@ __device__ __forceinline__ int q_index(int ch) { return (ch & 31) * 4 + (ch >> 5
 // the channel of value i of a partial result: a wave's 16 columns are four positions of each word
 __device__ __forceinline__ int part_channel(int i) { return ((i >> 2) & 3) * 32 + (i >> 5) * 8 + ((i >> 4) & 1) * 4 + (i & 3); }
 
-// All-reduce over the 16 lanes of a DPP row by rotations; every lane ends with the result (of a sum, with the
-// result of an order of its own).  The rotation is part of the operation: an addition folds the move of a builtin with no
-// old value into itself, a maximum does not (the compiler first makes its operands quiet numbers, two more
-// operations), so that one is written out, behind the wait states that a rotation of a fresh result needs.
-template <int CTRL>
-__device__ __forceinline__ float row_rot(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ float row16_max(float v) {
-  asm volatile("s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_ror:1 row_mask:0xf bank_mask:0xf\n\t"
-               "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_ror:2 row_mask:0xf bank_mask:0xf\n\t"
-               "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
-               "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf" : "+v"(v));
-  return v;
-}
-__device__ __forceinline__ float row16_sum(float v) {
-  v += row_rot<0x121>(v);
-  v += row_rot<0x122>(v);
-  v += row_rot<0x124>(v);
-  return v + row_rot<0x128>(v);
-}
-
 // the first E of four values of a lane group's rows
 template <int E>
 __device__ __forceinline__ void put_rows(float* dst, const float (&v)[4]) {

@@ -139,23 +139,6 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowsArgs a) { merge_row
 constexpr int kWeightsRows = 16 * 48;  // most query rows of a kv head
 constexpr int kWeightsPos = 256;
 
-template <int CTRL>
-__device__ __forceinline__ float rotated(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ float max_of_16(float v) {
-  v = fmaxf(v, rotated<0x121>(v));
-  v = fmaxf(v, rotated<0x122>(v));
-  v = fmaxf(v, rotated<0x124>(v));
-  return fmaxf(v, rotated<0x128>(v));
-}
-__device__ __forceinline__ float sum_of_16(float v) {
-  v += rotated<0x121>(v);
-  v += rotated<0x122>(v);
-  v += rotated<0x124>(v);
-  return v + rotated<0x128>(v);
-}
-
 __device__ __forceinline__ void add_weights(const RowsArgs& a, int block, int head, const float* in, float* out, int64_t ld) {
   __shared__ float2 row_ml[kWeightsRows];
   __shared__ rows_f32x4 joined[4][64];
@@ -191,7 +174,7 @@ __device__ __forceinline__ void add_weights(const RowsArgs& a, int block, int he
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (k == 0 || !wide) M[k] = max_of_16(M[k]);
+      if (k == 0 || !wide) M[k] = row16_max(M[k]);
       L[k] = __builtin_amdgcn_exp2f(p[k].x - M[wide ? 0 : k]) * p[k].y;
     }
     if (wide) {
@@ -204,7 +187,7 @@ __device__ __forceinline__ void add_weights(const RowsArgs& a, int block, int he
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if (k > 0 && wide) break;
-      L[k] = sum_of_16(L[k]);
+      L[k] = row16_sum(L[k]);
       if (i0 == 0 && r0 + 16 * k < rows) row_ml[r0 + 16 * k] = make_float2(M[k], 1.f / L[k]);
     }
   }

@@ -62,6 +62,28 @@ __device__ __forceinline__ float wave_max(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// All-reduce over the 16 lanes of a DPP row by rotations; every lane ends with the result (of a sum, with the
+// result of an order of its own).  The rotation is part of the operation: an addition folds the move of a builtin with no
+// old value into itself, a maximum does not (the compiler first makes its operands quiet numbers, two more
+// operations), so that one is written out, behind the wait states that a rotation of a fresh result needs.
+template <int CTRL>
+__device__ __forceinline__ float row_rot(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float row16_max(float v) {
+  asm volatile("s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_ror:1 row_mask:0xf bank_mask:0xf\n\t"
+               "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_ror:2 row_mask:0xf bank_mask:0xf\n\t"
+               "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+               "s_nop 1\n\tv_max_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf" : "+v"(v));
+  return v;
+}
+__device__ __forceinline__ float row16_sum(float v) {
+  v += row_rot<0x121>(v);
+  v += row_rot<0x122>(v);
+  v += row_rot<0x124>(v);
+  return v + row_rot<0x128>(v);
+}
+
 constexpr int kRawBufferFlags = 0x00020000;  // word 3 of a raw (unstructured, 32-bit data) buffer descriptor
 
 __device__ __forceinline__ float bf16_to_f32(uint16_t u) { return __uint_as_float(((uint32_t)u) << 16); }
