@@ -464,7 +464,7 @@ int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout,
  * Workspace: cas_attention_shared_bytes (host only; 0 for arguments that cas_attention_shared refuses).  Like
  * every call that uses the context's workspace, two of them that may overlap (two streams, two captured
  * graphs replayed side by side) need contexts with workspaces of their own.  CAS_EINVAL unless the context's
- * device is current.
+ * device is current.  Below some four sequences cas_attention_multi is the shorter call.
  */
 int cas_attention_shared(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const int32_t* h_seqs, int prefix_len,
                          int full, const uint16_t* const* h_d_Q, const int32_t* h_ncols, int n_q_heads,

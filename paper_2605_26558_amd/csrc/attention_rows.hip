@@ -2,8 +2,8 @@
 // cached position received.
 //
 // cas_attention decodes a page of the cache for the query rows of one sequence.  Where a batch of sequences begins with the
-// same pages, the decode, which is most of the time (some nine vector operations per value), is the same for all of them:
-// here a workgroup decodes a page once for up to 256 query rows whichever sequence they belong to, and goes through a run
+// same pages, the decode, which is most of the time (a step of a walk is some nine vector operations, and the walks of the exact
+// form take 25 + 18 steps for 32 values at 60 % kept, those of the fullest of 64 lanes), is the same for all of them: here a workgroup decodes a page once for up to 256 query rows whichever sequence they belong to, and goes through a run
 // of pages with running maxima and sums, so that a row has one partial result per run and not per page.  What follows the
 // prefix goes through the same kernel, sequence by sequence, in the same launch.
 //   grid: (runs of the prefix x blocks of all rows, then per sequence runs x blocks of its rows) x kv heads
@@ -14,10 +14,14 @@
 // a vector of K 131 in the draft form: cheaper than decoding K again.
 //
 // Measured (8 kv heads, 60 % kept, t = 4; us, both launches; in brackets the bytes of the streams at the rate of a copy): 16 sequences
-// of 4 query heads a kv head over a shared 8192 and 500 of their own, draft 29 (5.5); 8 of 5 columns, exact, 300 of
-// their own 41 (8.9); 32 of 8 query heads over 32768, exact, shared exponents 124 (29).  One sequence with weights: 8192 positions,
-// exact 21 (7.7), 30011 and 7 columns 55 (28).  Bound by the vector operations of the decode: 60 to 71 % of a
-// SIMD's cycles, the matrix products and the LDS beside them (busy 20 and 39 % of the time with 256 rows).
+// of 4 query heads a kv head over a shared 8192 and 500 of their own, draft 30 (5.5), with shared exponents 36 (3.1); 8 of 5 columns,
+// exact, 300 of their own 42 (8.9), with shared exponents 47 (7.0); 32 of 8 query heads over 32768, exact, shared exponents 120 (29).
+// One sequence with weights: 8192 positions, exact 21.5 (7.7), draft 18 (3.7), with shared exponents 26 (6.1) and 22 (2.1); 30011 and 7
+// columns, exact 56 (28), draft 42 (14).  Bound by the vector operations of the decode: 58 to 66 % of a SIMD's cycles, the matrix
+// products and the LDS beside them (busy 21 and 41 % of the time with 256 rows).
+// Against the sequences' own decodes (cas_attention_multi), sharing / not: 2 sequences behind 703 positions 10.0 / 8.6, 4 behind 2000
+// 14.1 / 13.6, 8 of 5 columns behind 500, exact, 25 / 27, 16 behind 256 15 / 34, behind 8192 29 / 107: it pays from
+// some four sequences on, and for more whatever the prefix is.
 #include <algorithm>
 #include "attention_rows_kernel.inl"
 
@@ -229,7 +233,7 @@ __global__ __launch_bounds__(256) void rows_merge_weights_kernel(RowsArgs a, int
 // sixteen a CU (slots for 128 / 192 / 256 / 512 CUs: 32 sequences over 32768 positions 164 / 122 / 120 / 141 us, 8 over 8192
 // 44.7 / 40.1 / 45.5 / 64); the length of the runs behind a prefix does not depend on the other sequences' lengths, so that a
 // sequence's values do not either.
-constexpr int kCus = 256;
+constexpr int kCus = 256;  // a constant: the calls that say how much workspace is needed have no context to ask
 
 struct RowsPlan {
   RowsArgs a;
@@ -239,9 +243,11 @@ struct RowsPlan {
 };
 
 // Pages of a run, whole steps of it, for `columns` workgroups side by side (kv heads x blocks of rows) and `others`
-// workgroups behind them.  As many runs as there are workgroups at a time; or fewer, so that the others start with them,
+// workgroups behind them.  As many runs as there are workgroups at a time; or fewer, with room for one workgroup of each other,
 // where that lengthens the runs by less than the others would take afterwards (some five steps: three before the first
-// products and behind the last, two of their own).  us with all / room for a workgroup a sequence and head: 16 sequences over
+// products and behind the last, two of their own).  Others that tail_run_of cuts more finely, or that have no room, take a second
+// turn all the same: prefix / others / places of 16 sequences over 8192 positions 344 / 363 / 512, of 8 of 5 columns 176 / 135 / 256, of
+// 32 of 64 query heads over 32768 256 / 256 / 256.  us with all / room for a workgroup a sequence and head: 16 sequences over
 // 8192 positions, draft 33.1 / 30.0, 8 sequences of 5 columns 45.5 / 40.1; 32 sequences of 64 query heads over 32768 positions
 // take the same run either way.
 static int run_of(int64_t pages, int64_t columns, int64_t others, int tiles) {

@@ -167,6 +167,9 @@ __device__ __forceinline__ void load_window(__amdgpu_buffer_rsrc_t rs, int off, 
 // not meet.  (With V 128 bytes apart and reads of four tokens, four lanes met in every bank: 104 of the 286 thousand cycles
 // that a CU was busy with 256 rows over 32768 positions, now 31 of 189.)  The walks' writes meet more often for it (some 4 lanes in
 // place of 2), which is less.
+//
+// 128 registers a lane are what sixteen waves a CU leave.  The draft forms fit; the exact ones spill 10, 14, 9 and 1 of them at t = 4
+// (RT = 2, 4, 8, 16; with shared exponents 8, 8, 8 and 0), 31 at the most (t = 6, RT = 4).
 template <int T, bool FULL, bool MX, int RT>
 __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kernel(RowsArgs a) {
   constexpr int kWaves = RowsShape<RT>::kWaves, kPages = RowsShape<RT>::kPages, kSet = RowsLds<RT>::kSet;

@@ -11,9 +11,10 @@ namespace cas {
 // the threshold (the highest value that enough of them reach) is found kSelBits at a time: counts per digit in LDS, then the
 // digit with which enough are reached by a sum over the counts; and of its equals the lower positions are taken.  Kept positions
 // are dealt their places by counting those before them: ballots within a wave, one table of counts per wave and step for the workgroup.
-// Bound by latency (three passes of four barriers), for long rows by vector issue.  us, also where all scores are equal, and with two
-// bits a turn by ballots instead of digits in LDS: 8 rows of 2049 7.1 / 8.5 / 9.9, of 8192 12.3 / 14.7 / 17, of 21647 27 / 32 / 42;
-// 256 of 8192 14.5 / 15.6 / 19.7 (8 MB read and 4 written: 3 at the rate of a copy).
+// Bound by latency (three passes of four barriers), for long rows by vector issue of the one CU that a row has: the counts of a
+// row meet in one LDS, so a layer's 8 rows use 8 of 256 CUs.  us, also where all scores are equal, and with two bits a turn by
+// ballots instead of digits in LDS: 8 rows of 2049 6.8 / 8.5 / 9.9, of 8192 12.0 / 14.7 / 17, of 21647 27 / 32 / 42; 256 of 8192
+// 14.6 / 15.6 / 19.7 (8 MB read and 4 written: 3 at the rate of a copy).
 constexpr int kSelBits = 11, kSelBins = 1 << kSelBits;
 constexpr int kGroup = 4;  // steps between two looks at the row's end
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
 // write the same words): one load and one store of 16 bytes each, on multiples of 4 bytes, for every stream of four words
 // or more.  Bound by latency and address units.  With 16 bytes of the destination to a thread, which may reach into the next
 // vector, a quarter of the threads needs four loads, and their waves five: 175 us for 32 layers of 2048 of 8192 positions
-// (549 MB read and written: 115 at the rate of a copy), now 142.
+// (549 MB read and written: 115 at the rate of a copy), now 141, or 160 in a row of such moves.
 struct MoveStream {
   int begin, w;       // first word in the pool's part of a tile, words of a vector
   int first, groups;  // threads before, and to a vector
@@ -321,8 +322,10 @@ __global__ __launch_bounds__(kMoveThreads, 8) void move_kernel(MoveArgs a) {
 // In place: a workgroup takes one stream (blockIdx.x) of a head (blockIdx.y: K heads, then V heads) of layer blockIdx.z, as many
 // vectors a step as its places hold; all are read before one is written.  Position i moves to or before the place it comes from (the indices
 // ascend), so that no step writes what a later one reads.  The places of the next step's vectors are looked up under the
-// loads of this one.  Bound by the latency of a step; us, with a tile of 64 vectors and all streams of a pool a step / this: one layer, 1024
-// of 2049 positions 35 / 8.8, 2048 of 8192 75 / 19, 16384 of 32768 663 / 126; 32 layers, 2048 of 8192 176 / 178.
+// loads of this one.  Bound by the latency of a step (a stream of 7 or 8 groups has one per 585 or 512 vectors), and one
+// after the other: what a step writes over may be what the step before reads, so that several workgroups to a stream would have
+// to wait for one another.  us, with a tile of 64 vectors and all streams of a pool a step / this: one layer, 1024 of 2049 positions
+// 35 / 8.9, 2048 of 8192 75 / 19, 16384 of 32768 663 / 124; 32 layers, 2048 of 8192 176 / 177.
 constexpr int kInPlaceThreads = 1024, kInPlaceEach = 4;
 __global__ __launch_bounds__(kInPlaceThreads, 8) void move_in_place_kernel(MoveArgs a) {
   const KvGeom& g = a.g;
@@ -383,7 +386,7 @@ __global__ __launch_bounds__(kInPlaceThreads, 8) void move_in_place_kernel(MoveA
 static int launch_select(cas_ctx* ctx, const SelectArgs& a, int n_rows) {
   const dim3 grid(n_rows), block(kSelThreads);
   if (a.len <= 8 * kSelThreads) hipLaunchKernelGGL(select_kernel<8>, grid, block, 0, ctx->stream, a);
-  // longer rows from registers as long as they have room: 8 rows of 60000 85 us, 136 reading them again
+  // longer rows from registers too, up to 64 scores a lane, where 66 of the 128 spill: 8 rows of 60000 85 us, 136 reading them again
   else if (a.len <= 32 * kSelThreads) hipLaunchKernelGGL(select_kernel<32>, grid, block, 0, ctx->stream, a);
   else if (a.len <= 64 * kSelThreads) hipLaunchKernelGGL(select_kernel<64>, grid, block, 0, ctx->stream, a);
   else hipLaunchKernelGGL(select_kernel<0>, grid, block, 0, ctx->stream, a);

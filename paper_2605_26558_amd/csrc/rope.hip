@@ -129,7 +129,9 @@ struct RopeUnits {
 // the first.  A workgroup takes some heads of one token: `units` threads to a head, each with its part of the table's row in
 // registers for all heads that it goes through.  4099 tokens of 40 heads of 256 values, 168 MB: 31 us, 5.4 TB/s (a
 // copy of as much 33); 5 tokens of 48 heads of 128 values: 3.3 us, a launch.  Two, three or five heads of a thread requested at once: 30.6,
-// 30.6, 31.0, and 512 tokens of fp32 heads 6.1 -> 6.4, 6.8, 8.7.
+// 30.6, 31.0, and 512 tokens of fp32 heads 6.1 -> 6.4, 6.8, 8.7.  4096 tokens of 40 heads of 128, halves, 20 us; one value at a time
+// (rows a value apart from the alignment) 42, 2.0 TB/s in accesses of 2 bytes a lane, of fp32 heads 30; heads of 80 of which 20 channels
+// turn 41.
 template <int V, bool INTER>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   using U = RopeUnits<V, INTER>;
