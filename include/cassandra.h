@@ -442,7 +442,7 @@ typedef struct {
  * CAS_ROPE_INTERLEAVED channels 2i and 2i+1; channels from rot on are taken over.
  *   y_a = x_a cos - x_b sin,  y_b = x_b cos + x_a sin      (fp32, rounded to bf16 once)
  * transposed != 0: sin with the other sign, which takes a rotation back (magnitude 1) and is what gradients of
- * rotated heads go through.  rot <= head_dim <= 256 (CAS_ENOTSUP above).  The h_parts are HOST structs; their data
+ * rotated heads go through.  rot <= head_dim <= 256 and n_tok < 2^24 (CAS_ENOTSUP above).  The h_parts are HOST structs; their data
  * pointers need the alignment of their elements only.  CAS_EINVAL unless the context's device is current. */
 int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout, int transposed,
              const int32_t* d_pos, int pos0, int n_tok, int head_dim, int n_parts, const cas_rope_part* h_parts);

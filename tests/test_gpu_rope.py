@@ -312,3 +312,23 @@ def test_magnitudes_at_the_ends_of_fp32(env, mag):
     got = B.cas_rope_table(ctx, cfg, 500, 1000).cpu().numpy()
     # the documented bound; below the normal numbers a product is off by 2^-150, 2^-24 of the smallest normal one
     assert np.abs(got / mag - np.stack([np.cos(a), np.sin(a)], -1)).max() <= 2e-7
+
+
+def test_as_many_tokens_as_a_launch_has(env):
+    torch, B, ctx = env
+    table = B.cas_rope_table(ctx, B.cas_rope_cfg(2, 0, 10000.0, 1.0, 0, 0.0, 0.0, 1.0), 0, 8)
+    n = 1 << 24
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") & 7
+    x = torch.randn(n, 1, 2, device="cuda").bfloat16()
+    y = torch.full_like(x, 5.0)
+    with pytest.raises(B.CasError) as e:
+        B.cas_rope(ctx, table, [x], pos=pos, outs=[y])
+    assert e.value.code == B.CAS_ENOTSUP
+    torch.cuda.synchronize()
+    assert bool((y == 5.0).all())
+    B.cas_rope(ctx, table, [x[1:]], pos=pos[1:], outs=[y[1:]])
+    torch.cuda.synchronize()
+    for at in (1, n // 2 + 3, n - 9):   # the same eight positions in calls of their own
+        want = B.cas_rope(ctx, table, [x[at:at + 9].contiguous()], pos=pos[at:at + 9].contiguous())[0]
+        assert torch.equal(y[at:at + 9], want)
+    assert bool((y[0] == 5.0).all()) and bool((y[1:, 0, 0].float() != 5.0).any())
