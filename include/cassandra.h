@@ -516,6 +516,35 @@ int cas_kv_select(cas_ctx* ctx, const float* d_score, int64_t ld, int n_rows, in
 int cas_kv_evict(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, int seq, int dst_seq, const int32_t* d_index,
                  int n_keep);
 
+/* ---- drafted tokens against the target's probabilities, on the device ----------------------- */
+
+/*
+ * Verification of the drafts of n_seqs (0..256) sequences and the token that follows them, from random numbers that the caller
+ * gives (Sec. 2.2, Eq. 1, with the draw behind it that leaves tokens distributed as the target's).  Sequence s has h_k[s] (0..64)
+ * drafted tokens; rows and tokens lie sequence after sequence, as in cas_verify_step_multi:
+ *   d_target: float [sum of h_k + n_seqs][ldt], the target's logits: row i of a sequence behind i of its drafts
+ *   d_draft : float [sum of h_k][ldd], the logits that draft i was drawn from; NULL for drafts that are certain (q is 1 on them)
+ *   d_tokens: int32 [sum of h_k]
+ *   d_temp  : float [n_seqs] temperatures, NULL for 1; a sequence with 0, a negative one or NaN is greedy
+ *   d_r     : double [sum of h_k + n_seqs], in [0, 1): one for each draft, then one for the draw, sequence after sequence
+ * With p_i and q_i the softmax of row i / T (greedy: 1 on the lowest of the largest, 0 elsewhere), draft i is kept while all before
+ * it are, p_i(x_i) > 0 and r_i <= p_i(x_i) / q_i(x_i).  With n drafts kept, weights w = max(0, p_n - q_n) if n < h_k[s] (p_n where
+ * that is 0 everywhere), p_n otherwise, and u the sequence's last number, the token behind them is the lowest i with w_i > 0 and
+ * w_0 + .. + w_i > u * (sum of w), the last one with w_i > 0 if rounding leaves none.  -infinity and NaN among the logits
+ * have probability 0 (so a caller rules tokens out), and of a row that holds +infinity only these count, alike.  A row without any
+ * token gives -1.  A drafted token outside the vocabulary is not kept.
+ * Probabilities, sums and comparisons are 64-bit; sums are in an order that depends on vocab alone.
+ * d_n_accepted: int32 [n_seqs]; d_out: int32 [n_seqs][ld_out], ld_out above every h_k: the kept drafts, the token behind them, -1 up
+ * to ld_out.  d_p, d_q: NULL or float [sum of h_k], the probabilities of the drafted tokens.  Pointers need the
+ * alignment of their elements only.  h_k = 0 is plain sampling, which is how drafts are drawn in the first place.
+ * vocab <= 2^22, more sequences or drafts: CAS_ENOTSUP.  Workspace: cas_accept_tokens_bytes (host only; 0 for arguments that are
+ * refused).  CAS_EINVAL unless the context's device is current.  Enqueues kernels only.
+ */
+int cas_accept_tokens(cas_ctx* ctx, int n_seqs, const int32_t* h_k, int vocab, const float* d_target, int64_t ldt,
+                      const float* d_draft, int64_t ldd, const int32_t* d_tokens, const float* d_temp, const double* d_r,
+                      int32_t* d_n_accepted, int32_t* d_out, int64_t ld_out, float* d_p, float* d_q);
+size_t cas_accept_tokens_bytes(int n_seqs, const int32_t* h_k, int vocab);
+
 /* ---- model-level steps of one speculative round (Sec. 2.2, Sec. 4.1) --------------------- */
 
 /* Llama-3 style decoder (Fig. 2_1): RMSNorm -> q,k,v projection -> rotary embedding ->

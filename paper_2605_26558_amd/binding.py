@@ -141,6 +141,9 @@ _SIGNATURES = {
     "cas_kv_select": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p,
                                 C.c_void_p, C.c_int64]),
     "cas_kv_evict": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int]),
+    "cas_accept_tokens": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "cas_accept_tokens_bytes": (C.c_size_t, [C.c_int, C.c_void_p, C.c_int]),
     "cas_model_act_bytes": (C.c_int, [C.POINTER(cas_model_cfg), C.POINTER(C.c_size_t)]),
     "cas_model_create": (C.c_int, [C.POINTER(cas_model_cfg), C.POINTER(cas_model_weights), C.c_void_p, C.c_size_t,
                                    C.POINTER(C.c_void_p)]),
@@ -811,6 +814,43 @@ def cas_kv_evict(ctx: Context, kv: KVCache, layer0, n_layers, seq, dst_seq, inde
     assert layers == n_layers and heads == kv.desc.n_kv_heads
     assert index.is_cuda and index.is_contiguous() and index.dtype == ctx._torch.int32
     ctx._check(_lib().cas_kv_evict(ctx.h, kv.h, layer0, n_layers, seq, dst_seq, index.data_ptr(), n_keep), "cas_kv_evict")
+
+
+def cas_accept_tokens(ctx: Context, target, draft, tokens, ks, r, temperature=None, probs=False, n_accepted=None, out=None):
+    """target: float32 [sum(ks) + len(ks), vocab], draft: the same [sum(ks), vocab] or None for drafts that are certain, rows any
+    stride apart; tokens: int32 [sum(ks)]; r: float64 [sum(ks) + len(ks)]; temperature: float32 [len(ks)] or None.  Returns int32
+    (n_accepted [len(ks)], out [len(ks), max(ks) + 1 or more]: kept drafts, the token behind them, -1), and with `probs` the
+    probabilities of the drafted tokens, float32 (p, q)."""
+    torch = ctx._torch
+    S, n, most = len(ks), sum(ks), max(ks, default=0)
+    (rows, vocab), (ldt, one) = target.shape, target.stride()
+    assert rows == n + S and target.is_cuda and target.dtype == torch.float32 and (one == 1 or vocab == 1)
+    ldt, ldd, dev = vocab if rows <= 1 else ldt, 0, target.device  # a single row has no next one
+    if draft is not None:
+        (rows, v), (ldd, one) = draft.shape, draft.stride()
+        assert rows == n and v == vocab and draft.is_cuda and draft.dtype == torch.float32 and (one == 1 or vocab == 1)
+        ldd = vocab if rows <= 1 else ldd
+    for t, size, dtype in ((tokens, n, torch.int32), (r, n + S, torch.float64), (temperature, S, torch.float32)):
+        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.numel() == size)
+    assert r is not None and (tokens is not None or n == 0)
+    if n_accepted is None:
+        n_accepted = torch.empty(S, dtype=torch.int32, device=dev)
+    if out is None:
+        out = torch.empty((S, most + 1), dtype=torch.int32, device=dev)
+    assert n_accepted.is_cuda and n_accepted.is_contiguous() and n_accepted.dtype == torch.int32 and n_accepted.numel() == S
+    assert out.is_cuda and out.is_contiguous() and out.dtype == torch.int32 and out.shape[0] == S
+    pq = torch.empty((2, n), dtype=torch.float32, device=dev) if probs else None
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    ctx._check(_lib().cas_accept_tokens(ctx.h, S, (C.c_int32 * S)(*ks), vocab, target.data_ptr(), ldt, at(draft), ldd, at(tokens), at(temperature),
+                                        r.data_ptr(), n_accepted.data_ptr(), out.data_ptr(), out.shape[1], at(pq), pq.data_ptr() + 4 * n if probs else None),
+               "cas_accept_tokens")
+    return (n_accepted, out, pq[0], pq[1]) if probs else (n_accepted, out)
+
+
+def cas_accept_tokens_bytes(ks, vocab) -> int:
+    """Workspace of cas_accept_tokens (0: arguments it refuses)."""
+    ks = _i32(ks)
+    return int(_lib().cas_accept_tokens_bytes(len(ks), ks, vocab))
 
 
 def _tensor(ew: EncodedWeight) -> cas_tensor:
