@@ -447,6 +447,20 @@ typedef struct {
 int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout, int transposed,
              const int32_t* d_pos, int pos0, int n_tok, int head_dim, int n_parts, const cas_rope_part* h_parts);
 
+/* cas_rope and cas_kv_append in one launch, for n_seqs (0..32) distinct sequences of one layer: h_n_tok[i] (0 or more) tokens of sequence
+ * h_seqs[i], sequence after sequence, go to its positions len .. len + h_n_tok[i] - 1.  h_k and h_v: the parts that hold the tokens'
+ * keys and values, n_kv_heads heads of 128 values each, turned where their `turn` says so (keys, as a rule) and encoded;
+ * their d_y may be NULL, otherwise the bf16 vectors are written there as well (in-flight vectors of an attention call, say).
+ * h_q: NULL or the part of the queries, as for cas_rope.  d_table, n_pos, rot (2..128) and layout as for cas_rope.  d_pos: int32, the
+ * rotary position of each token, or NULL for its place in the cache.  A token whose rotary position is outside 0 .. n_pos-1 is
+ * padding: nothing is written for it, its place in the cache keeps what it holds.
+ * Bits are those of cas_rope followed by cas_kv_append; alignment, aliasing and limits as for cas_rope, page table entries outside the
+ * pool as for cas_kv_append.  No length changes: cas_kv_set_len once all layers are done.  CAS_ENOMEM where a sequence has no room for its
+ * tokens.  CAS_EINVAL unless the context's device is current. */
+int cas_kv_append_rope(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const int32_t* h_seqs, const int32_t* h_n_tok,
+                       const float* d_table, int n_pos, int rot, int layout, const int32_t* d_pos, const cas_rope_part* h_q,
+                       const cas_rope_part* h_k, const cas_rope_part* h_v);
+
 /* ---- attention of a batch over a prefix that its sequences share --------------------------- */
 
 /*

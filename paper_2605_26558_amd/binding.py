@@ -131,6 +131,8 @@ _SIGNATURES = {
     # host arrays as plain addresses here: the wrappers of these calls are on the way of single tokens
     "cas_rope": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int,
                            C.c_int, C.c_int, C.c_void_p]),
+    "cas_kv_append_rope": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "cas_attention_shared": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
                                        C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "cas_attention_shared_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.POINTER(C.c_int32), C.c_int, C.POINTER(C.c_int32),
@@ -711,6 +713,41 @@ def cas_rope(ctx: Context, table, xs, pos=None, pos0=0, layout=CAS_ROPE_HALF, tr
                                None if pos is None else pos.data_ptr(), int(pos0), n_tok, dim, len(xs),
                                (C.c_int64 * len(parts))(*parts)), "cas_rope")
     return ys
+
+
+def cas_kv_append_rope(ctx: Context, kv: KVCache, layer, seqs, n_toks, table, k, v, q=None, pos=None, layout=CAS_ROPE_HALF,
+                       turn=(True, True, False), q_out=None, k_out=None, v_out=None):
+    """Appends n_toks[i] tokens to sequence seqs[i] out of a projection: q [n_tok, n_q_heads, 128] or None, k and v [n_tok, n_kv_heads,
+    128], tensors as for cas_rope; table, pos and layout as there (pos None: the places in the cache).  turn: of q, k and v.
+    k_out, v_out: tensors for the turned vectors, which are encoded into the cache in any case.  Returns the turned queries (None
+    without q), as cas_rope does."""
+    torch = ctx._torch
+    n_pos, half, two = table.shape
+    assert table.is_cuda and table.is_contiguous() and table.dtype == torch.float32 and two == 2
+    n_tok, n, bits = sum(n_toks), len(seqs), _bf16_bits(torch)
+    assert n == len(n_toks) and (pos is None or (pos.is_cuda and pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == n_tok))
+    if q is not None and q_out is None:
+        q_out = torch.empty_like(q, dtype=torch.int16 if q.dtype == torch.float32 else None, memory_format=torch.contiguous_format)
+    parts = []
+    for x, y, t in ((q, q_out, turn[0]), (k, k_out, turn[1]), (v, v_out, turn[2])):
+        if x is None:
+            parts.append(None)
+            continue
+        shape, (ldx, head, one), fp32, ldy = x.shape, x.stride(), x.dtype == torch.float32, 0
+        heads = shape[1]
+        assert x.is_cuda and shape[0] == n_tok and shape[2] == 128 and one == 1 and (head == 128 or heads <= 1) and (fp32 or x.dtype in bits)
+        assert x is q or heads == kv.desc.n_kv_heads
+        if y is not None:
+            ldy, yhead, yone = y.stride()
+            assert y.is_cuda and y.shape == shape and y.dtype in bits and yone == 1 and (yhead == 128 or heads <= 1)
+        if n_tok <= 1:  # no second token that a distance would lead to
+            ldx, ldy = max(ldx, heads * 128), max(ldy, heads * 128)
+        # the words of a cas_rope_part
+        parts.append((C.c_int64 * 6)(x.data_ptr(), 0 if y is None else y.data_ptr(), ldx, ldy, heads | fp32 << 32, int(bool(t))))
+    i32 = C.c_int32 * n
+    ctx._check(_lib().cas_kv_append_rope(ctx.h, kv.h, layer, n, i32(*seqs), i32(*n_toks), table.data_ptr(), n_pos, 2 * half, layout,
+                                         None if pos is None else pos.data_ptr(), *parts), "cas_kv_append_rope")
+    return q_out
 
 
 def _i32(v):
