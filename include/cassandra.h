@@ -487,6 +487,27 @@ int cas_attention_shared(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const 
 size_t cas_attention_shared_bytes(const cas_kv* kv, int n_seqs, const int32_t* h_seqs, int prefix_len,
                                   const int32_t* h_ncols, int n_q_heads, const int32_t* h_n_new);
 
+/* ---- attention within a window ---------------------------------------------------------------- */
+
+/*
+ * cas_attention for n_seqs (1..32) distinct sequences of one layer whose columns see the first n_first positions and the last
+ * `window` up to their own: column c, at place P = len + n_new - ncols + c, sees position i <= P if i < n_first or i > P - window.
+ * n_first >= 0 (0: none), window >= 1 (1: itself); positions are places in the cache, in-flight ones behind the committed.
+ * Only the pages that hold such a position are looked up in the page table and read: the others may have been given
+ * back and their entries hold anything.  What a column does not see does not reach it, infinities and NaN included; an infinity among
+ * the committed V that it sees makes its channel infinite or NaN, as in cas_attention.
+ * Other arguments, limits and the tolerance as for cas_attention_shared: pages are added in runs whose length depends on
+ * the positions that the sequence sees, the heads, and the numbers of sequences and columns; a sequence's values do not depend on what the
+ * others hold, nor on how long they are.
+ * Workspace: cas_attention_window_bytes (host only; 0 for arguments that cas_attention_window refuses).  CAS_EINVAL unless the
+ * context's device is current.
+ */
+int cas_attention_window(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const int32_t* h_seqs, int n_first, int window, int full,
+                         const uint16_t* const* h_d_Q, const int32_t* h_ncols, int n_q_heads, const uint16_t* const* h_d_Knew,
+                         const uint16_t* const* h_d_Vnew, const int32_t* h_n_new, uint16_t* const* h_d_O);
+size_t cas_attention_window_bytes(const cas_kv* kv, int n_seqs, const int32_t* h_seqs, int n_first, int window, const int32_t* h_ncols,
+                                  int n_q_heads, const int32_t* h_n_new);
+
 /* ---- eviction from the cache by accumulated attention weight ------------------------------ */
 
 /*

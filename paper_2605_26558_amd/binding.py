@@ -137,6 +137,10 @@ _SIGNATURES = {
                                        C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "cas_attention_shared_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.POINTER(C.c_int32), C.c_int, C.POINTER(C.c_int32),
                                                 C.c_int, C.POINTER(C.c_int32)]),
+    "cas_attention_window": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p,
+                                       C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "cas_attention_window_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.POINTER(C.c_int32), C.c_int, C.c_int, C.POINTER(C.c_int32),
+                                                C.c_int, C.POINTER(C.c_int32)]),
     "cas_attention_weights": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int,
                                         C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64]),
     "cas_attention_weights_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int]),
@@ -788,6 +792,28 @@ def cas_attention_shared_bytes(kv: KVCache, seqs, prefix_len, ncols, n_q_heads, 
     """Workspace of cas_attention_shared for these sequences at their present lengths (0: arguments it refuses)."""
     seqs = _i32(seqs)
     return int(_lib().cas_attention_shared_bytes(kv.h, len(seqs), seqs, int(prefix_len), _i32(ncols), n_q_heads, _i32(n_new)))
+
+
+def cas_attention_window(ctx: Context, kv: KVCache, layer, seqs, n_first, window, full, Qs, Knews, Vnews, outs=None):
+    """Attention of several sequences whose columns see the first n_first positions and the last `window` up to their own: lists
+    of per-sequence tensors as in cas_attention."""
+    torch = ctx._torch
+    n = len(seqs)
+    outs = [torch.empty_like(q) for q in Qs] if outs is None else outs
+    heads = Qs[0].shape[1]
+    cols, new, ptrs = _check_attention(kv, heads, Qs, Knews, Vnews, outs, _bf16_bits(torch))
+    assert n == len(cols)
+    i32, ptr = C.c_int32 * n, C.c_void_p * n
+    q, k, v, o = (ptr(*p) for p in ptrs)
+    ctx._check(_lib().cas_attention_window(ctx.h, kv.h, layer, n, i32(*seqs), n_first, window, 1 if full else 0, q, i32(*cols), heads, k, v,
+                                           i32(*new), o), "cas_attention_window")
+    return outs
+
+
+def cas_attention_window_bytes(kv: KVCache, seqs, n_first, window, ncols, n_q_heads, n_new) -> int:
+    """Workspace of cas_attention_window for these sequences at their present lengths (0: arguments it refuses)."""
+    seqs = _i32(seqs)
+    return int(_lib().cas_attention_window_bytes(kv.h, len(seqs), seqs, int(n_first), int(window), _i32(ncols), n_q_heads, _i32(n_new)))
 
 
 def cas_attention_weights(ctx: Context, kv: KVCache, layer, seq, full, Q, Knew, Vnew, score_in=None, score_out=None, out=None):

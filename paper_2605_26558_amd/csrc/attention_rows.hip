@@ -24,13 +24,18 @@
 // some four sequences on, and for more whatever the prefix is.
 #include <algorithm>
 #include "attention_rows_kernel.inl"
+#include "kv_value.hpp"
 
 namespace cas {
 
-extern template int launch_rows_partial<true, false>(cas_ctx*, const RowsArgs&, int, int);
-extern template int launch_rows_partial<false, false>(cas_ctx*, const RowsArgs&, int, int);
-extern template int launch_rows_partial<true, true>(cas_ctx*, const RowsArgs&, int, int);
-extern template int launch_rows_partial<false, true>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_rows_partial<true, false, RowsArgs>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_rows_partial<true, false, RowsWindowArgs>(cas_ctx*, const RowsWindowArgs&, int, int);
+extern template int launch_rows_partial<false, false, RowsArgs>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_rows_partial<false, false, RowsWindowArgs>(cas_ctx*, const RowsWindowArgs&, int, int);
+extern template int launch_rows_partial<true, true, RowsArgs>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_rows_partial<true, true, RowsWindowArgs>(cas_ctx*, const RowsWindowArgs&, int, int);
+extern template int launch_rows_partial<false, true, RowsArgs>(cas_ctx*, const RowsArgs&, int, int);
+extern template int launch_rows_partial<false, true, RowsWindowArgs>(cas_ctx*, const RowsWindowArgs&, int, int);
 
 // Joins the partial results of a row in kMergeSums sums, of every kMergeSums-th split each, in order; then these in order.  One
 // wave forms all four or four waves one each (PARTS), a lane two channels: how many waves there are goes by the row with the most
@@ -38,8 +43,9 @@ extern template int launch_rows_partial<false, true>(cas_ctx*, const RowsArgs&, 
 // are requested at once, the outputs through buffer descriptors, of no length past the end of the part: what lies there reads as 0
 // without a branch.
 constexpr int kMergeAhead = 16, kMergeSums = 4;
-template <int PARTS>
-__device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head) {
+template <int PARTS, class ARGS>
+__device__ __forceinline__ void merge_row(const ARGS& a, int block, int head) {
+  constexpr bool kWindow = std::is_same<ARGS, RowsWindowArgs>::value;
   static_assert(PARTS == 1 || PARTS == kMergeSums, "");
   constexpr int kOwn = kMergeSums / PARTS;  // sums of a wave
   __shared__ float2 joined[4][64];
@@ -117,26 +123,54 @@ __device__ __forceinline__ void merge_row(const RowsArgs& a, int block, int head
     num.y += add.y;
   }
   const int c = r / a.grp, gi = r - c * a.grp;
+  auto lo = [](uint32_t x) { return __uint_as_float(x << 16); };
+  auto hi = [](uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); };
+  int from = 0;  // the first position that the row sees in its window
+  if constexpr (kWindow) from = me.len + me.n_new - me.ncols + c - a.window + 1;
+  auto add = [&](uint32_t q, uint32_t k, uint32_t v) {  // channels 2 lane, 2 lane + 1: the infinities and NaN among the two of v
+    const float w = __builtin_amdgcn_exp2f(wave_sum(lo(q) * lo(k) + hi(q) * hi(k)) * a.scale2 - M);
+    if ((v & 0x7F80u) == 0x7F80u) num.x += w * lo(v);
+    if ((v & 0x7F800000u) == 0x7F800000u) num.y += w * hi(v);
+  };
   if (__builtin_amdgcn_ballot_w64(odd != 0)) {  // those that the row sees, which the partial results left out
     const uint32_t q = reinterpret_cast<const uint32_t*>(a.Q[si] + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128)[lane];
     for (int i = 0; i <= me.n_new - me.ncols + c; ++i) {
       const int t = me.len + i;
       if (!(__shfl(odd, (t >> 4) - 4 * page0) >> (4 * (t & 15)) & 0xF)) continue;
+      if constexpr (kWindow)
+        if (t < from && t >= a.n_first) continue;
       const uint32_t k = reinterpret_cast<const uint32_t*>(a.Knew[si] + ((size_t)i * a.g.n_kv_heads + head) * 128)[lane];
       const uint32_t v = reinterpret_cast<const uint32_t*>(a.Vnew[si] + ((size_t)i * a.g.n_kv_heads + head) * 128)[lane];
-      auto lo = [](uint32_t x) { return __uint_as_float(x << 16); };
-      auto hi = [](uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); };
-      const float w = __builtin_amdgcn_exp2f(wave_sum(lo(q) * lo(k) + hi(q) * hi(k)) * a.scale2 - M);
-      if ((v & 0x7F80u) == 0x7F80u) num.x += w * lo(v);
-      if ((v & 0x7F800000u) == 0x7F800000u) num.y += w * hi(v);
+      add(q, k, v);
+    }
+  }
+  if constexpr (kWindow) {  // and those among committed positions that only some columns see
+    const WindowPages pages(a.n_first, a.window, me.len, me.len + me.n_new, me.ncols);
+    if (pages.zone0 < pages.zone1) {
+      const uint32_t* edge = a.edge + ((size_t)si * a.g.n_kv_heads + head) * 2;
+      const int slab = pages.zone0 >> 4, slabs = ((pages.zone1 - 1) >> 4) - slab + 1;
+      const uint32_t bits = edge[0] | (slabs > 1 ? edge[1] << 16 : 0u);
+      if (bits) {
+        const SeqTable t_seq(a.seq);
+        const uint32_t q = reinterpret_cast<const uint32_t*>(a.Q[si] + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128)[lane];
+        for (int t = max(pages.zone0, from); t < pages.zone1; ++t) {
+          if (!(bits >> (t - 16 * slab) & 1)) continue;
+          const int page = min(max(a.table[(size_t)t_seq[si] * a.g.max_pages_per_seq + (t >> 6)], 0), a.g.n_pages - 1);
+          auto two = [&](int kv) {
+            auto one = [&](int col) -> uint32_t { return cached_value(a.g, a.spec_pool, a.verif_pool, a.layer, page, kv, head, t & 63, col, a.full); };
+            return one(2 * lane) | one(2 * lane + 1) << 16;
+          };
+          add(q, two(0), two(1));
+        }
+      }
     }
   }
   uint32_t* out = reinterpret_cast<uint32_t*>(a.O[si] + ((size_t)c * a.n_q_heads + head * a.grp + gi) * 128) + lane;
   *out = (uint32_t)f32_to_bf16(num.x / den) | ((uint32_t)f32_to_bf16(num.y / den) << 16);
 }
 
-template <int PARTS>
-__global__ __launch_bounds__(256) void rows_merge_kernel(RowsArgs a) { merge_row<PARTS>(a, blockIdx.x, blockIdx.y); }
+template <int PARTS, class ARGS>
+__global__ __launch_bounds__(256) void rows_merge_kernel(ARGS a) { merge_row<PARTS>(a, blockIdx.x, blockIdx.y); }
 
 // Weights of 256 positions of a kv head.  Every row's maximum and sum first, 16 lanes to a row; then the waves take every
 // fourth row each, four positions a lane and eight rows requested at once, and are added in order.
@@ -236,7 +270,7 @@ __global__ __launch_bounds__(256) void rows_merge_weights_kernel(RowsArgs a, int
 constexpr int kCus = 256;  // a constant: the calls that say how much workspace is needed have no context to ask
 
 struct RowsPlan {
-  RowsArgs a;
+  RowsWindowArgs a;  // windowless calls pass the part that is theirs
   int tiles;   // of 16 query rows of a workgroup
   int items;
   size_t bytes;
@@ -277,13 +311,21 @@ static int tail_run_of(int64_t pages, int64_t columns, int tiles) {
 static int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 
 // What a call will launch and need; Q, Knew, Vnew and O are left to the caller.
+struct RowsWindow {
+  int n_first, window;
+};
 static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int prefix_len, const int32_t* ncols, int n_q_heads,
-                     const int32_t* n_new, bool weights, RowsPlan* out) {
+                     const int32_t* n_new, bool weights, RowsPlan* out, const RowsWindow* window = nullptr) {
+  if (window && (window->n_first < 0 || window->window < 1)) return CAS_EINVAL;
   if (!kv || n_seqs < 1 || n_seqs > kRowsSeqs || !seqs || !ncols || !n_new || prefix_len < 0) return CAS_EINVAL;
   const KvGeom& g = kv->geom;
   if (n_q_heads < g.n_kv_heads || n_q_heads % g.n_kv_heads != 0) return CAS_EINVAL;
   RowsPlan p{};
-  RowsArgs& a = p.a;
+  RowsWindowArgs& a = p.a;
+  if (window) {
+    a.n_first = std::min(window->n_first, 0x7FFFFFFF - 63);
+    a.window = window->window;
+  }
   a.g = g;
   a.n_q_heads = n_q_heads;
   a.grp = n_q_heads / g.n_kv_heads;
@@ -304,6 +346,7 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
     const int64_t pages_i = ((int64_t)a.len[i] + a.n_new[i] + 63) / 64;
     if (pages_i > g.max_pages_per_seq) return CAS_ENOMEM;
     pages[i] = (int)pages_i;
+    if (window) pages[i] -= WindowPages(a.n_first, a.window, a.len[i], a.len[i] + a.n_new[i], a.ncols[i]).skip;
     a.row0[i] = (int)rows;
     rows += ncols[i] * a.grp;
     most = std::max(most, ncols[i] * a.grp);
@@ -349,6 +392,10 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
     a.score_ld = ((int64_t)a.len[0] + a.n_new[0] + 63) / 64 * 64;
     off += up256(a.score_ld * g.n_kv_heads * a.rows * 4);
   }
+  if (window) {
+    a.edge = (uint32_t*)(uintptr_t)off;
+    off += up256((int64_t)n_seqs * g.n_kv_heads * 8);
+  }
   p.bytes = (size_t)off;
   a.out_prefix = (float*)0;
   a.out_tail = (float*)(uintptr_t)(first * 512);
@@ -360,11 +407,18 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   return CAS_OK;
 }
 
-static void place(RowsArgs& a, void* ws) {  // offsets into the workspace become addresses
+static void place(RowsWindowArgs& a, void* ws) {  // offsets into the workspace become addresses
   char* b = (char*)ws;
   auto at = [&](auto*& p) { p = (std::remove_reference_t<decltype(p)>)(b + (uintptr_t)p); };
   at(a.out_prefix); at(a.out_tail); at(a.ml_prefix); at(a.ml_tail); at(a.odd);
   if (a.score) at(a.score);
+  if (a.edge) at(a.edge);
+}
+
+template <class ARGS>
+static int launch_partial_form(cas_ctx* ctx, const ARGS& a, int full, int tiles, int items) {
+  return a.g.mx ? (full ? launch_rows_partial<true, true, ARGS>(ctx, a, tiles, items) : launch_rows_partial<false, true, ARGS>(ctx, a, tiles, items))
+                : (full ? launch_rows_partial<true, false, ARGS>(ctx, a, tiles, items) : launch_rows_partial<false, false, ARGS>(ctx, a, tiles, items));
 }
 
 // weights: where the sums of a call for one sequence go
@@ -373,16 +427,17 @@ struct RowsWeights {
   float* out;
   int64_t ld;
 };
+template <class ARGS = RowsArgs>
 static int launch_rows(cas_ctx* ctx, cas_kv* kv, RowsPlan& p, int layer, int full, const RowsWeights* weights = nullptr) {
   if (!ctx->d_ws || !aligned256(ctx->d_ws) || p.bytes > ctx->ws_bytes) return ctx->d_ws && !aligned256(ctx->d_ws) ? CAS_EINVAL : CAS_ENOMEM;
-  RowsArgs& a = p.a;
-  place(a, ctx->d_ws);
+  place(p.a, ctx->d_ws);
+  p.a.full = full ? 1 : 0;
+  ARGS& a = p.a;
   a.spec_pool = (const uint32_t*)kv->d_spec;
   a.verif_pool = (const uint32_t*)kv->d_verif;
   a.table = kv->d_page_table;
   a.layer = layer;
-  const int rc = a.g.mx ? (full ? launch_rows_partial<true, true>(ctx, a, p.tiles, p.items) : launch_rows_partial<false, true>(ctx, a, p.tiles, p.items))
-                        : (full ? launch_rows_partial<true, false>(ctx, a, p.tiles, p.items) : launch_rows_partial<false, false>(ctx, a, p.tiles, p.items));
+  const int rc = launch_partial_form<ARGS>(ctx, a, full, p.tiles, p.items);
   if (rc != CAS_OK) return rc;
   int most = 0;  // splits of a row: one wave can have 16 outputs in flight, so longer rows are shared by four
   for (int i = 0; i < a.n_seqs; ++i) most = std::max(most, a.prefix_splits + a.splits[i]);
@@ -392,10 +447,20 @@ static int launch_rows(cas_ctx* ctx, cas_kv* kv, RowsPlan& p, int layer, int ful
     hipLaunchKernelGGL(parts == 1 ? rows_merge_weights_kernel<1> : rows_merge_weights_kernel<4>, grid, dim3(256), 0, ctx->stream, a, blocks,
                        weights->in, weights->out, weights->ld);
   } else {
-    hipLaunchKernelGGL(parts == 1 ? rows_merge_kernel<1> : rows_merge_kernel<4>, dim3(blocks, a.g.n_kv_heads), dim3(256), 0, ctx->stream, a);
+    hipLaunchKernelGGL((parts == 1 ? rows_merge_kernel<1, ARGS> : rows_merge_kernel<4, ARGS>), dim3(blocks, a.g.n_kv_heads), dim3(256), 0, ctx->stream, a);
   }
   CAS_HIP(ctx, hipGetLastError());
   return CAS_OK;
+}
+
+// The sequences' tensors; false if one is missing or not aligned
+static bool take_tensors(RowsArgs& a, const uint16_t* const* Q, const uint16_t* const* Knew, const uint16_t* const* Vnew, uint16_t* const* O) {
+  for (int i = 0; i < a.n_seqs; ++i) {
+    a.Q[i] = Q[i]; a.Knew[i] = Knew[i]; a.Vnew[i] = Vnew[i]; a.O[i] = O[i];
+    for (const void* d : {(const void*)Q[i], (const void*)Knew[i], (const void*)Vnew[i], (const void*)O[i]})
+      if (!d || !aligned256(d)) return false;
+  }
+  return true;
 }
 
 }  // namespace cas
@@ -410,12 +475,7 @@ int cas_attention_shared(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const 
   cas::RowsPlan p;
   const int rc = cas::plan_rows(kv, n_seqs, h_seqs, prefix_len, h_ncols, n_q_heads, h_n_new, false, &p);
   if (rc != CAS_OK) return rc;
-  for (int i = 0; i < n_seqs; ++i) {
-    p.a.Q[i] = h_d_Q[i]; p.a.Knew[i] = h_d_Knew[i]; p.a.Vnew[i] = h_d_Vnew[i]; p.a.O[i] = h_d_O[i];
-    for (const void* d : {(const void*)h_d_Q[i], (const void*)h_d_Knew[i], (const void*)h_d_Vnew[i], (const void*)h_d_O[i]})
-      if (!d || !cas::aligned256(d)) return CAS_EINVAL;
-  }
-  if (!cas::on_device(ctx)) return CAS_EINVAL;
+  if (!cas::take_tensors(p.a, h_d_Q, h_d_Knew, h_d_Vnew, h_d_O) || !cas::on_device(ctx)) return CAS_EINVAL;
   return cas::launch_rows(ctx, kv, p, layer, full);
 }
 
@@ -444,6 +504,25 @@ int cas_attention_weights(cas_ctx* ctx, cas_kv* kv, int layer, int seq, int full
 size_t cas_attention_weights_bytes(const cas_kv* kv, int seq, int ncols, int n_q_heads, int n_new) {
   cas::RowsPlan p;
   return cas::plan_rows(kv, 1, &seq, 0, &ncols, n_q_heads, &n_new, true, &p) == CAS_OK ? p.bytes : 0;
+}
+
+int cas_attention_window(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const int32_t* h_seqs, int n_first, int window, int full,
+                         const uint16_t* const* h_d_Q, const int32_t* h_ncols, int n_q_heads, const uint16_t* const* h_d_Knew,
+                         const uint16_t* const* h_d_Vnew, const int32_t* h_n_new, uint16_t* const* h_d_O) {
+  if (!ctx || !kv || layer < 0 || layer >= kv->desc.n_layers || !h_d_Q || !h_d_Knew || !h_d_Vnew || !h_d_O) return CAS_EINVAL;
+  cas::RowsPlan p;
+  const cas::RowsWindow w{n_first, window};
+  const int rc = cas::plan_rows(kv, n_seqs, h_seqs, 0, h_ncols, n_q_heads, h_n_new, false, &p, &w);
+  if (rc != CAS_OK) return rc;
+  if (!cas::take_tensors(p.a, h_d_Q, h_d_Knew, h_d_Vnew, h_d_O) || !cas::on_device(ctx)) return CAS_EINVAL;
+  return cas::launch_rows<cas::RowsWindowArgs>(ctx, kv, p, layer, full);
+}
+
+size_t cas_attention_window_bytes(const cas_kv* kv, int n_seqs, const int32_t* h_seqs, int n_first, int window, const int32_t* h_ncols,
+                                  int n_q_heads, const int32_t* h_n_new) {
+  cas::RowsPlan p;
+  const cas::RowsWindow w{n_first, window};
+  return cas::plan_rows(kv, n_seqs, h_seqs, 0, h_ncols, n_q_heads, h_n_new, false, &p, &w) == CAS_OK ? p.bytes : 0;
 }
 
 }  // extern "C"

@@ -2,5 +2,5 @@
 #include "attention_rows_kernel.inl"
 
 namespace cas {
-template int launch_rows_partial<true, false>(cas_ctx*, const RowsArgs&, int, int);
+template int launch_rows_partial<true, false, RowsArgs>(cas_ctx*, const RowsArgs&, int, int);
 }  // namespace cas

@@ -51,6 +51,30 @@ struct RowsArgs {
   uint32_t part0[kRowsSeqs]; // partial results (row, run, kv head) behind the prefix, of the sequences before
 };
 
+// The form of attention within a window (attention_rows.hip): column c, at place P = total - columns + c, sees position i <= P where
+// i < n_first or i > P - window.  Pages between the first positions and the window are left out: a run's pages are those that are left,
+// numbered one after the other.
+struct RowsWindowArgs : RowsArgs {
+  int n_first, window, full;
+  uint32_t* edge;  // [sequence][kv head][two slabs of 16 positions]: a bit per position that only some columns see and
+                   // whose V holds an infinity or a NaN
+};
+struct WindowPages {
+  int lowest;       // the first position that column 0 sees in its window; column c: c more.  May be below 0
+  int first_pages;  // pages with first positions
+  int skip;         // pages left out behind them
+  int zone0, zone1; // committed positions that only some columns see
+  __host__ __device__ __forceinline__ WindowPages(int n_first, int window, int len, int total, int ncols) {
+    lowest = total - ncols + 1 - window;
+    first_pages = (n_first + 63) >> 6;
+    const int from = lowest > 0 ? lowest >> 6 : 0;
+    skip = from > first_pages ? from - first_pages : 0;
+    zone0 = lowest > n_first ? lowest : n_first;
+    zone1 = lowest + ncols - 1 < len ? lowest + ncols - 1 : len;
+  }
+  __host__ __device__ __forceinline__ int page(int i) const { return i + (i >= first_pages ? skip : 0); }
+};
+
 // The tables of the sequences, an entry per lane: one load each, all at once; then the entry of the sequence whose share of a
 // table (of the numbers before each) holds n, as a scalar.
 struct SeqTable {
@@ -170,8 +194,9 @@ __device__ __forceinline__ void load_window(__amdgpu_buffer_rsrc_t rs, int off, 
 //
 // 128 registers a lane are what sixteen waves a CU leave.  The draft forms fit; the exact ones spill 10, 14, 9 and 1 of them at t = 4
 // (RT = 2, 4, 8, 16; with shared exponents 8, 8, 8 and 0), 31 at the most (t = 6, RT = 4).
-template <int T, bool FULL, bool MX, int RT>
-__global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kernel(RowsArgs a) {
+template <int T, bool FULL, bool MX, int RT, class ARGS>
+__global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kernel(ARGS a) {
+  constexpr bool kWindow = std::is_same<ARGS, RowsWindowArgs>::value;
   constexpr int kWaves = RowsShape<RT>::kWaves, kPages = RowsShape<RT>::kPages, kSet = RowsLds<RT>::kSet;
   extern __shared__ __align__(16) uint16_t tiles[];
   __shared__ float red[2][kWaves][16];
@@ -198,12 +223,28 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
   const int split = item / blocks, row_base = (item - split * blocks) * 16 * RT;
   const int len = prefix ? a.prefix_pages * 64 : t_len[si], total = prefix ? len : len + t_new[si];
   const int run = prefix ? a.prefix_run : t_run[si];
-  const int pg0 = (prefix ? 0 : a.prefix_pages) + split * run, pg1 = min(pg0 + run, (total + 63) / 64), steps = (pg1 - pg0 + kPages - 1) / kPages;
+  const int ncols = t_cols[si];
+  auto pages_of = [&]() {
+    if constexpr (kWindow) return WindowPages(a.n_first, a.window, len, total, ncols);
+    else return 0;
+  };
+  const auto win_pages = pages_of();
+  auto page_at = [&](int i) {  // which page of the sequence the i-th of a run is
+    if constexpr (kWindow) return win_pages.page(i);
+    else return i;
+  };
+  auto committed = [&](int pos) {  // a position of the cache that some row sees
+    if constexpr (kWindow) return pos < len && (pos >= win_pages.lowest || pos < a.n_first);
+    else return pos < len;
+  };
+  int left_out = 0;
+  if constexpr (kWindow) left_out = win_pages.skip;
+  const int pg0 = (prefix ? 0 : a.prefix_pages) + split * run, pg1 = min(pg0 + run, (total + 63) / 64 - left_out), steps = (pg1 - pg0 + kPages - 1) / kPages;
   const int32_t* page_row = a.table + (size_t)t_seq[si] * g.max_pages_per_seq;
   const uint32_t first = prefix ? 0 : (uint32_t)t_part0[si];  // of the partial results
   const int splits = prefix ? a.prefix_splits : t_splits[si];
   const bool idle = row_base + tile * 16 >= rows;   // a wave without rows decodes only
-  const int all_see = prefix ? 0x7FFFFFFF : total - t_cols[si];  // the last position that every row sees
+  const int all_see = prefix ? 0x7FFFFFFF : total - ncols;  // the last position that every row sees
 
   // ---- the wave's unit of a step: pool pages two steps ahead, bitmap words one, fields as soon as those are there.  The pools
   // are touched only for pages that hold committed positions
@@ -213,8 +254,8 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
   const int pitch = 2 * (kv ? kVPos : kKPos);  // bytes
   constexpr int kNone = -1, kFresh = -2;       // no page; one without committed positions
   auto page_of = [&](int step) {
-    const int pg = pg0 + kPages * step + slot;
-    return pg >= pg1 ? kNone : pg * 64 >= len ? kFresh : min(max(page_row[pg], 0), g.n_pages - 1);
+    const int i = pg0 + kPages * step + slot, pg = page_at(i);
+    return i >= pg1 ? kNone : pg * 64 >= len ? kFresh : min(max(page_row[pg], 0), g.n_pages - 1);
   };
   auto tile_of = [&](int page) { return (((size_t)a.layer * g.n_pages + page) * 2 + kv) * g.n_kv_heads + head; };
   uint32_t next_mask = 0, next_exp = 0;
@@ -222,7 +263,7 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
     next_mask = next_exp = 0;
     if (page < 0) return;
     const uint32_t* sp = a.spec_pool + tile_of(page) * g.tile_spec_words;
-    if ((pg0 + kPages * step + slot) * 64 + r < len) {
+    if (committed(page_at(pg0 + kPages * step + slot) * 64 + r)) {
       next_mask = sp[r * 4 + j];
       if constexpr (MX) next_exp = sp[64 * 4 + r];
     }
@@ -264,8 +305,9 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
   };
   auto decode = [&](int step, int page) {
     if (page == kNone) return;
-    const int set = step & 1, tok0 = (pg0 + kPages * step + slot) * 64;
-    const bool whole = tok0 + 64 <= len;  // of committed positions
+    const int set = step & 1, tok0 = page_at(pg0 + kPages * step + slot) * 64;
+    bool whole = tok0 + 64 <= len;  // of committed positions
+    if constexpr (kWindow) whole = whole && (tok0 >= win_pages.lowest || tok0 + 64 <= a.n_first);
     const uint32_t to = lds_address(tiles + set * kSet + col);
     if (!FULL || !whole) {  // what is not written has to read as 0: 512 or 576 groups of eight values
       uint16_t* const slab = tiles + set * kSet + slot * kRowsPage + (kv ? 4 * kKSlab + (u & 3) * kVSlab + kVPos : (u & 3) * kKSlab + kKPos);
@@ -278,7 +320,7 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
     if (page >= 0) {
       if constexpr (FULL && kLate) request_pruned(page);
       win.k.decode(mask, [&](int bp, uint16_t v) { lds_write(to, bp, pitch, v); }, shared_exp);
-      if constexpr (FULL) win.pr.decode(tok0 + r < len ? ~mask : 0u, [&](int bp, uint16_t v) { lds_write(to, bp, pitch, v); });
+      if constexpr (FULL) win.pr.decode(committed(tok0 + r) ? ~mask : 0u, [&](int bp, uint16_t v) { lds_write(to, bp, pitch, v); });
     }
     if (!whole) {  // in-flight vectors, eight values at a time
       const int pos = tok0 + r;
@@ -301,9 +343,35 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
           asm volatile("" ::: "memory");
         }
       }
-      if (kv) {
+      if (kv && (!kWindow || tok0 + 64 > len)) {
         const uint64_t lanes = __builtin_amdgcn_ballot_w64(odd);
         if (lane == 0) a.odd[(((size_t)si * g.n_kv_heads + head) * 2 + (tok0 - (len & ~63)) / 64) * 4 + (u & 3)] = lanes;
+      }
+    }
+    if constexpr (kWindow) {
+      // Committed positions that the later columns no longer see: an infinity or a NaN of their V, times 0, would reach these.  0 here,
+      // added where the partial results are joined
+      const int slab0 = tok0 + 16 * (u & 3);
+      if (kv && win_pages.zone0 < win_pages.zone1 && slab0 < win_pages.zone1 && slab0 + 16 > win_pages.zone0) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        uint16_t* const slab = tiles + set * kSet + slot * kRowsPage + 4 * kKSlab + (u & 3) * kVSlab + kVPos;
+        uint32_t odd = 0;
+        for (int k = lane; k < 256; k += 64) {  // eight tokens of a position and word
+          uint16_t* const at = slab + (k >> 3) * kVPos + (k & 7) * 8;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int token = (k & 1) * 8 + e, pos = slab0 + token;
+            if (pos >= win_pages.zone0 && pos < win_pages.zone1 && (at[e] & 0x7F80u) == 0x7F80u) {
+              odd |= 1u << token;
+              at[e] = 0;
+            }
+          }
+        }
+        uint32_t any = 0;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) any |= __builtin_amdgcn_ballot_w64(odd >> t & 1) ? 1u << t : 0u;
+        if (lane == 0) a.edge[((size_t)si * g.n_kv_heads + head) * 2 + (slab0 >> 4) - (win_pages.zone0 >> 4)] = any;
       }
     }
   };
@@ -357,8 +425,8 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
   // token of a page that the lane holds as element e of product tt: four of the slab (NS = 1), or of every eight of two
   auto token = [&](int tt) { return NS == 1 ? slab0 * 16 + 4 * mq : slab0 * 16 + 32 * (tt >> 1) + 8 * mq + 4 * (tt & 1); };
   auto products = [&](int step, int page) {
-    const int pg = pg0 + kPages * step + page, set = step & 1;
-    if (idle || pg >= pg1) return;
+    const int i = pg0 + kPages * step + page, set = step & 1, pg = page_at(i);
+    if (idle || i >= pg1) return;
     const uint16_t* const at = tiles + set * kSet + page * kRowsPage;
     rows_f32x4 x[NS];
 #pragma unroll
@@ -374,12 +442,18 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
       }
     }
     const int row = row_base + tile * 16 + mi;
-    if (pg * 64 + 63 > all_see) {
+    bool all_in = pg * 64 + 63 <= all_see;  // for every row
+    if constexpr (kWindow) all_in = all_in && (pg * 64 + 63 < a.n_first || pg * 64 >= win_pages.lowest + ncols - 1);
+    if (!all_in) {
       const int seen = all_see + (int)((uint32_t)row * a.grp_inv >> 16);  // column c sees c positions more
+      auto sees = [&](int pos) {
+        if constexpr (kWindow) return pos <= seen && (pos < a.n_first || pos > seen - a.window);
+        else return pos <= seen;
+      };
 #pragma unroll
       for (int tt = 0; tt < NS; ++tt) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[tt][e] = pg * 64 + token(tt) + e <= seen ? x[tt][e] : -INFINITY;
+        for (int e = 0; e < 4; ++e) x[tt][e] = sees(pg * 64 + token(tt) + e) ? x[tt][e] : -INFINITY;
       }
     }
     if (a.score != nullptr && row < rows) {
@@ -508,26 +582,26 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
   }
 }
 
-template <int T, bool FULL, bool MX, int RT>
-int launch_rows_tiles(cas_ctx* ctx, const RowsArgs& a, dim3 grid) {
+template <int T, bool FULL, bool MX, int RT, class ARGS>
+int launch_rows_tiles(cas_ctx* ctx, const ARGS& a, dim3 grid) {
   static LdsLimit lim;
-  const int rc = allow_lds(ctx, (const void*)attn_rows_kernel<T, FULL, MX, RT>, RowsLds<RT>::kBytes, lim);
+  const int rc = allow_lds(ctx, (const void*)attn_rows_kernel<T, FULL, MX, RT, ARGS>, RowsLds<RT>::kBytes, lim);
   if (rc != CAS_OK) return rc;
-  hipLaunchKernelGGL((attn_rows_kernel<T, FULL, MX, RT>), grid, dim3(64 * RowsShape<RT>::kWaves), RowsLds<RT>::kBytes, ctx->stream, a);
+  hipLaunchKernelGGL((attn_rows_kernel<T, FULL, MX, RT, ARGS>), grid, dim3(64 * RowsShape<RT>::kWaves), RowsLds<RT>::kBytes, ctx->stream, a);
   CAS_HIP(ctx, hipGetLastError());
   return CAS_OK;
 }
 
 // tiles: of 16 query rows a workgroup, 2, 4, 8 or 16
-template <bool FULL, bool MX>
-int launch_rows_partial(cas_ctx* ctx, const RowsArgs& a, int tiles, int items) {
+template <bool FULL, bool MX, class ARGS>
+int launch_rows_partial(cas_ctx* ctx, const ARGS& a, int tiles, int items) {
   const dim3 grid((unsigned)items * (unsigned)a.g.n_kv_heads);
 #define CAS_LAUNCH(TV)                                                           \
   case TV:                                                                       \
-    return tiles == 2   ? launch_rows_tiles<TV, FULL, MX, 2>(ctx, a, grid)       \
-           : tiles == 4 ? launch_rows_tiles<TV, FULL, MX, 4>(ctx, a, grid)       \
-           : tiles == 8 ? launch_rows_tiles<TV, FULL, MX, 8>(ctx, a, grid)       \
-                        : launch_rows_tiles<TV, FULL, MX, 16>(ctx, a, grid);
+    return tiles == 2   ? launch_rows_tiles<TV, FULL, MX, 2, ARGS>(ctx, a, grid)       \
+           : tiles == 4 ? launch_rows_tiles<TV, FULL, MX, 4, ARGS>(ctx, a, grid)       \
+           : tiles == 8 ? launch_rows_tiles<TV, FULL, MX, 8, ARGS>(ctx, a, grid)       \
+                        : launch_rows_tiles<TV, FULL, MX, 16, ARGS>(ctx, a, grid);
   switch (a.g.t) {
     CAS_LAUNCH(0) CAS_LAUNCH(1) CAS_LAUNCH(2) CAS_LAUNCH(3) CAS_LAUNCH(4) CAS_LAUNCH(5) CAS_LAUNCH(6) CAS_LAUNCH(7)
     default: return CAS_EINVAL;

@@ -5,6 +5,7 @@
 // head_dim = 128 values, K kept per row, in the same four-stream layout as a weight matrix
 // (bitmap and spec in the speculation pool; lo and pruned in the verification pool).
 #include "kv_append_kernel.inl"
+#include "kv_value.hpp"
 
 namespace cas {
 
@@ -65,32 +66,9 @@ __global__ __launch_bounds__(128) void kv_read_kernel(KvGeom g, const uint32_t* 
     (kv ? Vo : Ko)[((size_t)tok * g.n_kv_heads + head) * 128 + col] = 0;
     return;
   }
-  const int row = pos % g.page_tokens;
-  const size_t tile = (((size_t)layer * g.n_pages + page) * 2 + kv) * g.n_kv_heads + head;
-  const uint32_t* ts = spec_pool + tile * g.tile_spec_words;
-  const uint32_t* tv = verif_pool + tile * g.tile_verif_words;
-  const uint32_t* bm = ts + row * 4;
-  const int j = col >> 5, c = col & 31;
-  uint32_t p = 0;
-  for (int i = 0; i < j; ++i) p += __popc(bm[i]);
-  const uint32_t m = bm[j];
-  p += __popc(m & ((1u << c) - 1u));
-  const int fw = g.mx ? 9 - g.t : 16 - g.t;
-  uint32_t v;
-  if ((m >> c) & 1u) {
-    v = read_field(ts + g.spec_off + row * g.sw, p * fw, fw);
-    const uint32_t lo = (full && g.t) ? read_field(tv + row * g.lw, p * g.t, g.t) : 0u;
-    if (g.mx) {
-      const int E = (int)((ts[g.page_tokens * 4 + row] >> (8 * j)) & 0xFFu);
-      v = mx_word(v >> (8 - g.t), E, ((v & ((1u << (8 - g.t)) - 1u)) << g.t) | lo);
-    } else {
-      v = (v << g.t) | lo;
-    }
-  } else {
-    v = full ? read_field(tv + g.page_tokens * g.lw + row * g.pw, ((uint32_t)col - p) * 16, 16) : 0u;
-  }
+  const uint16_t v = cached_value(g, spec_pool, verif_pool, layer, page, kv, head, pos % g.page_tokens, col, full);
   uint16_t* dst = (kv ? Vo : Ko) + ((size_t)tok * g.n_kv_heads + head) * 128;
-  dst[col] = (uint16_t)v;
+  dst[col] = v;
 }
 
 int launch_kv_append(cas_ctx* ctx, cas_kv* kv, int layer, int seq, const uint16_t* K, const uint16_t* V, int n_tok,
