@@ -896,12 +896,12 @@ def cas_accept_tokens(ctx: Context, target, draft, tokens, ks, r, temperature=No
     for t, size, dtype in ((tokens, n, torch.int32), (r, n + S, torch.float64), (temperature, S, torch.float32)):
         assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.numel() == size)
     assert r is not None and (tokens is not None or n == 0)
+    for t, shape in ((n_accepted, (S,)), (out, (S, most + 1 if out is None else max(out.shape[1], most + 1)))):
+        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.int32 and t.shape == shape)
     if n_accepted is None:
         n_accepted = torch.empty(S, dtype=torch.int32, device=dev)
     if out is None:
         out = torch.empty((S, most + 1), dtype=torch.int32, device=dev)
-    assert n_accepted.is_cuda and n_accepted.is_contiguous() and n_accepted.dtype == torch.int32 and n_accepted.numel() == S
-    assert out.is_cuda and out.is_contiguous() and out.dtype == torch.int32 and out.shape[0] == S
     pq = torch.empty((2, n), dtype=torch.float32, device=dev) if probs else None
     at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     ctx._check(_lib().cas_accept_tokens(ctx.h, S, (C.c_int32 * S)(*ks), vocab, target.data_ptr(), ldt, at(draft), ldd, at(tokens), at(temperature),

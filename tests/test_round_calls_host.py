@@ -1,0 +1,146 @@
+"""Host parts of cas_kv_append_rope, cas_attention_window and cas_accept_tokens: refusals and sizes that need no device, and what
+the wrappers take."""
+import ctypes as C
+import math
+import types
+
+import pytest
+
+
+def _kv(B, n_kv=2, pages=8, seqs=3, per_seq=8):
+    """A cache object without memory behind it: nothing here reaches a launch."""
+    d = B.cas_kv_desc()
+    d.n_layers, d.n_kv_heads, d.head_dim, d.page_tokens, d.n_pages, d.max_seqs, d.max_pages_per_seq = 1, n_kv, 128, 64, pages, seqs, per_seq
+    d.fmt = B.cas_fmt(600, 4, 0)
+    assert B._lib().cas_kv_desc_init(C.byref(d)) == B.CAS_OK
+    h = C.c_void_p()
+    assert B._lib().cas_kv_create(C.byref(d), 4096, 4096, 4096, C.byref(h)) == B.CAS_OK
+    return types.SimpleNamespace(h=h, desc=d)
+
+
+def test_refusals_without_a_device():
+    from paper_2605_26558_amd import binding as B
+    lib, one = B._lib(), (C.c_int32 * 1)(1)
+    assert lib.cas_kv_append_rope(None, None, 0, 1, one, one, None, 4, 64, 0, None, None, None, None) == B.CAS_EINVAL
+    assert lib.cas_attention_window(None, None, 0, 1, one, 0, 8, 1, None, one, 8, None, None, one, None) == B.CAS_EINVAL
+    assert lib.cas_accept_tokens(None, 1, one, 10, None, 10, None, 0, None, None, None, None, None, 2, None, None) == B.CAS_EINVAL
+    assert lib.cas_attention_window_bytes(None, 1, one, 0, 8, one, 8, one) == 0
+
+
+def test_sizes_of_the_verification():
+    from paper_2605_26558_amd import binding as B
+    size = B.cas_accept_tokens_bytes
+    assert size([], 100) == 0 and size([0], 1) > 0
+    # 16 bytes a chunk of 4096 tokens and row, 8 a chunk and sequence, 4 a sequence, each rounded up to 256
+    assert size([4], 128256) == (9 * 32 * 16 + 255) // 256 * 256 + 256 + 256
+    assert size([64] * 256, 1 << 22) == (2 * 64 + 1) * 256 * 1024 * 16 + 256 * 1024 * 8 + 1024
+    for ks, vocab in (([65], 10), ([-1], 10), ([0] * 257, 10), ([1], 0), ([1], (1 << 22) + 1)):
+        assert size(ks, vocab) == 0, (ks, vocab)
+
+
+def test_workspace_of_a_window_goes_by_what_is_seen():
+    from paper_2605_26558_amd import binding as B
+    kv = _kv(B, pages=8, per_seq=1 << 20)
+    at = lambda length, first, window, cols=1: (B.cas_kv_set_len(kv, 0, length), B.cas_attention_window_bytes(kv, [0], first, window, [cols], 8, [cols]))[1]  # noqa: E731
+    whole = at(1000, 0, 2 ** 31 - 1)
+    assert whole == at(1000, 2 ** 31 - 1, 1) == at(1000, 0, 1001) and whole > at(1000, 0, 100)
+    assert at(1000, 4, 100) == at(60_000_000 // 64 * 64 + 1000 % 64, 4, 100)   # a far end costs nothing
+    assert at(1000, 4, 100) == at(1064, 4, 100)
+    for first, window, cols, new, heads in ((-1, 5, 1, 1, 8), (0, 0, 1, 1, 8), (0, -3, 1, 1, 8), (0, 5, 17, 17, 8), (0, 5, 2, 1, 8), (0, 5, 1, 65, 8), (0, 5, 1, 1, 7)):
+        assert B.cas_attention_window_bytes(kv, [0], first, window, [cols], heads, [new]) == 0
+    assert B.cas_attention_window_bytes(kv, [0, 0], 0, 5, [1, 1], 8, [1, 1]) == 0
+    B._lib().cas_kv_destroy(kv.h)
+
+
+@pytest.fixture
+def wrappers(monkeypatch):
+    """The binding with tensors that say they are on the GPU and a context that is none: a call whose arguments the wrapper takes
+    comes back from the library as CAS_EINVAL, one that it does not take raises AssertionError."""
+    import torch
+    from paper_2605_26558_amd import binding as B
+
+    class OnGpu(torch.Tensor):
+        is_cuda = True
+
+    def check(rc, what):
+        if rc != B.CAS_OK:
+            raise B.CasError(rc, what)
+
+    ctx = types.SimpleNamespace(_torch=torch, h=None, _check=check)
+    kv = types.SimpleNamespace(h=None, desc=types.SimpleNamespace(n_kv_heads=2, head_dim=128))
+    return torch, B, ctx, kv, lambda *shape, dtype=torch.bfloat16: torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+def _taken(B, call):
+    with pytest.raises((B.CasError, AssertionError)) as e:
+        call()
+    return isinstance(e.value, B.CasError) and e.value.code == B.CAS_EINVAL
+
+
+def test_types_that_the_wrappers_take(wrappers):
+    torch, B, ctx, kv, t = wrappers
+    bits = (torch.bfloat16, torch.int16, torch.uint16)
+    f32 = lambda *shape: t(*shape, dtype=torch.float32)  # noqa: E731
+    table = f32(4, 64, 2)
+    for dtype in (*bits, torch.float32, torch.float16, torch.float64, torch.int32):
+        for i in range(3):
+            x = [t(3, 4, 128), t(3, 2, 128), t(3, 2, 128)]
+            x[i] = x[i].to(dtype).as_subclass(type(table))
+            assert _taken(B, lambda: B.cas_kv_append_rope(ctx, kv, 0, [0], [3], table, x[1], x[2], q=x[0])) == (dtype in bits or dtype == torch.float32)
+            y = [None, None, None]
+            y[i] = t(*x[i].shape, dtype=dtype)
+            assert _taken(B, lambda: B.cas_kv_append_rope(ctx, kv, 0, [0], [3], table, t(3, 2, 128), t(3, 2, 128), q=t(3, 4, 128), q_out=y[0], k_out=y[1],
+                                                          v_out=y[2])) == (dtype in bits)
+        for i in range(4):
+            a = [t(1, 4, 128), t(1, 2, 128), t(1, 2, 128), t(1, 4, 128)]
+            a[i] = a[i].to(dtype).as_subclass(type(table))
+            assert _taken(B, lambda: B.cas_attention_window(ctx, kv, 0, [0], 4, 9, True, [a[0]], [a[1]], [a[2]], outs=[a[3]])) == (dtype in bits)
+        target, near, tokens, r, temp = f32(3, 50), f32(2, 50), t(2, dtype=torch.int32), t(3, dtype=torch.float64), f32(1)
+        accept = lambda a=target, b=near, c=tokens, d=r, e=temp, **how: B.cas_accept_tokens(ctx, a, b, c, [2], d, temperature=e, **how)  # noqa: E731
+        assert _taken(B, accept) and _taken(B, lambda: accept(b=None)) and _taken(B, lambda: accept(e=None))
+        assert _taken(B, lambda: accept(a=t(3, 50, dtype=dtype))) == (dtype == torch.float32) == _taken(B, lambda: accept(b=t(2, 50, dtype=dtype)))
+        assert _taken(B, lambda: accept(c=t(2, dtype=dtype))) == (dtype == torch.int32) == _taken(B, lambda: accept(out=t(1, 3, dtype=dtype)))
+        assert _taken(B, lambda: accept(d=t(3, dtype=dtype))) == (dtype == torch.float64)
+        assert _taken(B, lambda: accept(e=t(1, dtype=dtype))) == (dtype == torch.float32)
+
+
+def test_shapes_that_the_wrappers_do_not_take(wrappers):
+    torch, B, ctx, kv, t = wrappers
+    table = t(4, 64, 2, dtype=torch.float32)
+    append = lambda q=t(3, 4, 128), k=t(3, 2, 128), v=t(3, 2, 128), toks=[3], **how: B.cas_kv_append_rope(ctx, kv, 0, [0], toks, table, k, v, q=q, **how)  # noqa: E731,B006
+    assert _taken(B, append) and _taken(B, lambda: append(q=None))
+    for bad in (dict(k=t(3, 3, 128)), dict(v=t(2, 2, 128)), dict(q=t(3, 4, 64)), dict(toks=[2]), dict(toks=[1, 2]), dict(k=t(3, 128, 2).transpose(1, 2)),
+                dict(q=t(4, 3, 128).transpose(0, 1)), dict(pos=t(2, dtype=torch.int32)), dict(pos=t(3, dtype=torch.int64)), dict(q_out=t(3, 3, 128)),
+                dict(k_out=t(3, 2, 64))):
+        assert not _taken(B, lambda: append(**bad)), bad
+    f32 = lambda *shape: t(*shape, dtype=torch.float32)  # noqa: E731
+    accept = lambda a=f32(3, 50), b=f32(2, 50), c=t(2, dtype=torch.int32), d=t(3, dtype=torch.float64), **how: B.cas_accept_tokens(ctx, a, b, c, [2], d, **how)  # noqa: E731
+    assert _taken(B, accept)
+    for bad in (dict(a=f32(2, 50)), dict(b=f32(3, 50)), dict(b=f32(2, 51)), dict(c=t(3, dtype=torch.int32)), dict(c=None), dict(d=t(2, dtype=torch.float64)),
+                dict(a=f32(50, 3).T), dict(temperature=f32(2)), dict(out=t(2, 3, dtype=torch.int32)), dict(n_accepted=t(2, dtype=torch.int32))):
+        assert not _taken(B, lambda: accept(**bad)), bad
+    for tensors in ((t(1, 4, 128), t(1, 3, 128), t(1, 3, 128)), (t(1, 4, 64), t(1, 2, 128), t(1, 2, 128)), (t(1, 4, 128), t(2, 2, 128), t(1, 2, 128))):
+        assert not _taken(B, lambda: B.cas_attention_window(ctx, kv, 0, [0], 4, 9, True, *([x] for x in tensors), outs=[t(1, 4, 128)]))
+
+
+def test_exponential_of_the_verification_in_64_bits():
+    """The series and the reduction of exp64 in accept.hip, operation by operation: within 3e-16 of e^x where that is a normal number."""
+    import numpy as np
+    from fractions import Fraction
+
+    def fma(a, b, c):
+        return float(Fraction(a) * Fraction(b) + Fraction(c))
+    rng = np.random.Generator(np.random.Philox(2))
+    for x in [0.0, -1e-300, -1e-9, -0.34657359027997264, -0.3465735902799727, -0.5, -1.0, -708.3, *(-rng.exponential(20.0, 300)), *(-rng.random(200))]:
+        x = float(x)
+        n = float(np.rint(x * 1.4426950408889634))
+        r = fma(n, 4.2009150726810846e-11, fma(n, -0.69314718060195446, x))
+        assert abs(r) <= 0.34657359 * (1 + 1e-6)
+        y = 1.0 / math.factorial(13)
+        for i in range(12, -1, -1):
+            y = fma(y, r, 1.0 / math.factorial(i))
+        got = math.ldexp(y, int(n))
+        from decimal import Decimal, getcontext
+        getcontext().prec = 40
+        want = Decimal(x).exp()
+        assert abs(Decimal(got) - want) <= Decimal(3e-16) * want, x
