@@ -31,9 +31,9 @@ def test_sizes_of_the_verification():
     from paper_2605_26558_amd import binding as B
     size = B.cas_accept_tokens_bytes
     assert size([], 100) == 0 and size([0], 1) > 0
-    # 16 bytes a chunk of 4096 tokens and row, 8 a chunk and sequence, 4 a sequence, each rounded up to 256
-    assert size([4], 128256) == (9 * 32 * 16 + 255) // 256 * 256 + 256 + 256
-    assert size([64] * 256, 1 << 22) == (2 * 64 + 1) * 256 * 1024 * 16 + 256 * 1024 * 8 + 1024
+    # 16 bytes a chunk of 4096 tokens and row, 8 a piece of 2048 and sequence, 40 a sequence, each rounded up to 256
+    assert size([4], 128256) == (9 * 32 * 16 + 255) // 256 * 256 + 512 + 256
+    assert size([64] * 256, 1 << 22) == (2 * 64 + 1) * 256 * 1024 * 16 + 256 * 2048 * 8 + 256 * 40
     for ks, vocab in (([65], 10), ([-1], 10), ([0] * 257, 10), ([1], 0), ([1], (1 << 22) + 1)):
         assert size(ks, vocab) == 0, (ks, vocab)
 
@@ -124,23 +124,33 @@ def test_shapes_that_the_wrappers_do_not_take(wrappers):
 
 
 def test_exponential_of_the_verification_in_64_bits():
-    """The series and the reduction of exp64 in accept.hip, operation by operation: within 3e-16 of e^x where that is a normal number."""
-    import numpy as np
+    """exp2_64 of accept.hip, operation by operation: within 4e-14 of 2^y where that is a normal number, 1 at 0."""
+    import os
+    import re
+    from decimal import Decimal, getcontext
     from fractions import Fraction
+    import numpy as np
+    import paper_2605_26558_amd as P
+    getcontext().prec = 40
+    text = open(os.path.join(os.path.dirname(P.__file__), "csrc", "accept.hip"), encoding="utf-8").read()
+    body = text[text.index("double exp2_64(double y)"):]
+    body = body[:body.index("return")]
+    steps = [float(x) for x in re.findall(r"double e = ([0-9.e+-]+);", body) + re.findall(r"e = fma\(e, f, ([0-9.e+-]+)\);", body)]
+    assert len(steps) == 10
 
     def fma(a, b, c):
         return float(Fraction(a) * Fraction(b) + Fraction(c))
     rng = np.random.Generator(np.random.Philox(2))
-    for x in [0.0, -1e-300, -1e-9, -0.34657359027997264, -0.3465735902799727, -0.5, -1.0, -708.3, *(-rng.exponential(20.0, 300)), *(-rng.random(200))]:
-        x = float(x)
-        n = float(np.rint(x * 1.4426950408889634))
-        r = fma(n, 4.2009150726810846e-11, fma(n, -0.69314718060195446, x))
-        assert abs(r) <= 0.34657359 * (1 + 1e-6)
-        y = 1.0 / math.factorial(13)
-        for i in range(12, -1, -1):
-            y = fma(y, r, 1.0 / math.factorial(i))
-        got = math.ldexp(y, int(n))
-        from decimal import Decimal, getcontext
-        getcontext().prec = 40
-        want = Decimal(x).exp()
-        assert abs(Decimal(got) - want) <= Decimal(3e-16) * want, x
+    for y in [0.0, -1e-300, -1e-9, -0.5, -0.49999999999999994, -0.5000000000000001, -1.0, -1.5, -1021.9, *(-rng.exponential(30.0, 400)), *(-rng.random(400))]:
+        y = float(y)
+        m = y + 6755399441055744.0
+        n = int(m - 6755399441055744.0)
+        f = y - (m - 6755399441055744.0)
+        assert abs(f) <= 0.5 and (int(np.float64(m).view(np.int64)) & 0xFFFFFFFF) == n & 0xFFFFFFFF
+        e = steps[0]
+        for c in steps[1:]:
+            e = fma(e, f, c)
+        got = math.ldexp(e, n)
+        want = Decimal(2) ** Decimal(y)
+        assert abs(Decimal(got) - want) <= Decimal(4e-14) * want, y
+        assert y != 0.0 or got == 1.0
