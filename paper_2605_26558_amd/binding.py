@@ -4,6 +4,7 @@ path runs in the HIP kernels.  Loading fails loudly if the library has not been 
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -227,7 +228,7 @@ def _lib():
 
 def _bf16_bits(torch):
     """Types that hold a bf16 number: other numbers of two bytes would be read as bits of one."""
-    return (torch.bfloat16, torch.int16, torch.uint16)
+    return {torch.bfloat16, torch.int16, torch.uint16}
 
 
 def _ptr(t):
@@ -775,17 +776,22 @@ def cas_attention_shared(ctx: Context, kv: KVCache, layer, seqs, prefix_len, ful
     return outs
 
 
+_DTYPE, _IS_CUDA, _SHAPE, _NBYTES = (operator.attrgetter(x) for x in ("dtype", "is_cuda", "shape", "nbytes"))
+
+
 def _check_attention(kv: KVCache, heads, Qs, Knews, Vnews, outs, bits):
     """Shapes, types and layout of the sequences' tensors: their columns, in-flight vectors, and addresses."""
-    d = kv.desc.head_dim
-    qs, ks = [t.shape for t in Qs], [t.shape for t in Knews]
-    cols, new = [s[0] for s in qs], [s[0] for s in ks]
-    qt, kt = (heads, d), (kv.desc.n_kv_heads, d)
-    assert all([s[1:] == qt for s in qs]) and all([s[1:] == kt for s in ks]) and len(cols) == len(new) == len(Vnews) == len(outs)
-    assert [t.nbytes for t in Vnews] == [2 * c * kt[0] * d for c in new] and [t.nbytes for t in outs] == [2 * c * heads * d for c in cols]
-    for ts in (Qs, Knews, Vnews, outs):
-        assert all([t.is_contiguous() and t.is_cuda and t.dtype in bits for t in ts])
-    return cols, new, [[t.data_ptr() for t in ts] for ts in (Qs, Knews, Vnews, outs)]
+    d, n, ts = kv.desc.head_dim, len(Qs), [*Qs, *Knews, *Vnews, *outs]
+    assert n == len(Knews) == len(Vnews) == len(outs)
+    qs, ks = list(map(_SHAPE, Qs)), list(map(_SHAPE, Knews))
+    cols, new, sizes = [s[0] for s in qs], [s[0] for s in ks], list(map(_NBYTES, ts))
+    kh = kv.desc.n_kv_heads
+    assert qs == [(c, heads, d) for c in cols] and ks == [(c, kh, d) for c in new]
+    assert sizes[2 * n:] == sizes[n:2 * n] + sizes[:n] and all(map(_IS_CUDA, ts)) and set(map(_DTYPE, ts)) <= bits
+    tensor = type(ts[0])
+    assert all(map(tensor.is_contiguous, ts))
+    ptrs = list(map(tensor.data_ptr, ts))
+    return cols, new, [ptrs[i:i + n] for i in range(0, 4 * n, n)]
 
 
 def cas_attention_shared_bytes(kv: KVCache, seqs, prefix_len, ncols, n_q_heads, n_new) -> int:
@@ -907,7 +913,7 @@ def cas_accept_tokens(ctx: Context, target, draft, tokens, ks, r, temperature=No
     ctx._check(_lib().cas_accept_tokens(ctx.h, S, (C.c_int32 * S)(*ks), vocab, target.data_ptr(), ldt, at(draft), ldd, at(tokens), at(temperature),
                                         r.data_ptr(), n_accepted.data_ptr(), out.data_ptr(), out.shape[1], at(pq), pq.data_ptr() + 4 * n if probs else None),
                "cas_accept_tokens")
-    return (n_accepted, out, pq[0], pq[1]) if probs else (n_accepted, out)
+    return (n_accepted, out, *pq.unbind(0)) if probs else (n_accepted, out)
 
 
 def cas_accept_tokens_bytes(ks, vocab) -> int:

@@ -368,7 +368,7 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
   for (int i = 0; i < n_seqs; ++i) {
     const int r = ncols[i] * a.grp;
     const int64_t tail = pages[i] - a.prefix_pages, blocks = (r + block - 1) / block;
-    a.run[i] = weights ? run_of(tail, g.n_kv_heads * blocks, 0, p.tiles) : tail_run_of(tail, (int64_t)n_seqs * g.n_kv_heads * blocks, p.tiles);
+    a.run[i] = weights || window ? run_of(tail, (int64_t)n_seqs * g.n_kv_heads * blocks, 0, p.tiles) : tail_run_of(tail, (int64_t)n_seqs * g.n_kv_heads * blocks, p.tiles);
     a.splits[i] = (int)((tail + a.run[i] - 1) / a.run[i]);
     a.item0[i] = (int)items;
     a.part0[i] = (uint32_t)parts;

@@ -208,7 +208,11 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
   const int slot = kPages == 1 ? 0 : wv >> 3, u = wv & 7;  // page of the step, place among its waves
   const int kv = u >> 2, r = (u & 3) * 16 + (lane >> 2), j = lane & 3;  // decode role: K or V, token, word
   const int mi = lane & 15, mq = lane >> 4;            // role in the products: query row (token, channel) mi, group mq
-  const int tile = RT == 16 ? wv : u % RT, slab0 = RT >= 8 ? 0 : (u / RT) * NS;   // and the wave's: tile of rows, first slab
+  // and the wave's: tile of rows, first slab.  Waves of a workgroup go to the SIMDs in turn: where fewer rows leave tiles empty, the
+  // waves that have products are spread over all four
+  const int tile = RT == 16 ? wv : RT == 2 ? u >> 2 : RT == 4 ? (u + (u >> 2)) & 3 : u;
+  const int slab0 = RT >= 8 ? 0 : RT == 2 ? u & 3 : (u >> 2) * NS;
+  auto wave_of = [](int t, int w) { return RT == 2 ? 4 * t + w : RT == 4 ? 4 * w + ((t - w) & 3) : w * RT + t; };  // w-th wave of a tile
 
   // ---- what this workgroup works on (uniform)
   const SeqTable t_item0(a.item0), t_len(a.len), t_new(a.n_new), t_cols(a.ncols), t_seq(a.seq), t_splits(a.splits), t_part0(a.part0), t_run(a.run);
@@ -319,7 +323,24 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
     }
     if (page >= 0) {
       if constexpr (FULL && kLate) request_pruned(page);
-      win.k.decode(mask, [&](int bp, uint16_t v) { lds_write(to, bp, pitch, v); }, shared_exp);
+      if constexpr (MX) {
+        win.k.decode_finite(mask, [&](int bp, uint32_t v) { lds_write(to, bp, pitch, (uint16_t)(v >> 16)); }, shared_exp);
+        if (__builtin_amdgcn_ballot_w64(shared_exp == 255 && mask != 0u)) {  // words of infinities or NaN: value by value, from memory
+          const uint32_t* const sp = a.spec_pool + tile_of(page) * g.tile_spec_words + g.spec_off + r * g.sw;
+          const uint32_t* const lo = a.verif_pool + tile_of(page) * g.tile_verif_words + r * g.lw;
+          uint32_t m = shared_exp == 255 ? mask : 0u, at = kept_before;
+          while (m) {
+            uint32_t v = read_field(sp, at * (9 - T), 9 - T), mag = v & ((1u << (8 - T)) - 1u);
+            mag <<= T;
+            if constexpr (FULL && T > 0) mag |= read_field(lo, at * T, T);
+            lds_write(to, lowest_bit(m), pitch, (uint16_t)mx_word(v >> (8 - T), shared_exp, mag));
+            m &= m - 1u;
+            ++at;
+          }
+        }
+      } else {
+        win.k.decode(mask, [&](int bp, uint16_t v) { lds_write(to, bp, pitch, v); });
+      }
       if constexpr (FULL) win.pr.decode(committed(tok0 + r) ? ~mask : 0u, [&](int bp, uint16_t v) { lds_write(to, bp, pitch, v); });
     }
     if (!whole) {  // in-flight vectors, eight values at a time
@@ -559,24 +580,24 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
     __syncthreads();
     float top = kLowest, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves / RT; ++w) top = fmaxf(top, red[0][w * RT + tile][mi]);
+    for (int w = 0; w < kWaves / RT; ++w) top = fmaxf(top, red[0][wave_of(tile, w)][mi]);
 #pragma unroll
-    for (int w = 0; w < kWaves / RT; ++w) sum += red[1][w * RT + tile][mi] * __builtin_amdgcn_exp2f(red[0][w * RT + tile][mi] - top);
+    for (int w = 0; w < kWaves / RT; ++w) sum += red[1][wave_of(tile, w)][mi] * __builtin_amdgcn_exp2f(red[0][wave_of(tile, w)][mi] - top);
     const float f = __builtin_amdgcn_exp2f(m - top);
     rows_f32x4* const stage = reinterpret_cast<rows_f32x4*>(tiles);
     if (!idle) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) stage[(wv * 8 + i) * kStageRun + lane] = eight[i] * f;
-      if (wv < RT && mq == 0 && tile * 16 + mi < left) ml[(size_t)(tile * 16 + mi) * splits] = make_float2(top, sum);
+      if (slab0 == 0 && mq == 0 && tile * 16 + mi < left) ml[(size_t)(tile * 16 + mi) * splits] = make_float2(top, sum);
     }
     __syncthreads();
     for (int e = tid; e < RT * 16 * 32; e += 64 * kWaves) {  // four channels c4 of row rr
       const int rr = e >> 5, c4 = e & 31;
       if (rr >= left) break;
-      const rows_f32x4* const from = stage + ((rr >> 4) * 8 + (c4 >> 3) * 2 + (c4 & 1)) * kStageRun + ((c4 >> 1) & 3) * 16 + (rr & 15);
-      rows_f32x4 sum4 = from[0];
+      const rows_f32x4* const from = stage + ((c4 >> 3) * 2 + (c4 & 1)) * kStageRun + ((c4 >> 1) & 3) * 16 + (rr & 15);
+      rows_f32x4 sum4 = from[wave_of(rr >> 4, 0) * 8 * kStageRun];
 #pragma unroll
-      for (int w = 1; w < kWaves / RT; ++w) sum4 += from[w * RT * 8 * kStageRun];
+      for (int w = 1; w < kWaves / RT; ++w) sum4 += from[wave_of(rr >> 4, w) * 8 * kStageRun];
       *reinterpret_cast<rows_f32x4*>(out + (size_t)rr * 128 + 4 * c4) = sum4;
     }
   }

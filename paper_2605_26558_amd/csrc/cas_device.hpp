@@ -318,6 +318,52 @@ struct KeptWindows {
       kept_tail(kept_tail, std::integral_constant<int, 8>{});
     }
   }
+
+  // The same for the shared-exponent form, without words of infinities and NaN (blocks whose exponent is 255 come out as the
+  // finite numbers of their fields): 11 vector operations a value where decode() has 16, as the magnitude is taken from the low byte of a
+  // word that holds the sign above it, and the upper half of the fp32 number is written as it is.
+  // write: (position, fp32 pattern whose lower half is 0)
+  template <class W>
+  __device__ __forceinline__ void decode_finite(uint32_t m, W&& write, int shared_exp) const {
+    static_assert(MX, "");
+    uint32_t ws[FW], wl[LW];
+#pragma unroll
+    for (int q = 0; q < FW; ++q) ws[q] = __builtin_amdgcn_alignbit(ds[q + 1], ds[q], shs);
+    if constexpr (FULL && T > 0) {
+#pragma unroll
+      for (int q = 0; q < T; ++q) wl[q] = __builtin_amdgcn_alignbit(dl[q + 1], dl[q], shl);
+    }
+    const int scale = max(shared_exp, 1) - 134;
+    auto kept = [&](auto E) {
+      constexpr int e = decltype(E)::value, bit = e * FW, w = bit >> 5, sh = bit & 31;
+      int pos = lowest_bit(m);
+      m = drop_lowest(m);
+      uint32_t v;  // the field, the fields behind it above
+      if constexpr (sh + FW <= 32) v = ws[w] >> sh;
+      else v = __builtin_amdgcn_alignbit(ws[w + 1], ws[w], sh);
+      if constexpr (T > 0) {
+        uint32_t low = 0;
+        if constexpr (FULL) low = field_at<T, e>(wl);
+        v = (v << T) | low;  // magnitude in the low byte, sign in bit 8
+      }
+      const float f = __builtin_amdgcn_ldexpf((float)(v & 0xFFu), scale);
+      write(pos, (__float_as_uint(f) & 0x7FFFFFFFu) | ((v << 23) & 0x80000000u));
+    };
+    auto kept_tail = [&](auto self, auto E) -> void {
+      constexpr int e = decltype(E)::value;
+      if constexpr (e < 32) {
+        if (__builtin_amdgcn_ballot_w64(m != 0u)) {
+          kept(std::integral_constant<int, e>{});
+          kept(std::integral_constant<int, e + 1>{});
+          self(self, std::integral_constant<int, e + 2>{});
+        }
+      }
+    };
+    if (__builtin_amdgcn_ballot_w64(m != 0u)) {
+      static_for<0, 8>(kept);
+      kept_tail(kept_tail, std::integral_constant<int, 8>{});
+    }
+  }
 };
 
 struct PrunedWindows {

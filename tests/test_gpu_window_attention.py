@@ -203,18 +203,21 @@ def test_what_a_column_does_not_see_does_not_reach_it(env, full, mode):
         _check(torch, out, ref, tol, (length, cols, new, first, window))
 
 
-def test_an_infinity_that_every_column_sees_stays_in_its_channel(env):
+@pytest.mark.parametrize("full,mode", [(True, 0), (False, 0), (True, 2), (False, 2)])
+def test_an_infinity_that_every_column_sees_stays_in_its_channel(env, full, mode):
+    """(Under a shared exponent the other values of its 32 channels lose their bits; they are what cas_kv_read gives.)"""
     torch, B, ctx = env
 
     def plant(s, k, v):
-        v[250, :, 7] = 0x7F80
-    kv = _cache(torch, B, ctx, 2, [300], plant=plant)
-    q, kn, vn = _inputs(torch, [3], [3], 4, 2)
-    out = B.cas_attention_window(ctx, kv, 0, [0], 4, 100, True, q, kn, vn)[0].double()
-    ref, tol = _of_sequence(torch, B, ctx, kv, 0, 0, True, q[0], kn[0], vn[0], 4, 100)
-    other = torch.arange(128, device="cuda") != 7
-    assert not bool(torch.isfinite(out[..., 7]).any())
-    assert bool(((out - ref).abs() <= tol)[..., other].all())
+        v[250, :, 7], v[260, 0, 40], v[2, 1, 90] = 0x7F80, 0xFF80, 0x7FC0
+    for mode_cols in (1, 3, 16):
+        kv = _cache(torch, B, ctx, 2, [300], mode=mode, plant=plant)
+        q, kn, vn = _inputs(torch, [mode_cols], [mode_cols], 12, 2)
+        out = B.cas_attention_window(ctx, kv, 0, [0], 4, 100, full, q, kn, vn)[0].double()
+        ref, tol = _of_sequence(torch, B, ctx, kv, 0, 0, full, q[0], kn[0], vn[0], 4, 100)
+        touched = ~torch.isfinite(ref)
+        assert torch.equal(touched, ~torch.isfinite(out)) and int(touched.sum()) == mode_cols * (12 + 6 + 6)
+        assert bool(((out - ref).abs() <= tol)[~touched].all())
 
 
 @pytest.mark.parametrize("full", [False, True])
