@@ -15,7 +15,7 @@ namespace cas {
 // One wave per vector with ballots (kv_append_few_kernel) is bound on a full chip by the scalar unit, which the SIMDs of a CU
 // share (298 scalar instructions per vector): 1021 tokens of 8 heads 11.6 us, so 7.7, of which the search takes 2 (5.6 with one step of the
 // fifteen, 6.7 with eight: some 19 vector instructions a step and four vectors); the rest is launch, memory and packing.
-constexpr int kAppendWaves = 4, kAppendRows = 4 * kAppendWaves;
+constexpr int kAppendWaves = 4, kAppendRows = 16;
 constexpr int kKeptPitch = 136;  // values of a list of kept ones: 16-byte steps, and vectors four banks apart
 
 // over the 16 lanes of a DPP row: the sum in every lane, and the sum of the lanes before
@@ -180,6 +180,222 @@ __device__ __forceinline__ void format_four(const KvGeom& g, uint32_t* spec_pool
     if (k < 2 && 16 * k < g.lw) flush(vl[k & 1], tv, g.lw, 64 * k + lane);
     if (16 * k < g.pw) flush(vp[k], tv + 64 * g.lw, g.pw, 64 * k + lane);
   }
+}
+
+// A wave formats sixteen 128-value vectors, the tokens of sixteen rows of a page from a multiple of sixteen on, so that whole runs
+// of lines are written: four lanes per vector, the 32 columns of a bitmap word per lane.
+// The K-th largest magnitude is found bit by bit on bit planes: the lane's 32 magnitudes are turned into 15 words with a bit for
+// each column (112 operations), and a step is then nine operations for all sixteen vectors: the columns that are as large as the
+// candidate's bits so far and have the next one are counted, and either they or the others stay.  Equals of the K-th are kept in the order of
+// the columns.  Kept values go to a list in LDS by rank, of which a lane packs 16 into the 16-T half words that their
+// fields fill; the pruned ones to their place in the row.
+
+// Of a wave.  First the lists of kept values, each to a whole group of 16 and eight more (so that vectors lie in different
+// banks), and behind them the pruned values, two to a word, row by row; then, once the lists are in registers, the fields and behind them the
+// dropped bits of all rows in the lists' place.
+struct RowsStage {
+  uint32_t words[kAppendRows * 78];  // (128 + 15 + 8 kept, none pruned) or less: 76 words a vector
+};
+
+// columns (2 i, 2 i + 1) of the first and the last 16 of a word, two registers each -> (2 i, 16 + 2 i) and (2 i + 1, 17 + 2 i)
+__device__ __forceinline__ uint32_t low_pair(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_pair(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); }
+
+// Two 16 x 16 matrices of bits, in the lower and the upper halves of 16 words, turned over
+__device__ __forceinline__ void bit_planes(uint32_t (&p)[16]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t a = p[i], b = p[i + 8];
+    p[i] = __builtin_amdgcn_perm(b, a, 0x06020400u);
+    p[i + 8] = __builtin_amdgcn_perm(b, a, 0x07030501u);
+  }
+  auto stage = [&](auto K, uint32_t m) {
+    constexpr int k = decltype(K)::value;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i & k) continue;
+      const uint32_t a = p[i], b = p[i + k];
+      p[i] = (a & m) | ((b << k) & ~m);
+      p[i + k] = ((a >> k) & m) | (b & ~m);
+    }
+  };
+  stage(std::integral_constant<int, 4>{}, 0x0F0F0F0Fu);
+  stage(std::integral_constant<int, 2>{}, 0x33333333u);
+  stage(std::integral_constant<int, 1>{}, 0x55555555u);
+}
+
+__device__ __forceinline__ int quad_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true);  // the lane beside, the other pair
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true);
+}
+__device__ __forceinline__ int quad_before(int v, int j) {  // of the lanes before j
+  const int b0 = quad_dpp<0x00>(v), b1 = quad_dpp<0x55>(v), b2 = quad_dpp<0xAA>(v);
+  return (j > 0 ? b0 : 0) + (j > 1 ? b1 : 0) + (j > 2 ? b2 : 0);
+}
+
+// The wave's vectors: columns 32 j + i and 32 j + 16 + i of vector lane / 4 in the halves of w[i], j = lane & 3.  They become rows row0 ..
+// row0 + 15 of the tile of (layer, page, K or V, head), those whose bit of `rows` is set.
+template <int T, bool MX>
+__device__ __forceinline__ void format_rows(const KvGeom& g, uint32_t* spec_pool, uint32_t* verif_pool, RowsStage& st, const uint32_t (&w)[16],
+                                            int lane, int layer, int page, int kv, int head, int row0, uint32_t rows) {
+  constexpr int FW = MX ? 9 - T : 16 - T;
+  const int r = lane >> 2, j = lane & 3;
+  uint32_t plane[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) plane[i] = w[i];
+  bit_planes(plane);
+  // columns as large as the K-th in the bits so far, larger ones, and how many of the former are still to be taken
+  uint32_t alive = 0xFFFFFFFFu, kept = 0;
+  int spare = g.K - 1;  // to be taken but for one: below 0 where that is none
+#pragma unroll
+  for (int bit = 14; bit >= 0; --bit) {
+    const uint32_t ones = alive & plane[bit];
+    const int after = spare - quad_sum(__popc(ones));
+    // stay: all bits where the larger ones are enough.  alive = stay ? ones : alive & ~ones; kept |= ones & ~stay.  Written out: the
+    // compiler takes five operations for the latter two
+    uint32_t stay;
+    asm("v_ashrrev_i32 %0, 31, %1" : "=v"(stay) : "v"(after));
+    asm("v_bitop3_b32 %0, %0, %1, %2 bitop3:0x98" : "+v"(alive) : "v"(ones), "v"(stay));
+    asm("v_bitop3_b32 %0, %0, %1, %2 bitop3:0xf4" : "+v"(kept) : "v"(ones), "v"(stay));
+    spare = (int)min((uint32_t)spare, (uint32_t)after);  // after, or spare where that is below 0
+  }
+  const int need = spare + 1, n_equal = __popc(alive), mine = need - quad_before(n_equal, j);  // of this lane's equals and those behind
+  kept |= mine >= n_equal ? alive : 0u;
+  if (__builtin_amdgcn_ballot_w64(mine > 0 && mine < n_equal)) {  // the line falls among the equals of a lane
+    int left = mine < n_equal ? mine : 0;
+    for (; __builtin_amdgcn_ballot_w64(left > 0); --left) {
+      const uint32_t low = left > 0 ? alive & (0u - alive) : 0u;
+      kept |= low;
+      alive ^= low;
+    }
+  }
+  const int before = quad_before(__popc(kept), j);
+
+  // shared-exponent form: the exponent of the word's largest magnitude, which is kept if any of the word is (0 for a word
+  // without kept values)
+  int E = 0;
+  if constexpr (MX) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+    E = kept ? eff_exponent(top) : 0;
+  }
+  const int pitch = ((g.K + 15) & ~15) + 8;  // of a list
+  uint16_t* const lists = reinterpret_cast<uint16_t*>(st.words);
+  uint32_t* const spec = st.words;
+  uint32_t* const lo = spec + kAppendRows * g.sw;
+  uint32_t* const pruned = st.words + kAppendRows / 2 * pitch;
+  uint16_t* kp = lists + r * pitch;
+  uint16_t* pr = reinterpret_cast<uint16_t*>(pruned + r * g.pw);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (g.K + 4 * j + e < pitch) kp[g.K + 4 * j + e] = 0;  // up to a whole group of 16
+  if (j == 0 && (g.K & 1)) pr[128 - g.K] = 0;  // the upper half of a row's last word belongs to no value
+  // Where the next kept and the next pruned value go, both less 2 bytes for each column before: a column is then at either plus 2 i, and moves
+  // the one that it does not take back by 2.  Five operations a value
+  typedef __attribute__((address_space(3))) uint16_t lds_u16;
+  auto address = [](uint16_t* p) { return (uint32_t)(uintptr_t)(lds_u16*)p; };
+  uint32_t to_kept = address(kp + before), to_pruned = address(pr + 32 * j - before);
+  const uint32_t others = ~kept;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const uint32_t v = i < 16 ? w[i & 15] & 0xFFFFu : w[i & 15] >> 16;
+    uint32_t is, is_not;  // 0 or all bits.  Written out: the compiler makes comparisons and counts of these, eight operations and more
+    asm("v_bfe_i32 %0, %1, %2, 1" : "=v"(is) : "v"(kept), "n"(i));
+    asm("v_bfe_i32 %0, %1, %2, 1" : "=v"(is_not) : "v"(others), "n"(i));
+    uint32_t u = v;
+    if constexpr (MX) {  // sign + magnitude: the significand shifted down to the block's exponent
+      const int sh = E - eff_exponent(v);
+      u = is ? ((v >> 15) << 8) | (sh < 8 ? significand(v) >> sh : 0u) : v;
+    }
+    *(lds_u16*)(uintptr_t)(((to_kept & is) | (to_pruned & ~is)) + 2 * i) = (uint16_t)u;
+    asm("v_lshl_add_u32 %0, %1, 1, %0" : "+v"(to_pruned) : "v"(is));
+    asm("v_lshl_add_u32 %0, %1, 1, %0" : "+v"(to_kept) : "v"(is_not));
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+
+  const int groups = (g.K + 15) >> 4;  // of 16 kept values of a vector: up to 128 of all, two to a lane
+  const uint32_t groups_inv = groups ? 65536u / (uint32_t)groups + 1u : 0u;
+  uint32_t v[2][8];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int t = lane + 64 * k, q = (int)((uint32_t)t * groups_inv >> 16), l = t - q * groups;
+    if (t >= kAppendRows * groups) continue;
+    const uint4* const src = reinterpret_cast<const uint4*>(lists + q * pitch) + 2 * l;
+    *reinterpret_cast<uint4*>(v[k]) = src[0];
+    *reinterpret_cast<uint4*>(v[k] + 4) = src[1];
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  // the upper half of a row's last word may belong to no value
+  if (j == 1 && g.sw > 0) spec[r * g.sw + g.sw - 1] = 0;
+  if (j == 2 && g.lw > 0) lo[r * g.lw + g.lw - 1] = 0;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {  // FW half words of fields, T of dropped bits
+    const int t = lane + 64 * k, q = (int)((uint32_t)t * groups_inv >> 16), l = t - q * groups;
+    if (t >= kAppendRows * groups) continue;
+    const bool inner = l + 1 < groups;  // the last group of a row ends where its words do
+    auto pack = [&](auto W, auto DOWN, uint32_t* out, int words) {
+      constexpr int width = decltype(W)::value, down = decltype(DOWN)::value, NW = (width + 1) / 2;
+      uint32_t o[NW];
+#pragma unroll
+      for (int i = 0; i < NW; ++i) o[i] = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t f = __builtin_amdgcn_ubfe(v[k][i >> 1], 16 * (i & 1) + down, width);
+        const int bit = i * width, at = bit >> 5, sh = bit & 31;
+        o[at] |= f << sh;
+        if (sh + width > 32) o[min(at + 1, NW - 1)] |= f >> (32 - sh);
+      }
+      if constexpr ((width & 1) == 0) {
+        const int last = words - (groups - 1) * NW;
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+          if (i < last || inner) out[l * NW + i] = o[i];
+      } else {
+        uint16_t* const h = reinterpret_cast<uint16_t*>(out) + l * width;
+        const int last = 2 * words - (groups - 1) * width;
+#pragma unroll
+        for (int i = 0; i < width; ++i)
+          if (i < last || inner) h[i] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
+      }
+    };
+    pack(std::integral_constant<int, FW>{}, std::integral_constant<int, T>{}, spec + q * g.sw, g.sw);
+    if constexpr (T > 0) pack(std::integral_constant<int, T>{}, std::integral_constant<int, 0>{}, lo + q * g.lw, g.lw);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+
+  if (page < 0 || page >= g.n_pages) return;  // a page table entry outside the pool: nothing is written
+  const size_t tile = (((size_t)layer * g.n_pages + page) * 2 + kv) * g.n_kv_heads + head;
+  uint32_t* ts = spec_pool + tile * g.tile_spec_words;
+  uint32_t* tv = verif_pool + tile * g.tile_verif_words;
+  const bool written = rows >> r & 1u;
+  if (written) ts[row0 * 4 + lane] = kept;
+  if constexpr (MX) {
+    const int e01 = quad_dpp<0x00>(E) | quad_dpp<0x55>(E) << 8, e23 = quad_dpp<0xAA>(E) | quad_dpp<0xFF>(E) << 8;
+    if (written && j == 0) ts[256 + row0 + r] = (uint32_t)(e01 | e23 << 16);
+  }
+  // rows of a stream lie side by side in the tile as they do here, sixteen of them from a multiple of 64 bytes on
+  auto flush = [&](const uint32_t* from, uint32_t* to, int words) {
+    if (rows == 0xFFFFu) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = lane + 64 * k;
+        if (64 * k < 4 * words && i < 4 * words) reinterpret_cast<uint4*>(to)[i] = reinterpret_cast<const uint4*>(from)[i];
+      }
+    } else {
+      const uint32_t inv = words ? 65536u / (uint32_t)words + 1u : 0u;  // rows of up to 64 words
+      for (int i = lane; i < kAppendRows * words; i += 64)
+        if (rows >> ((uint32_t)i * inv >> 16) & 1u) to[i] = from[i];
+    }
+  };
+  flush(spec, ts + g.spec_off + row0 * g.sw, g.sw);
+  flush(lo, tv + row0 * g.lw, g.lw);
+  flush(pruned, tv + 64 * g.lw + row0 * g.pw, g.pw);
 }
 
 // One wave per vector, for launches that leave most of the chip idle (see the launch): what counts there is how long one

@@ -25,10 +25,10 @@ struct RopeAppendArgs {
   const float* angles;    // cos, sin
   const int32_t* pos;     // NULL: the place in the cache
   int n_pos, half, inter, layer, n_tok, n_q;
-  int append_blocks, q_blocks;          // workgroups that append; workgroups of a token's queries
+  int units, append_blocks, q_blocks;   // waves and workgroups that append; workgroups of a token's queries
   RopeAppendPart part[3];               // q, k, v
   int tok0[kRopeAppendSeqs];            // tokens of the sequences before; the largest number behind the last
-  int block0[kRopeAppendSeqs];          // groups of sixteen rows of the sequences before; as above
+  int group0[kRopeAppendSeqs];          // groups of sixteen rows of the sequences before; as above
   int seq[kRopeAppendSeqs], len[kRopeAppendSeqs], n[kRopeAppendSeqs];
 };
 
@@ -98,142 +98,211 @@ __global__ __launch_bounds__(64 * kAppendWaves) void rope_append_few_kernel(Rope
   format_one(g, a.spec_pool, a.verif_pool, stages[wv], v0, v1, lane, a.layer, page, which - 1, head, place & 63);
 }
 
-// Eight channels 8 l .. 8 l + 7 of a vector, two to a word
-__device__ __forceinline__ void load_eight(uint64_t row, int l, bool fp32, uint32_t (&w)[4]) {
-  if (fp32) {
-    float f[8];
-    __builtin_memcpy(f, reinterpret_cast<const void*>(row + 32u * (uint32_t)l), 32);
+// N channels of a vector from c on, as they lie in memory: floats, or bf16 in half as many words; and rounded, two to a word
+template <int N>
+__device__ __forceinline__ void request(uint64_t row, int c, bool fp32, uint32_t (&w)[N]) {
+  if (fp32) __builtin_memcpy(w, reinterpret_cast<const void*>(row + 4u * (uint32_t)c), 4 * N);
+  else __builtin_memcpy(w, reinterpret_cast<const void*>(row + 2u * (uint32_t)c), 2 * N);
+}
+template <int N>
+__device__ __forceinline__ void take(const uint32_t (&raw)[N], bool fp32, uint32_t (&w)[N / 2]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)f32_to_bf16(f[2 * i]) | (uint32_t)f32_to_bf16(f[2 * i + 1]) << 16;
-  } else {
-    __builtin_memcpy(w, reinterpret_cast<const void*>(row + 16u * (uint32_t)l), 16);
-  }
+  for (int i = 0; i < N / 2; ++i)
+    w[i] = fp32 ? (uint32_t)f32_to_bf16(__uint_as_float(raw[2 * i])) | (uint32_t)f32_to_bf16(__uint_as_float(raw[2 * i + 1])) << 16 : raw[i];
 }
 __device__ __forceinline__ float low_value(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_value(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// cos and sin (with the sign that its channel takes it with) of a lane's eight channels at one position
-struct EightAngles {
-  float c[8], s[8];
-  __device__ __forceinline__ void load(const RopeAppendArgs& a, int p, int l) {
-    const float2* cs = reinterpret_cast<const float2*>(a.angles) + (size_t)p * a.half;
-    if (!a.inter && (a.half & 7) == 0) {  // eight channels of one half
-      const Pairing at(8 * l, a.half, false);
-      float f[16];
-      __builtin_memcpy(f, cs + at.pair, 64);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        c[i] = f[2 * i];
-        s[i] = at.first ? -f[2 * i + 1] : f[2 * i + 1];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const Pairing at(8 * l + i, a.half, a.inter);
-        const float2 v = cs[at.pair];
-        c[i] = v.x;
-        s[i] = at.first ? -v.y : v.y;
-      }
-    }
-  }
-};
-// Turns the lane's eight channels; row: 128 values of LDS of the vector's 16 lanes.  All 64 lanes of the wave call it together.
-__device__ __forceinline__ void turn_eight(const RopeAppendArgs& a, const EightAngles& cs, int l, uint16_t* row, uint32_t (&w)[4]) {
-  float other[8];
-  if (a.inter) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      other[2 * i] = high_value(w[i]);
-      other[2 * i + 1] = low_value(w[i]);
-    }
-  } else {
-    *reinterpret_cast<uint4*>(row + 8 * l) = make_uint4(w[0], w[1], w[2], w[3]);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if ((a.half & 7) == 0) {
-      const uint4 o = *reinterpret_cast<const uint4*>(row + Pairing(8 * l, a.half, false).other);
-      const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        other[2 * i] = low_value(ow[i]);
-        other[2 * i + 1] = high_value(ow[i]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) other[i] = bf16_to_f32(row[Pairing(8 * l + i, a.half, false).other]);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = 8 * l + 2 * i;
-    const float y0 = low_value(w[i]) * cs.c[2 * i] + other[2 * i] * cs.s[2 * i];
-    const float y1 = high_value(w[i]) * cs.c[2 * i + 1] + other[2 * i + 1] * cs.s[2 * i + 1];
-    if (c < 2 * a.half) w[i] = (uint32_t)f32_to_bf16(y0) | (uint32_t)f32_to_bf16(y1) << 16;  // an even number of channels turns
+// How the partners of eight channels from a multiple of eight on are reached: half a vector away, in the same words, eight that follow one
+// another, or one by one
+enum Partners { kHalfAway, kNeighbours, kEights, kSingles };
+__device__ __forceinline__ Partners partners_of(const RopeAppendArgs& a) {
+  return a.inter ? kNeighbours : a.half == 64 ? kHalfAway : (a.half & 7) == 0 ? kEights : kSingles;
+}
+// Calls f with the kind as a constant: as branches inside, the kinds' registers add up (64 to 188 of them spilled)
+template <class F>
+__device__ __forceinline__ void with_partners(const RopeAppendArgs& a, F&& f) {
+  switch (partners_of(a)) {
+    case kHalfAway: f(std::integral_constant<int, kHalfAway>{}); break;
+    case kNeighbours: f(std::integral_constant<int, kNeighbours>{}); break;
+    case kEights: f(std::integral_constant<int, kEights>{}); break;
+    default: f(std::integral_constant<int, kSingles>{});
   }
 }
 
-// A wave for four vectors, 16 lanes each: the tokens of four rows of a page (k, v), or four heads of a token (q).
+// cos and sin of channels c0 .. c0 + 7 at one position
+template <int HOW>
+struct EightAngles {
+  float c[8], s[8];
+  __device__ __forceinline__ void load(const RopeAppendArgs& a, int p, int c0) {
+    const float2* cs = reinterpret_cast<const float2*>(a.angles) + (size_t)p * a.half;
+    if constexpr (HOW == kHalfAway || HOW == kEights) {  // eight channels of one half
+      float f[16];
+      __builtin_memcpy(f, cs + Pairing(c0, a.half, false).pair, 64);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        c[i] = f[2 * i];
+        s[i] = f[2 * i + 1];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (HOW == kNeighbours && (i & 1)) {
+          c[i] = c[i - 1];
+          s[i] = s[i - 1];
+        } else {
+          const float2 v = cs[Pairing(c0 + i, a.half, HOW == kNeighbours).pair];
+          c[i] = v.x;
+          s[i] = v.y;
+        }
+      }
+    }
+  }
+  // w: channels c0 .. c0 + 7, two to a word; o: their partners
+  __device__ __forceinline__ void turn(const RopeAppendArgs& a, int c0, const uint32_t (&o)[4], uint32_t (&w)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const Pairing p0(c0 + 2 * i, a.half, HOW == kNeighbours), p1(c0 + 2 * i + 1, a.half, HOW == kNeighbours);
+      const uint32_t x = o[i] ^ ((p0.first ? 0x8000u : 0u) | (p1.first ? 0x80000000u : 0u));  // y_a = x_a cos + (-x_b) sin
+      const float y0 = low_value(w[i]) * c[2 * i] + low_value(x) * s[2 * i];
+      const float y1 = high_value(w[i]) * c[2 * i + 1] + high_value(x) * s[2 * i + 1];
+      const uint32_t y = (uint32_t)f32_to_bf16(y0) | (uint32_t)f32_to_bf16(y1) << 16;
+      w[i] = HOW == kHalfAway || p0.turns ? y : w[i];  // an even number of channels turns
+    }
+  }
+};
+// The partners of channels c0 .. c0 + 7: of the words themselves, of a lane DPP control AWAY, or out of the vector's 128 values in LDS
+template <int HOW, int AWAY>
+__device__ __forceinline__ void partners(const RopeAppendArgs& a, int c0, const uint16_t* row, const uint32_t (&w)[4], uint32_t (&o)[4]) {
+  if constexpr (HOW == kEights) {
+    const uint4 x = *reinterpret_cast<const uint4*>(row + Pairing(c0, a.half, false).other);
+    o[0] = x.x; o[1] = x.y; o[2] = x.z; o[3] = x.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (HOW == kHalfAway) o[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[i], AWAY, 0xf, 0xf, true);
+      else if constexpr (HOW == kNeighbours) o[i] = __builtin_amdgcn_alignbit(w[i], w[i], 16);
+      else o[i] = (uint32_t)row[Pairing(c0 + 2 * i, a.half, false).other] | (uint32_t)row[Pairing(c0 + 2 * i + 1, a.half, false).other] << 16;
+    }
+  }
+}
+
+// Sixteen vectors to a wave: the tokens of sixteen rows of a page (k, v; four lanes each), or four heads of a token at a time (q; 16
+// lanes each).  A workgroup's waves do not wait for each other.
 template <int T, bool MX>
-__global__ __launch_bounds__(64 * kAppendWaves) void rope_append_kernel(RopeAppendArgs a) {
-  __shared__ __attribute__((aligned(16))) AppendStage stages[kAppendWaves];
+__global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeAppendArgs a) {
+  __shared__ __attribute__((aligned(16))) RowsStage stages[kAppendWaves];
   const KvGeom& g = a.g;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q = lane >> 4, l = lane & 15;
-  AppendStage& st = stages[wv];
-  const LaneTable t_tok0(a.tok0), t_seq(a.seq), t_len(a.len), t_n(a.n), t_block0(a.block0);
-  int block = blockIdx.x;
-  EightAngles cs;
-  uint32_t w[4];
-  if (block >= a.append_blocks) {  // the queries of a token
-    block -= a.append_blocks;
+  RowsStage& st = stages[wv];
+  // vectors of 128 values that lanes exchange, in different banks
+  auto vector_row = [&](int i) { return reinterpret_cast<uint16_t*>(st.words) + 136 * i; };
+  const LaneTable t_tok0(a.tok0), t_seq(a.seq), t_len(a.len), t_n(a.n), t_group0(a.group0);
+  auto share = [] {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  if ((int)blockIdx.x >= a.append_blocks) {  // the queries of a token
+    const int block = (int)blockIdx.x - a.append_blocks, q = lane >> 4, l = lane & 15;
     const int tok = block / a.q_blocks, first = (block - tok * a.q_blocks) * 4 * kAppendWaves + 4 * wv;
     const int s = t_tok0.which(tok), p = a.pos ? a.pos[tok] : t_len[s] + tok - t_tok0[s];
     if (p < 0 || p >= a.n_pos) return;
     const RopeAppendPart part = a.part[0];
-    if (part.turn) cs.load(a, p, l);
-    for (int h0 = first; h0 < a.n_q; h0 += a.q_blocks * 4 * kAppendWaves) {  // uniform in the wave
-      const int head = min(h0 + q, a.n_q - 1);
-      load_eight(part.x + (uint64_t)(tok * part.ldx) + (uint32_t)head * (part.fp32 ? 512u : 256u), l, part.fp32, w);
-      if (part.turn) turn_eight(a, cs, l, st.kept[q], w);
-      if (h0 + q < a.n_q)
-        __builtin_memcpy(reinterpret_cast<uint16_t*>(part.y + (uint64_t)(tok * part.ldy)) + head * 128 + 8 * l, w, 16);
+    auto heads = [&](auto&& turn) {
+      for (int h0 = first; h0 < a.n_q; h0 += a.q_blocks * 4 * kAppendWaves) {  // uniform in the wave
+        const int head = min(h0 + q, a.n_q - 1);
+        uint32_t raw[8], w[4];
+        request(part.x + (uint64_t)(tok * part.ldx) + (uint32_t)head * (part.fp32 ? 512u : 256u), 8 * l, part.fp32, raw);
+        take(raw, part.fp32, w);
+        turn(w);
+        if (h0 + q < a.n_q)
+          __builtin_memcpy(reinterpret_cast<uint16_t*>(part.y + (uint64_t)(tok * part.ldy)) + head * 128 + 8 * l, w, 16);
+      }
+    };
+    if (!part.turn) {
+      heads([](uint32_t (&)[4]) {});
+      return;
     }
+    with_partners(a, [&](auto H) {
+      constexpr int how = decltype(H)::value;
+      EightAngles<how> cs;
+      cs.load(a, p, 8 * l);
+      heads([&](uint32_t (&w)[4]) {
+        uint32_t o[4];
+        if constexpr (how >= kEights) {
+          *reinterpret_cast<uint4*>(vector_row(q) + 8 * l) = make_uint4(w[0], w[1], w[2], w[3]);
+          share();
+        }
+        partners<how, 0x128>(a, 8 * l, vector_row(q), w, o);  // row_ror:8
+        if constexpr (how >= kEights) share();
+        cs.turn(a, 8 * l, o, w);
+      });
+    });
     return;
   }
-  const int head = block % g.n_kv_heads, kv = block / g.n_kv_heads & 1;
-  block = block / g.n_kv_heads >> 1;
-  const int s = t_block0.which(block), pos0 = t_len[s];
-  const int posw = (pos0 & -kAppendRows) + (block - t_block0[s]) * kAppendRows + 4 * wv;  // place of the wave's first row
-  const int ra = max(pos0 - posw, 0), rb = min(pos0 + t_n[s] - posw, 4);                  // the wave's rows ra .. rb - 1 are new
-  if (ra >= rb) return;  // the waves do not wait for each other
-  const int page = a.table[(size_t)t_seq[s] * g.max_pages_per_seq + posw / 64];
+  const int unit = (int)blockIdx.x * kAppendWaves + wv;
+  if (unit >= a.units) return;
+  const int rest = unit / g.n_kv_heads, head = unit - rest * g.n_kv_heads, kv = rest & 1, group = rest >> 1;
+  const int r = lane >> 2, c0 = 32 * (lane & 3);
+  const int s = t_group0.which(group), pos0 = t_len[s];
+  const int posw = (pos0 & -kAppendRows) + (group - t_group0[s]) * kAppendRows;     // place of the wave's first row
+  const int ra = max(pos0 - posw, 0), rb = min(pos0 + t_n[s] - posw, kAppendRows);  // the wave's rows ra .. rb - 1 are new
   const RopeAppendPart part = a.part[1 + kv];
-  const int place = posw + min(max(q, ra), rb - 1), tok = t_tok0[s] + place - pos0;  // rows that are not new repeat one that is
+  const int place = posw + min(max(r, ra), rb - 1), tok = t_tok0[s] + place - pos0;  // rows that are not new repeat one that is
+  uint32_t raw[32];
+  request(part.x + (uint64_t)(tok * part.ldx) + (uint32_t)head * (part.fp32 ? 512u : 256u), c0, part.fp32, raw);
+  const int page = a.table[(size_t)t_seq[s] * g.max_pages_per_seq + posw / 64];
   const int p = a.pos ? a.pos[tok] : place;
-  const bool there = p >= 0 && p < a.n_pos;
-  const uint64_t rows = __builtin_amdgcn_ballot_w64(there && q >= ra && q < rb);  // bit 16 r: row r is written
-  if (rows == 0) return;
-  load_eight(part.x + (uint64_t)(tok * part.ldx) + (uint32_t)head * (part.fp32 ? 512u : 256u), l, part.fp32, w);
-  if (part.turn) {
-    cs.load(a, there ? p : 0, l);
-    turn_eight(a, cs, l, st.kept[q], w);
+  const uint64_t lanes = __builtin_amdgcn_ballot_w64(p >= 0 && p < a.n_pos && r >= ra && r < rb);
+  if (lanes == 0) return;
+  uint32_t rows = 0;  // those that are written
+#pragma unroll
+  for (int i = 0; i < kAppendRows; ++i) rows |= (uint32_t)(lanes >> (4 * i) & 1) << i;
+  uint32_t x[4][4];  // eight channels each
+  {
+    uint32_t y[16];
+    take(raw, part.fp32, y);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i >> 2][i & 3] = y[i];
   }
-  if (part.y && (rows >> (16 * q) & 1))
-    __builtin_memcpy(reinterpret_cast<uint16_t*>(part.y + (uint64_t)(tok * part.ldy)) + head * 128 + 8 * l, w, 16);
-  const bool gaps = __popcll(rows) != 16 * (rb - ra);  // some of the rows are padding
-  format_four<T, MX>(g, a.spec_pool, a.verif_pool, st, w, lane, a.layer, page, kv, head, posw & 63, [&](int i, int words) {
-    bool in = i >= ra * words && i < rb * words;
-    if (gaps) in = in && (rows >> (16 * ((i >= words) + (i >= 2 * words) + (i >= 3 * words))) & 1);
-    return in;
-  });
+  if (part.turn) {
+    with_partners(a, [&](auto H) {
+      constexpr int how = decltype(H)::value;
+      uint16_t* const row = vector_row(r);
+      if constexpr (how >= kEights) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(row + c0 + 8 * i) = make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]);
+        share();
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        EightAngles<how> cs;
+        uint32_t o[4];
+        cs.load(a, min(max(p, 0), a.n_pos - 1), c0 + 8 * i);
+        partners<how, 0x4E>(a, c0 + 8 * i, row, x[i], o);  // the other pair of the four lanes
+        cs.turn(a, c0 + 8 * i, o, x[i]);
+        asm volatile("" ::: "memory");  // the angles of all four eights at once do not fit the registers
+      }
+      if constexpr (how >= kEights) share();
+    });
+  }
+  if (part.y && (rows >> r & 1))
+    __builtin_memcpy(reinterpret_cast<uint16_t*>(part.y + (uint64_t)(tok * part.ldy)) + head * 128 + c0, x, 64);
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    w[2 * i] = low_pair(x[i >> 2][i & 3], x[2 + (i >> 2)][i & 3]);
+    w[2 * i + 1] = high_pair(x[i >> 2][i & 3], x[2 + (i >> 2)][i & 3]);
+  }
+  format_rows<T, MX>(g, a.spec_pool, a.verif_pool, st, w, lane, a.layer, page, kv, head, posw & 63, rows);
 }
 
 static int launch_rope_append(cas_ctx* ctx, RopeAppendArgs& a, int n_seqs) {
   const KvGeom& g = a.g;
-  // as launch_kv_append_layers chooses
-  if ((int64_t)a.n_tok * g.n_kv_heads * 2 <= (int64_t)(g.mx ? 10 : 12) * ctx->num_cu) {
+  // Up to 24 vectors of K and V per CU (30 over shared exponents) a wave takes each, above sixteen.  us, one / sixteen a wave, tokens of 8
+  // heads bf16 without queries: 128 4.0 / 7.6, 384 6.6 / 7.8, 512 7.8 / 7.9, 1021 13.1 / 9.2; fp32 with 32 query heads: 256 7.8 / 9.2, 384 10.0 /
+  // 9.7, 512 12.1 / 10.1, 1021 23.6 / 12.5; over shared exponents 384 7.0 / 9.5 and 10.4 / 11.3, 512 8.3 / 9.6 and 12.3 / 11.8
+  if ((int64_t)a.n_tok * g.n_kv_heads * 2 <= (int64_t)(g.mx ? 30 : 24) * ctx->num_cu) {
     const dim3 grid((a.n_tok + kAppendWaves - 1) / kAppendWaves, a.n_q + 2 * g.n_kv_heads);
     hipLaunchKernelGGL(rope_append_few_kernel, grid, dim3(64 * kAppendWaves), 0, ctx->stream, a);
     CAS_HIP(ctx, hipGetLastError());
@@ -241,14 +310,17 @@ static int launch_rope_append(cas_ctx* ctx, RopeAppendArgs& a, int n_seqs) {
   }
   int64_t groups = 0;
   for (int i = 0; i < n_seqs; ++i) {
-    a.block0[i] = (int)groups;
+    a.group0[i] = (int)groups;
     if (a.n[i] > 0) groups += (a.len[i] + a.n[i] - 1) / kAppendRows - a.len[i] / kAppendRows + 1;
   }
-  for (int i = n_seqs; i < kRopeAppendSeqs; ++i) a.block0[i] = 0x7FFFFFFF;
+  for (int i = n_seqs; i < kRopeAppendSeqs; ++i) a.group0[i] = 0x7FFFFFFF;
   a.q_blocks = a.n_q > 0 ? std::max(1, std::min((a.n_q + 4 * kAppendWaves - 1) / (4 * kAppendWaves), 1024 / a.n_tok)) : 0;
-  const int64_t grid = groups * g.n_kv_heads * 2 + (int64_t)a.n_tok * a.q_blocks;
+  const int64_t units = groups * g.n_kv_heads * 2;
+  if (units > 0x7FFFFFFF) return CAS_ENOTSUP;
+  a.units = (int)units;
+  a.append_blocks = (int)((units + kAppendWaves - 1) / kAppendWaves);
+  const int64_t grid = a.append_blocks + (int64_t)a.n_tok * a.q_blocks;
   if (grid > 0xFFFFFF) return CAS_ENOTSUP;  // a launch has fewer than 2^32 threads
-  a.append_blocks = (int)(groups * g.n_kv_heads * 2);
 #define CAS_LAUNCH(TV)                                                                                                        \
   case TV:                                                                                                                    \
     hipLaunchKernelGGL(g.mx ? (rope_append_kernel<TV, true>) : (rope_append_kernel<TV, false>), dim3((unsigned)grid),         \

@@ -35,6 +35,33 @@ __global__ __launch_bounds__(64 * kAppendWaves) void kv_append_kernel(KvGeom g, 
                      [&](int i, int words) { return i >= ra * words && i < rb * words; });
 }
 
+// Sixteen vectors to a wave, for many
+template <int T, bool MX>
+__global__ __launch_bounds__(64 * kAppendWaves) void kv_append_rows_kernel(KvGeom g, uint32_t* spec_pool, uint32_t* verif_pool,
+                                                                           const int32_t* __restrict__ page_row, int layer0,
+                                                                           int pos0, int n_tok, const uint16_t* __restrict__ Kn,
+                                                                           const uint16_t* __restrict__ Vn, size_t layer_stride) {
+  __shared__ __attribute__((aligned(16))) RowsStage stages[kAppendWaves];
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // grid.z = 2 * (layers of this launch), as above
+  const int head = blockIdx.y, kv = blockIdx.z & 1, layer = layer0 + (blockIdx.z >> 1);
+  const int posw = (pos0 & -kAppendRows) + (blockIdx.x * kAppendWaves + wv) * kAppendRows;  // position of the wave's first row
+  const int ra = max(pos0 - posw, 0), rb = min(pos0 + n_tok - posw, kAppendRows);           // the wave's rows ra .. rb - 1 are new
+  if (ra >= rb) return;  // the waves do not wait for each other
+  const int page = page_row[posw / 64];
+  const int tok = posw + min(max(lane >> 2, ra), rb - 1) - pos0;  // rows that are not new repeat one that is
+  const uint16_t* src = (kv ? Vn : Kn) + (size_t)(blockIdx.z >> 1) * layer_stride +
+                        ((size_t)tok * g.n_kv_heads + head) * 128 + 32 * (lane & 3);
+  uint32_t x[16], w[16];
+  __builtin_memcpy(x, src, 64);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    w[2 * i] = low_pair(x[i], x[8 + i]);
+    w[2 * i + 1] = high_pair(x[i], x[8 + i]);
+  }
+  format_rows<T, MX>(g, spec_pool, verif_pool, stages[wv], w, lane, layer, page, kv, head, posw & 63, (0xFFFFu << ra) & (0xFFFFu >> (kAppendRows - rb)));
+}
+
 __global__ __launch_bounds__(64 * kAppendWaves) void kv_append_few_kernel(KvGeom g, uint32_t* spec_pool, uint32_t* verif_pool,
                                                                           const int32_t* __restrict__ page_row, int layer0,
                                                                           int pos0, int n_tok, const uint16_t* __restrict__ Kn,
@@ -92,12 +119,16 @@ int launch_kv_append_layers(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, 
     CAS_HIP(ctx, hipGetLastError());
     return CAS_OK;
   }
-  const int blocks = (pos0 + n_tok - 1) / kAppendRows - pos0 / kAppendRows + 1;
-  const dim3 grid(blocks, g.n_kv_heads, 2 * n_layers);
+  const int groups = (pos0 + n_tok - 1) / kAppendRows - pos0 / kAppendRows + 1;
+  // Of sixteen from 48 vectors per CU on (72 over shared exponents).  us, four / sixteen: 512 tokens of 8 heads 5.17 / 5.45, 768 6.1 / 5.6, 1021 7.1 /
+  // 6.6, 4096 18.6 / 11.4; over shared exponents 1021 7.8 / 8.0, 2048 12.3 / 9.3, 4096 21.3 / 14.7
+  const bool many = (int64_t)n_tok * g.n_kv_heads * 2 * n_layers >= (int64_t)(g.mx ? 72 : 48) * ctx->num_cu;
+  const dim3 grid(many ? (groups + kAppendWaves - 1) / kAppendWaves : groups, g.n_kv_heads, 2 * n_layers);
 #define CAS_LAUNCH(TV)                                                                                              \
   case TV:                                                                                                          \
-    hipLaunchKernelGGL(g.mx ? (kv_append_kernel<TV, true>) : (kv_append_kernel<TV, false>), grid,                   \
-                       dim3(64 * kAppendWaves), 0, ctx->stream, g, (uint32_t*)kv->d_spec, (uint32_t*)kv->d_verif,   \
+    hipLaunchKernelGGL(many ? (g.mx ? (kv_append_rows_kernel<TV, true>) : (kv_append_rows_kernel<TV, false>))       \
+                            : (g.mx ? (kv_append_kernel<TV, true>) : (kv_append_kernel<TV, false>)),                \
+                       grid, dim3(64 * kAppendWaves), 0, ctx->stream, g, (uint32_t*)kv->d_spec, (uint32_t*)kv->d_verif, \
                        kv->d_page_table + (size_t)seq * g.max_pages_per_seq, layer0, pos0, n_tok, K, V, layer_stride); \
     break;
   switch (g.t) {
