@@ -727,32 +727,41 @@ def cas_kv_append_rope(ctx: Context, kv: KVCache, layer, seqs, n_toks, table, k,
     k_out, v_out: tensors for the turned vectors, which are encoded into the cache in any case.  Returns the turned queries (None
     without q), as cas_rope does."""
     torch = ctx._torch
+    f32 = torch.float32
     n_pos, half, two = table.shape
-    assert table.is_cuda and table.is_contiguous() and table.dtype == torch.float32 and two == 2
-    n_tok, n, bits = sum(n_toks), len(seqs), _bf16_bits(torch)
-    assert n == len(n_toks) and (pos is None or (pos.is_cuda and pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == n_tok))
+    assert table.is_cuda and table.is_contiguous() and table.dtype == f32 and two == 2
+    n_tok, n, bits, kv_heads = sum(n_toks), len(seqs), _bf16_bits(torch), kv.desc.n_kv_heads
+    assert n == len(n_toks)
+    if pos is not None:
+        assert pos.is_cuda and pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == n_tok
+        pos = pos.data_ptr()
     if q is not None and q_out is None:
-        q_out = torch.empty_like(q, dtype=torch.int16 if q.dtype == torch.float32 else None, memory_format=torch.contiguous_format)
+        q_out = torch.empty_like(q, dtype=torch.int16 if q.dtype == f32 else None, memory_format=torch.contiguous_format)
     parts = []
-    for x, y, t in ((q, q_out, turn[0]), (k, k_out, turn[1]), (v, v_out, turn[2])):
+    for x, y, t, heads in ((q, q_out, turn[0], None), (k, k_out, turn[1], kv_heads), (v, v_out, turn[2], kv_heads)):
         if x is None:
             parts.append(None)
             continue
-        shape, (ldx, head, one), fp32, ldy = x.shape, x.stride(), x.dtype == torch.float32, 0
-        heads = shape[1]
-        assert x.is_cuda and shape[0] == n_tok and shape[2] == 128 and one == 1 and (head == 128 or heads <= 1) and (fp32 or x.dtype in bits)
-        assert x is q or heads == kv.desc.n_kv_heads
+        shape, (ldx, head, one), dtype = x.shape, x.stride(), x.dtype
+        tokens, wide, dim = shape
+        fp32 = dtype == f32
+        assert tokens == n_tok and dim == 128 and one == 1 and (head == 128 or wide <= 1) and x.is_cuda and (fp32 or dtype in bits)
+        assert heads is None or wide == heads
+        to = ldy = 0
         if y is not None:
-            ldy, yhead, yone = y.stride()
-            assert y.is_cuda and y.shape == shape and y.dtype in bits and yone == 1 and (yhead == 128 or heads <= 1)
+            ldy, head, one = y.stride()
+            assert y.shape == shape and one == 1 and (head == 128 or wide <= 1) and y.is_cuda and y.dtype in bits
+            to = y.data_ptr()
         if n_tok <= 1:  # no second token that a distance would lead to
-            ldx, ldy = max(ldx, heads * 128), max(ldy, heads * 128)
-        # the words of a cas_rope_part
-        parts.append((C.c_int64 * 6)(x.data_ptr(), 0 if y is None else y.data_ptr(), ldx, ldy, heads | fp32 << 32, int(bool(t))))
+            ldx, ldy = max(ldx, wide * 128), max(ldy, wide * 128)
+        parts.append(_PART(x.data_ptr(), to, ldx, ldy, wide | fp32 << 32, 1 if t else 0))
     i32 = C.c_int32 * n
-    ctx._check(_lib().cas_kv_append_rope(ctx.h, kv.h, layer, n, i32(*seqs), i32(*n_toks), table.data_ptr(), n_pos, 2 * half, layout,
-                                         None if pos is None else pos.data_ptr(), *parts), "cas_kv_append_rope")
+    ctx._check(_lib().cas_kv_append_rope(ctx.h, kv.h, layer, n, i32(*seqs), i32(*n_toks), table.data_ptr(), n_pos, 2 * half, layout, pos, *parts),
+               "cas_kv_append_rope")
     return q_out
+
+
+_PART = C.c_int64 * 6  # the words of a cas_rope_part
 
 
 def _i32(v):
@@ -892,27 +901,41 @@ def cas_accept_tokens(ctx: Context, target, draft, tokens, ks, r, temperature=No
     probabilities of the drafted tokens, float32 (p, q)."""
     torch = ctx._torch
     S, n, most = len(ks), sum(ks), max(ks, default=0)
+    i32, f32 = torch.int32, torch.float32
     (rows, vocab), (ldt, one) = target.shape, target.stride()
-    assert rows == n + S and target.is_cuda and target.dtype == torch.float32 and (one == 1 or vocab == 1)
-    ldt, ldd, dev = vocab if rows <= 1 else ldt, 0, target.device  # a single row has no next one
+    assert rows == n + S and target.is_cuda and target.dtype == f32 and (one == 1 or vocab == 1)
+    assert r.is_cuda and r.is_contiguous() and r.dtype == torch.float64 and r.numel() == n + S
+    near = drafted = heat = ldd = 0
+    if rows <= 1:  # a single row has no next one
+        ldt = vocab
     if draft is not None:
         (rows, v), (ldd, one) = draft.shape, draft.stride()
-        assert rows == n and v == vocab and draft.is_cuda and draft.dtype == torch.float32 and (one == 1 or vocab == 1)
-        ldd = vocab if rows <= 1 else ldd
-    for t, size, dtype in ((tokens, n, torch.int32), (r, n + S, torch.float64), (temperature, S, torch.float32)):
-        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.numel() == size)
-    assert r is not None and (tokens is not None or n == 0)
-    for t, shape in ((n_accepted, (S,)), (out, (S, most + 1 if out is None else max(out.shape[1], most + 1)))):
-        assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == torch.int32 and t.shape == shape)
+        assert rows == n and v == vocab and draft.is_cuda and draft.dtype == f32 and (one == 1 or vocab == 1)
+        ldd, near = vocab if rows <= 1 else ldd, draft.data_ptr()
+    if tokens is not None:
+        assert tokens.is_cuda and tokens.is_contiguous() and tokens.dtype == i32 and tokens.numel() == n
+        drafted = tokens.data_ptr()
+    assert n == 0 or drafted
+    if temperature is not None:
+        assert temperature.is_cuda and temperature.is_contiguous() and temperature.dtype == f32 and temperature.numel() == S
+        heat = temperature.data_ptr()
     if n_accepted is None:
-        n_accepted = torch.empty(S, dtype=torch.int32, device=dev)
+        n_accepted = target.new_empty(S, dtype=i32)
+    else:
+        assert n_accepted.is_cuda and n_accepted.is_contiguous() and n_accepted.dtype == i32 and n_accepted.shape == (S,)
     if out is None:
-        out = torch.empty((S, most + 1), dtype=torch.int32, device=dev)
-    pq = torch.empty((2, n), dtype=torch.float32, device=dev) if probs else None
-    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    ctx._check(_lib().cas_accept_tokens(ctx.h, S, (C.c_int32 * S)(*ks), vocab, target.data_ptr(), ldt, at(draft), ldd, at(tokens), at(temperature),
-                                        r.data_ptr(), n_accepted.data_ptr(), out.data_ptr(), out.shape[1], at(pq), pq.data_ptr() + 4 * n if probs else None),
-               "cas_accept_tokens")
+        wide = most + 1
+        out = target.new_empty((S, wide), dtype=i32)
+    else:
+        wide = max(out.shape[1], most + 1)
+        assert out.is_cuda and out.is_contiguous() and out.dtype == i32 and out.shape == (S, wide)
+    p = q = 0
+    if probs:
+        pq = target.new_empty((2, n))
+        p = pq.data_ptr()
+        q = p + 4 * n
+    ctx._check(_lib().cas_accept_tokens(ctx.h, S, (C.c_int32 * S)(*ks), vocab, target.data_ptr(), ldt, near, ldd, drafted, heat, r.data_ptr(),
+                                        n_accepted.data_ptr(), out.data_ptr(), wide, p, q), "cas_accept_tokens")
     return (n_accepted, out, *pq.unbind(0)) if probs else (n_accepted, out)
 
 
