@@ -3,6 +3,7 @@ marshalling only.  torch tensors provide device memory and the stream; every ste
 path runs in the HIP kernels.  Loading fails loudly if the library has not been built."""
 from __future__ import annotations
 
+import array
 import ctypes as C
 import operator
 import os
@@ -773,34 +774,32 @@ def cas_attention_shared(ctx: Context, kv: KVCache, layer, seqs, prefix_len, ful
     """Attention of several sequences whose first prefix_len positions are the same: lists of per-sequence tensors as in
     cas_attention."""
     torch = ctx._torch
-    n = len(seqs)
     outs = [torch.empty_like(q) for q in Qs] if outs is None else outs
     heads = Qs[0].shape[1]
-    cols, new, ptrs = _check_attention(kv, heads, Qs, Knews, Vnews, outs, _bf16_bits(torch))
-    assert n == len(cols)
-    i32, ptr = C.c_int32 * n, C.c_void_p * n
-    q, k, v, o = (ptr(*p) for p in ptrs)
-    ctx._check(_lib().cas_attention_shared(ctx.h, kv.h, layer, n, i32(*seqs), prefix_len, 1 if full else 0, q, i32(*cols), heads, k, v,
-                                           i32(*new), o), "cas_attention_shared")
+    held, (s, cols, new), (q, k, v, o) = _attention_args(kv, seqs, heads, Qs, Knews, Vnews, outs, _bf16_bits(torch))
+    ctx._check(_lib().cas_attention_shared(ctx.h, kv.h, layer, len(seqs), s, prefix_len, 1 if full else 0, q, cols, heads, k, v, new, o),
+               "cas_attention_shared")
     return outs
 
 
 _DTYPE, _IS_CUDA, _SHAPE, _NBYTES = (operator.attrgetter(x) for x in ("dtype", "is_cuda", "shape", "nbytes"))
 
 
-def _check_attention(kv: KVCache, heads, Qs, Knews, Vnews, outs, bits):
-    """Shapes, types and layout of the sequences' tensors: their columns, in-flight vectors, and addresses."""
-    d, n, ts = kv.desc.head_dim, len(Qs), [*Qs, *Knews, *Vnews, *outs]
-    assert n == len(Knews) == len(Vnews) == len(outs)
+def _attention_args(kv: KVCache, seqs, heads, Qs, Knews, Vnews, outs, bits):
+    """Shapes, types and layout of the sequences' tensors, and the host arrays of a call: the sequences with their columns and
+    in-flight vectors as int32, the addresses of the four lists, and where each of these begins."""
+    d, kh, n, ts = kv.desc.head_dim, kv.desc.n_kv_heads, len(Qs), [*Qs, *Knews, *Vnews, *outs]
+    assert n == len(seqs) == len(Knews) == len(Vnews) == len(outs)
     qs, ks = list(map(_SHAPE, Qs)), list(map(_SHAPE, Knews))
-    cols, new, sizes = [s[0] for s in qs], [s[0] for s in ks], list(map(_NBYTES, ts))
-    kh = kv.desc.n_kv_heads
+    cols, new = [s[0] for s in qs], [s[0] for s in ks]
     assert qs == [(c, heads, d) for c in cols] and ks == [(c, kh, d) for c in new]
-    assert sizes[2 * n:] == sizes[n:2 * n] + sizes[:n] and all(map(_IS_CUDA, ts)) and set(map(_DTYPE, ts)) <= bits
+    assert all(map(_IS_CUDA, ts)) and set(map(_DTYPE, ts)) <= bits
     tensor = type(ts[0])
     assert all(map(tensor.is_contiguous, ts))
-    ptrs = list(map(tensor.data_ptr, ts))
-    return cols, new, [ptrs[i:i + n] for i in range(0, 4 * n, n)]
+    assert list(map(_NBYTES, ts[2 * n:])) == [2 * kh * d * c for c in new] + [2 * heads * d * c for c in cols]
+    ints, ptrs = array.array("i", [*seqs, *cols, *new]), array.array("Q", map(tensor.data_ptr, ts))
+    i, p = ints.buffer_info()[0], ptrs.buffer_info()[0]
+    return (ints, ptrs), (i, i + 4 * n, i + 8 * n), (p, p + 8 * n, p + 16 * n, p + 24 * n)
 
 
 def cas_attention_shared_bytes(kv: KVCache, seqs, prefix_len, ncols, n_q_heads, n_new) -> int:
@@ -813,15 +812,11 @@ def cas_attention_window(ctx: Context, kv: KVCache, layer, seqs, n_first, window
     """Attention of several sequences whose columns see the first n_first positions and the last `window` up to their own: lists
     of per-sequence tensors as in cas_attention."""
     torch = ctx._torch
-    n = len(seqs)
     outs = [torch.empty_like(q) for q in Qs] if outs is None else outs
     heads = Qs[0].shape[1]
-    cols, new, ptrs = _check_attention(kv, heads, Qs, Knews, Vnews, outs, _bf16_bits(torch))
-    assert n == len(cols)
-    i32, ptr = C.c_int32 * n, C.c_void_p * n
-    q, k, v, o = (ptr(*p) for p in ptrs)
-    ctx._check(_lib().cas_attention_window(ctx.h, kv.h, layer, n, i32(*seqs), n_first, window, 1 if full else 0, q, i32(*cols), heads, k, v,
-                                           i32(*new), o), "cas_attention_window")
+    held, (s, cols, new), (q, k, v, o) = _attention_args(kv, seqs, heads, Qs, Knews, Vnews, outs, _bf16_bits(torch))
+    ctx._check(_lib().cas_attention_window(ctx.h, kv.h, layer, len(seqs), s, n_first, window, 1 if full else 0, q, cols, heads, k, v, new, o),
+               "cas_attention_window")
     return outs
 
 
