@@ -79,7 +79,7 @@ CASES = [  # kv heads, query heads, lengths, tokens, keep, t, mode, channels tha
     (2, 0, [63, 64, 0], [1, 1, 2], 600, 4, 2, 128, 1, False),
     (2, 6, [5, 0, 127, 9], [0, 70, 1, 0], 700, 3, 0, 64, 0, False),
     (3, 3, [31] * 32, [1 + i % 6 for i in range(32)], 500, 1, 2, 2, 1, True),
-    (8, 8, [100], [300], 600, 4, 0, 128, 0, True),               # from here on four vectors to a wave
+    (8, 8, [100], [300], 600, 4, 0, 128, 0, True),
     (8, 24, [1021], [1000], 600, 4, 0, 128, 0, True),
     (8, 3, [13, 0, 64, 200], [100, 1, 0, 150], 600, 4, 2, 96, 0, False),
     (8, 17, [13, 0, 64, 201], [130, 3, 64, 77], 400, 0, 0, 128, 1, True),
@@ -88,6 +88,23 @@ CASES = [  # kv heads, query heads, lengths, tokens, keep, t, mode, channels tha
     (8, 0, [3] * 20, [17] * 20, 333, 2, 2, 32, 0, True),
     (16, 16, [250], [515], 600, 6, 0, 16, 0, False),
     (4, 70, [0], [900], 600, 4, 0, 6, 0, True),
+    # sixteen vectors to a wave, from 24 for each CU (30 over shared exponents) on: every t, both forms, all kinds of partners
+    (8, 3, [13, 0, 64, 200], [260, 1, 0, 259], 600, 4, 2, 96, 0, False),
+    (8, 17, [13, 0, 64, 201], [330, 3, 64, 177], 400, 0, 0, 128, 1, True),
+    (8, 17, [15, 0, 64, 201], [331, 3, 65, 176], 400, 0, 2, 128, 1, True),
+    (8, 4, [7, 1], [601, 3], 1000, 7, 0, 62, 0, True),
+    (8, 4, [7, 1], [601, 3], 1000, 7, 2, 126, 0, False),
+    (8, 5, [7, 1], [601, 3], 0, 5, 0, 126, 1, False),
+    (8, 5, [7, 1], [601, 3], 0, 5, 2, 128, 0, True),
+    (8, 0, [3] * 20, [33] * 20, 333, 2, 2, 32, 0, True),
+    (8, 1, [i for i in range(32)], [17 + i % 7 for i in range(32)], 333, 2, 0, 128, 0, False),
+    (16, 2, [47], [400], 500, 1, 0, 2, 0, True),
+    (16, 2, [47], [400], 8, 1, 2, 2, 1, True),
+    (16, 0, [48], [400], 992, 3, 0, 64, 0, False),
+    (16, 0, [48], [400], 700, 3, 2, 6, 1, False),
+    (8, 8, [63], [641], 600, 5, 2, 64, 1, True),
+    (8, 8, [63], [641], 600, 6, 2, 16, 0, True),
+    (48, 8, [1], [130], 600, 2, 0, 30, 0, True),
 ]
 
 
@@ -200,7 +217,7 @@ def test_pages_outside_the_pool_are_not_written(env, n_tok):
             assert torch.equal(got, want), entry
 
 
-@pytest.mark.parametrize("n_tok", [2, 300])
+@pytest.mark.parametrize("n_tok", [2, 500])
 def test_pools_beyond_32_bits(env, n_tok):
     """The last pages of the last layer, tens of gigabytes into the pools."""
     torch, B, ctx = env
@@ -215,7 +232,7 @@ def test_pools_beyond_32_bits(env, n_tok):
     assert torch.equal(K, kb) and torch.equal(V, vb)
 
 
-@pytest.mark.parametrize("n_tok", [4, 400])
+@pytest.mark.parametrize("n_tok", [4, 500])
 def test_streams_and_captured_calls(env, n_tok):
     """A captured call replayed over new heads and positions, with eager calls and waits between."""
     torch, B, _ = env
@@ -247,6 +264,34 @@ def test_streams_and_captured_calls(env, n_tok):
             assert torch.equal(out, want), seed
             assert torch.equal(held.spec_pool, eager.spec_pool) and torch.equal(held.verif_pool, eager.verif_pool), seed
             pos.copy_(held_pos)
+
+
+@pytest.mark.parametrize("mode", [0, 2])
+@pytest.mark.parametrize("t,keep,start,n_tok", [(0, 600, 5, 1301), (1, 700, 0, 1300), (2, 1000, 63, 1298), (3, 8, 64, 1216), (4, 600, 1, 1215), (5, 0, 16, 1297), (6, 992, 17, 1300),
+                                                (7, 400, 31, 1300)])
+def test_long_appends_are_their_pieces(env, t, keep, start, n_tok, mode):
+    """cas_kv_append of enough vectors for sixteen to a wave, against appends of a few tokens each; infinities, NaN, equal
+    magnitudes and zeros among them."""
+    torch, B, ctx = env
+    g = torch.Generator(device="cuda").manual_seed(t)
+    k, v = (torch.randn(n_tok, 8, 128, generator=g, device="cuda").bfloat16() for _ in range(2))
+    k[3::7] = k[3::7].round()                       # many equal magnitudes
+    v[5::11] = 0
+    v[6::11, :, ::2] = -0.0
+    k[8::13, :, 5] = float("inf")
+    k[9::13, :, 100:] = float("nan")
+    k[10::13] *= 2.0 ** 100                         # exponents far apart
+    k[11::13, :, :64] *= 2.0 ** -126                # subnormal numbers
+    one, two = _caches(torch, B, ctx, 2, 8, [start], [n_tok], keep, t, mode)
+    k, v = k.view(torch.int16), v.view(torch.int16)
+    B.cas_kv_append(ctx, one, 1, 0, k, v)
+    i = 0
+    while i < n_tok:
+        n = min(3 + i % 14, n_tok - i)
+        B.cas_kv_set_len(two, 0, start + i)
+        B.cas_kv_append(ctx, two, 1, 0, k[i:i + n].contiguous(), v[i:i + n].contiguous())
+        i += n
+    assert torch.equal(one.spec_pool, two.spec_pool) and torch.equal(one.verif_pool, two.verif_pool)
 
 
 def test_refusals(env):
