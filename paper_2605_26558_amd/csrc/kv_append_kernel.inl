@@ -197,6 +197,33 @@ struct RowsStage {
   uint32_t words[kAppendRows * 78];  // (128 + 15 + 8 kept, none pruned) or less: 76 words a vector
 };
 
+// A vector of 128 values in the stage, by which lanes exchange them: eights of values at places that lie in different banks for four
+// lanes with neighbouring eights and for four that are four eights apart, of four rows
+struct VectorRow {
+  uint16_t* base;
+  int turn;
+  __device__ __forceinline__ VectorRow(RowsStage& st, int r) : base(reinterpret_cast<uint16_t*>(st.words) + 128 * r), turn(40 * (r & 3)) {}
+  __device__ __forceinline__ void put(int c, const uint32_t (&w)[4]) const {
+    *reinterpret_cast<uint4*>(base + (c ^ turn)) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ void eight(int c, uint32_t (&w)[4]) const {
+    const uint4 v = *reinterpret_cast<const uint4*>(base + (c ^ turn));
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  }
+  __device__ __forceinline__ uint32_t one(int c) const { return base[c ^ turn]; }
+  // Four lanes j: channels 32 k + 8 j .. + 7 of x[k] -> 32 j + 8 k .. + 7
+  __device__ __forceinline__ void swap(uint32_t (&x)[4][4], int j) const {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) put(32 * k + 8 * j, x[k]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) eight(32 * j + 8 * k, x[k]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+};
+
 // columns (2 i, 2 i + 1) of the first and the last 16 of a word, two registers each -> (2 i, 16 + 2 i) and (2 i + 1, 17 + 2 i)
 __device__ __forceinline__ uint32_t low_pair(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_pair(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); }

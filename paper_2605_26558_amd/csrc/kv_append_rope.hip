@@ -98,17 +98,27 @@ __global__ __launch_bounds__(64 * kAppendWaves) void rope_append_few_kernel(Rope
   format_one(g, a.spec_pool, a.verif_pool, stages[wv], v0, v1, lane, a.layer, page, which - 1, head, place & 63);
 }
 
-// N channels of a vector from c on, as they lie in memory: floats, or bf16 in half as many words; and rounded, two to a word
-template <int N>
-__device__ __forceinline__ void request(uint64_t row, int c, bool fp32, uint32_t (&w)[N]) {
-  if (fp32) __builtin_memcpy(w, reinterpret_cast<const void*>(row + 4u * (uint32_t)c), 4 * N);
-  else __builtin_memcpy(w, reinterpret_cast<const void*>(row + 2u * (uint32_t)c), 2 * N);
+typedef float rope_f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 rope_bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t two_bf16(float x, float y) {  // in one operation
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(rope_f32x2{x, y}, rope_bf16x2));
 }
+// N eights of channels of a vector, from c on and 32 apart, rounded, two to a word
 template <int N>
-__device__ __forceinline__ void take(const uint32_t (&raw)[N], bool fp32, uint32_t (&w)[N / 2]) {
+__device__ __forceinline__ void request(uint64_t row, int c, bool fp32, uint32_t (&x)[N][4]) {
+  if (fp32) {
+    float raw[N][8];
 #pragma unroll
-  for (int i = 0; i < N / 2; ++i)
-    w[i] = fp32 ? (uint32_t)f32_to_bf16(__uint_as_float(raw[2 * i])) | (uint32_t)f32_to_bf16(__uint_as_float(raw[2 * i + 1])) << 16 : raw[i];
+    for (int k = 0; k < N; ++k) __builtin_memcpy(raw[k], reinterpret_cast<const float*>(row) + c + 32 * k, 32);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[k][i] = two_bf16(raw[k][2 * i], raw[k][2 * i + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) __builtin_memcpy(x[k], reinterpret_cast<const uint16_t*>(row) + c + 32 * k, 16);
+  }
 }
 __device__ __forceinline__ float low_value(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_value(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -158,32 +168,46 @@ struct EightAngles {
       }
     }
   }
-  // w: channels c0 .. c0 + 7, two to a word; o: their partners
+  // w: channels c0 .. c0 + 7, two to a word; o: their partners; SECOND: of the second half (HOW = kHalfAway)
+  template <bool SECOND = false>
   __device__ __forceinline__ void turn(const RopeAppendArgs& a, int c0, const uint32_t (&o)[4], uint32_t (&w)[4]) const {
+    const Pairing all(c0, a.half, false);  // eight channels that follow one another are alike but for kSingles
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const Pairing p0(c0 + 2 * i, a.half, HOW == kNeighbours), p1(c0 + 2 * i + 1, a.half, HOW == kNeighbours);
-      const uint32_t x = o[i] ^ ((p0.first ? 0x8000u : 0u) | (p1.first ? 0x80000000u : 0u));  // y_a = x_a cos + (-x_b) sin
+      uint32_t x = o[i];  // y_a = x_a cos + (-x_b) sin
+      bool turns = true;
+      if constexpr (HOW == kHalfAway) {
+        x ^= SECOND ? 0u : 0x80008000u;
+      } else if constexpr (HOW == kNeighbours) {
+        x ^= 0x00008000u;
+        turns = c0 + 2 * i < 2 * a.half;  // an even number of channels turns
+      } else if constexpr (HOW == kEights) {
+        x ^= all.first ? 0x80008000u : 0u;
+        turns = all.turns;
+      } else {
+        const Pairing p0(c0 + 2 * i, a.half, false), p1(c0 + 2 * i + 1, a.half, false);
+        x ^= (p0.first ? 0x8000u : 0u) | (p1.first ? 0x80000000u : 0u);
+        turns = p0.turns;
+      }
       const float y0 = low_value(w[i]) * c[2 * i] + low_value(x) * s[2 * i];
       const float y1 = high_value(w[i]) * c[2 * i + 1] + high_value(x) * s[2 * i + 1];
-      const uint32_t y = (uint32_t)f32_to_bf16(y0) | (uint32_t)f32_to_bf16(y1) << 16;
-      w[i] = HOW == kHalfAway || p0.turns ? y : w[i];  // an even number of channels turns
+      const uint32_t y = two_bf16(y0, y1);
+      w[i] = turns ? y : w[i];
     }
   }
 };
-// The partners of channels c0 .. c0 + 7: of the words themselves, of a lane DPP control AWAY, or out of the vector's 128 values in LDS
-template <int HOW, int AWAY>
-__device__ __forceinline__ void partners(const RopeAppendArgs& a, int c0, const uint16_t* row, const uint32_t (&w)[4], uint32_t (&o)[4]) {
-  if constexpr (HOW == kEights) {
-    const uint4 x = *reinterpret_cast<const uint4*>(row + Pairing(c0, a.half, false).other);
-    o[0] = x.x; o[1] = x.y; o[2] = x.z; o[3] = x.w;
+// The partners of channels c0 .. c0 + 7 where they are not in words of the lane's own: of the words themselves, or out of the vector's values in LDS
+template <int HOW>
+__device__ __forceinline__ void partners(const RopeAppendArgs& a, int c0, const VectorRow& row, const uint32_t (&w)[4], uint32_t (&o)[4]) {
+  if constexpr (HOW == kNeighbours) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_alignbit(w[i], w[i], 16);
+  } else if constexpr (HOW == kEights) {
+    row.eight(Pairing(c0, a.half, false).other, o);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (HOW == kHalfAway) o[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[i], AWAY, 0xf, 0xf, true);
-      else if constexpr (HOW == kNeighbours) o[i] = __builtin_amdgcn_alignbit(w[i], w[i], 16);
-      else o[i] = (uint32_t)row[Pairing(c0 + 2 * i, a.half, false).other] | (uint32_t)row[Pairing(c0 + 2 * i + 1, a.half, false).other] << 16;
-    }
+    for (int i = 0; i < 4; ++i)
+      o[i] = row.one(Pairing(c0 + 2 * i, a.half, false).other) | row.one(Pairing(c0 + 2 * i + 1, a.half, false).other) << 16;
   }
 }
 
@@ -195,8 +219,6 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
   const KvGeom& g = a.g;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   RowsStage& st = stages[wv];
-  // vectors of 128 values that lanes exchange, in different banks
-  auto vector_row = [&](int i) { return reinterpret_cast<uint16_t*>(st.words) + 136 * i; };
   const LaneTable t_tok0(a.tok0), t_seq(a.seq), t_len(a.len), t_n(a.n), t_group0(a.group0);
   auto share = [] {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -211,9 +233,9 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
     auto heads = [&](auto&& turn) {
       for (int h0 = first; h0 < a.n_q; h0 += a.q_blocks * 4 * kAppendWaves) {  // uniform in the wave
         const int head = min(h0 + q, a.n_q - 1);
-        uint32_t raw[8], w[4];
-        request(part.x + (uint64_t)(tok * part.ldx) + (uint32_t)head * (part.fp32 ? 512u : 256u), 8 * l, part.fp32, raw);
-        take(raw, part.fp32, w);
+        uint32_t x[1][4];
+        uint32_t (&w)[4] = x[0];
+        request(part.x + (uint64_t)(tok * part.ldx) + (uint32_t)head * (part.fp32 ? 512u : 256u), 8 * l, part.fp32, x);
         turn(w);
         if (h0 + q < a.n_q)
           __builtin_memcpy(reinterpret_cast<uint16_t*>(part.y + (uint64_t)(tok * part.ldy)) + head * 128 + 8 * l, w, 16);
@@ -229,12 +251,18 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
       cs.load(a, p, 8 * l);
       heads([&](uint32_t (&w)[4]) {
         uint32_t o[4];
-        if constexpr (how >= kEights) {
-          *reinterpret_cast<uint4*>(vector_row(q) + 8 * l) = make_uint4(w[0], w[1], w[2], w[3]);
-          share();
+        if constexpr (how == kHalfAway) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[i], 0x128, 0xf, 0xf, true) ^ (l < 8 ? 0u : 0x80008000u);  // row_ror:8
+        } else {
+          const VectorRow row(st, q);
+          if constexpr (how >= kEights) {
+            row.put(8 * l, w);
+            share();
+          }
+          partners<how>(a, 8 * l, row, w, o);
+          if constexpr (how >= kEights) share();
         }
-        partners<how, 0x128>(a, 8 * l, vector_row(q), w, o);  // row_ror:8
-        if constexpr (how >= kEights) share();
         cs.turn(a, 8 * l, o, w);
       });
     });
@@ -243,51 +271,64 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
   const int unit = (int)blockIdx.x * kAppendWaves + wv;
   if (unit >= a.units) return;
   const int rest = unit / g.n_kv_heads, head = unit - rest * g.n_kv_heads, kv = rest & 1, group = rest >> 1;
-  const int r = lane >> 2, c0 = 32 * (lane & 3);
+  const int r = lane >> 2, c0 = 8 * (lane & 3);  // the lane's channels: c0 + 32 k .. c0 + 32 k + 7, as four lanes read side by side
   const int s = t_group0.which(group), pos0 = t_len[s];
   const int posw = (pos0 & -kAppendRows) + (group - t_group0[s]) * kAppendRows;     // place of the wave's first row
   const int ra = max(pos0 - posw, 0), rb = min(pos0 + t_n[s] - posw, kAppendRows);  // the wave's rows ra .. rb - 1 are new
   const RopeAppendPart part = a.part[1 + kv];
   const int place = posw + min(max(r, ra), rb - 1), tok = t_tok0[s] + place - pos0;  // rows that are not new repeat one that is
-  uint32_t raw[32];
-  request(part.x + (uint64_t)(tok * part.ldx) + (uint32_t)head * (part.fp32 ? 512u : 256u), c0, part.fp32, raw);
-  const int page = a.table[(size_t)t_seq[s] * g.max_pages_per_seq + posw / 64];
   const int p = a.pos ? a.pos[tok] : place;
+  const int page = a.table[(size_t)t_seq[s] * g.max_pages_per_seq + posw / 64];
+  asm volatile("" ::: "memory");
+  uint32_t x[4][4];
+  request(part.x + (uint64_t)(tok * part.ldx) + (uint32_t)head * (part.fp32 ? 512u : 256u), c0, part.fp32, x);
   const uint64_t lanes = __builtin_amdgcn_ballot_w64(p >= 0 && p < a.n_pos && r >= ra && r < rb);
   if (lanes == 0) return;
   uint32_t rows = 0;  // those that are written
 #pragma unroll
   for (int i = 0; i < kAppendRows; ++i) rows |= (uint32_t)(lanes >> (4 * i) & 1) << i;
-  uint32_t x[4][4];  // eight channels each
-  {
-    uint32_t y[16];
-    take(raw, part.fp32, y);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i >> 2][i & 3] = y[i];
-  }
+  const VectorRow row(st, r);
   if (part.turn) {
+    const int at = min(max(p, 0), a.n_pos - 1);
     with_partners(a, [&](auto H) {
       constexpr int how = decltype(H)::value;
-      uint16_t* const row = vector_row(r);
-      if constexpr (how >= kEights) {
+      if constexpr (how == kHalfAway) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(row + c0 + 8 * i) = make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]);
-        share();
-      }
+        for (int k = 0; k < 2; ++k) {
+          EightAngles<how> cs;
+          uint32_t o[4];
+          cs.load(a, at, c0 + 32 * k);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        EightAngles<how> cs;
-        uint32_t o[4];
-        cs.load(a, min(max(p, 0), a.n_pos - 1), c0 + 8 * i);
-        partners<how, 0x4E>(a, c0 + 8 * i, row, x[i], o);  // the other pair of the four lanes
-        cs.turn(a, c0 + 8 * i, o, x[i]);
-        asm volatile("" ::: "memory");  // the angles of all four eights at once do not fit the registers
+          for (int i = 0; i < 4; ++i) o[i] = x[k][i];
+          cs.turn(a, c0 + 32 * k, x[k + 2], x[k]);
+          cs.template turn<true>(a, c0 + 32 * k, o, x[k + 2]);
+          asm volatile("" ::: "memory");  // the angles of all at once do not fit the registers
+        }
+      } else {
+        if constexpr (how >= kEights) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) row.put(c0 + 32 * k, x[k]);
+          share();
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          EightAngles<how> cs;
+          uint32_t o[4];
+          cs.load(a, at, c0 + 32 * k);
+          partners<how>(a, c0 + 32 * k, row, x[k], o);
+          cs.turn(a, c0 + 32 * k, o, x[k]);
+          asm volatile("" ::: "memory");
+        }
+        if constexpr (how >= kEights) share();
       }
-      if constexpr (how >= kEights) share();
     });
   }
-  if (part.y && (rows >> r & 1))
-    __builtin_memcpy(reinterpret_cast<uint16_t*>(part.y + (uint64_t)(tok * part.ldy)) + head * 128 + c0, x, 64);
+  if (part.y && (rows >> r & 1)) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      __builtin_memcpy(reinterpret_cast<uint16_t*>(part.y + (uint64_t)(tok * part.ldy)) + head * 128 + c0 + 32 * k, x[k], 16);
+  }
+  row.swap(x, lane & 3);
   uint32_t w[16];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {

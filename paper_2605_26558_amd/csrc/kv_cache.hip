@@ -51,13 +51,15 @@ __global__ __launch_bounds__(64 * kAppendWaves) void kv_append_rows_kernel(KvGeo
   const int page = page_row[posw / 64];
   const int tok = posw + min(max(lane >> 2, ra), rb - 1) - pos0;  // rows that are not new repeat one that is
   const uint16_t* src = (kv ? Vn : Kn) + (size_t)(blockIdx.z >> 1) * layer_stride +
-                        ((size_t)tok * g.n_kv_heads + head) * 128 + 32 * (lane & 3);
-  uint32_t x[16], w[16];
-  __builtin_memcpy(x, src, 64);
+                        ((size_t)tok * g.n_kv_heads + head) * 128 + 8 * (lane & 3);
+  uint32_t x[4][4], w[16];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) __builtin_memcpy(x[k], src + 32 * k, 16);
+  VectorRow(stages[wv], lane >> 2).swap(x, lane & 3);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    w[2 * i] = low_pair(x[i], x[8 + i]);
-    w[2 * i + 1] = high_pair(x[i], x[8 + i]);
+    w[2 * i] = low_pair(x[i >> 2][i & 3], x[2 + (i >> 2)][i & 3]);
+    w[2 * i + 1] = high_pair(x[i >> 2][i & 3], x[2 + (i >> 2)][i & 3]);
   }
   format_rows<T, MX>(g, spec_pool, verif_pool, stages[wv], w, lane, layer, page, kv, head, posw & 63, (0xFFFFu << ra) & (0xFFFFu >> (kAppendRows - rb)));
 }
