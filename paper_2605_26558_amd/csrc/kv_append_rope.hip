@@ -340,10 +340,11 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
 
 static int launch_rope_append(cas_ctx* ctx, RopeAppendArgs& a, int n_seqs) {
   const KvGeom& g = a.g;
-  // Up to 24 vectors of K and V per CU (30 over shared exponents) a wave takes each, above sixteen.  us, one / sixteen a wave, tokens of 8
-  // heads bf16 without queries: 128 4.0 / 7.6, 384 6.6 / 7.8, 512 7.8 / 7.9, 1021 13.1 / 9.2; fp32 with 32 query heads: 256 7.8 / 9.2, 384 10.0 /
-  // 9.7, 512 12.1 / 10.1, 1021 23.6 / 12.5; over shared exponents 384 7.0 / 9.5 and 10.4 / 11.3, 512 8.3 / 9.6 and 12.3 / 11.8
-  if ((int64_t)a.n_tok * g.n_kv_heads * 2 <= (int64_t)(g.mx ? 30 : 24) * ctx->num_cu) {
+  // Up to 24 vectors of K and V per CU (32 over shared exponents) a wave takes each, above sixteen; four of a token's queries are
+  // one of these.  us, one / sixteen a wave, tokens of 8 heads bf16 without queries: 256 5.3 / 6.5, 384 6.5 / 6.5, 512 7.8 / 6.6, 1021
+  // 13.0 / 7.9; fp32 with 32 query heads: 192 6.7 / 6.9, 256 7.6 / 7.2, 512 12.5 / 8.3, 1021 23.4 / 10.8; over shared exponents 384 7.0 /
+  // 8.3, 512 8.3 / 8.3, 640 9.6 / 8.3 and 320 9.2 / 9.0, 384 10.5 / 9.4
+  if ((int64_t)a.n_tok * (g.n_kv_heads * 2 + a.n_q / 4) <= (int64_t)(g.mx ? 32 : 24) * ctx->num_cu) {
     const dim3 grid((a.n_tok + kAppendWaves - 1) / kAppendWaves, a.n_q + 2 * g.n_kv_heads);
     hipLaunchKernelGGL(rope_append_few_kernel, grid, dim3(64 * kAppendWaves), 0, ctx->stream, a);
     CAS_HIP(ctx, hipGetLastError());

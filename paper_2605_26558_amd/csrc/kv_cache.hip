@@ -122,9 +122,9 @@ int launch_kv_append_layers(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, 
     return CAS_OK;
   }
   const int groups = (pos0 + n_tok - 1) / kAppendRows - pos0 / kAppendRows + 1;
-  // Of sixteen from 48 vectors per CU on (72 over shared exponents).  us, four / sixteen: 512 tokens of 8 heads 5.17 / 5.45, 768 6.1 / 5.6, 1021 7.1 /
-  // 6.6, 4096 18.6 / 11.4; over shared exponents 1021 7.8 / 8.0, 2048 12.3 / 9.3, 4096 21.3 / 14.7
-  const bool many = (int64_t)n_tok * g.n_kv_heads * 2 * n_layers >= (int64_t)(g.mx ? 72 : 48) * ctx->num_cu;
+  // Of sixteen from 36 vectors per CU on (72 over shared exponents).  us, four / sixteen: 512 tokens of 8 heads 5.06 / 5.32, 640 5.93 / 5.45,
+  // 1021 7.1 / 6.6, 4096 19.0 / 11.8; over shared exponents 768 6.5 / 7.1, 1021 7.7 / 7.8, 1500 10.0 / 9.4, 4096 21.5 / 15.1
+  const bool many = (int64_t)n_tok * g.n_kv_heads * 2 * n_layers >= (int64_t)(g.mx ? 72 : 36) * ctx->num_cu;
   const dim3 grid(many ? (groups + kAppendWaves - 1) / kAppendWaves : groups, g.n_kv_heads, 2 * n_layers);
 #define CAS_LAUNCH(TV)                                                                                              \
   case TV:                                                                                                          \

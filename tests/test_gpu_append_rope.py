@@ -88,7 +88,7 @@ CASES = [  # kv heads, query heads, lengths, tokens, keep, t, mode, channels tha
     (8, 0, [3] * 20, [17] * 20, 333, 2, 2, 32, 0, True),
     (16, 16, [250], [515], 600, 6, 0, 16, 0, False),
     (4, 70, [0], [900], 600, 4, 0, 6, 0, True),
-    # sixteen vectors to a wave, from 24 for each CU (30 over shared exponents) on: every t, both forms, all kinds of partners
+    # sixteen vectors to a wave, from 24 for each CU (32 over shared exponents) on: every t, both forms, all kinds of partners
     (8, 3, [13, 0, 64, 200], [260, 1, 0, 259], 600, 4, 2, 96, 0, False),
     (8, 17, [13, 0, 64, 201], [330, 3, 64, 177], 400, 0, 0, 128, 1, True),
     (8, 17, [15, 0, 64, 201], [331, 3, 65, 176], 400, 0, 2, 128, 1, True),
