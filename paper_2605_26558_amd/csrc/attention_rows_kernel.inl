@@ -216,10 +216,10 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
 
   // ---- what this workgroup works on (uniform)
   const SeqTable t_item0(a.item0), t_len(a.len), t_new(a.n_new), t_cols(a.ncols), t_seq(a.seq), t_splits(a.splits), t_part0(a.part0), t_run(a.run);
-  const bool prefix = item < a.prefix_items;
+  const bool prefix = !kWindow && item < a.prefix_items;  // none within a window
   int si = 0;
   if (!prefix) {
-    item -= a.prefix_items;
+    if (!kWindow) item -= a.prefix_items;
     si = t_item0.which(item);
     item -= t_item0[si];
   }
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
   };
   int left_out = 0;
   if constexpr (kWindow) left_out = win_pages.skip;
-  const int pg0 = (prefix ? 0 : a.prefix_pages) + split * run, pg1 = min(pg0 + run, (total + 63) / 64 - left_out), steps = (pg1 - pg0 + kPages - 1) / kPages;
+  const int pg0 = (prefix || kWindow ? 0 : a.prefix_pages) + split * run, pg1 = min(pg0 + run, (total + 63) / 64 - left_out), steps = (pg1 - pg0 + kPages - 1) / kPages;
   const int32_t* page_row = a.table + (size_t)t_seq[si] * g.max_pages_per_seq;
   const uint32_t first = prefix ? 0 : (uint32_t)t_part0[si];  // of the partial results
   const int splits = prefix ? a.prefix_splits : t_splits[si];
@@ -378,9 +378,12 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
         __builtin_amdgcn_wave_barrier();
         uint16_t* const slab = tiles + set * kSet + slot * kRowsPage + 4 * kKSlab + (u & 3) * kVSlab + kVPos;
         uint32_t odd = 0;
-        for (int k = lane; k < 256; k += 64) {  // eight tokens of a position and word
+        int k = lane;
+        asm volatile("" : "+v"(k));  // nothing of this ahead of the loop over pages, where it would take registers of it
+#pragma unroll 1
+        for (; k < 256; k += 64) {  // eight tokens of a position and word
           uint16_t* const at = slab + (k >> 3) * kVPos + (k & 7) * 8;
-#pragma unroll
+#pragma unroll 1
           for (int e = 0; e < 8; ++e) {
             const int token = (k & 1) * 8 + e, pos = slab0 + token;
             if (pos >= win_pages.zone0 && pos < win_pages.zone1 && (at[e] & 0x7F80u) == 0x7F80u) {
@@ -390,7 +393,7 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
           }
         }
         uint32_t any = 0;
-#pragma unroll
+#pragma unroll 1
         for (int t = 0; t < 16; ++t) any |= __builtin_amdgcn_ballot_w64(odd >> t & 1) ? 1u << t : 0u;
         if (lane == 0) a.edge[((size_t)si * g.n_kv_heads + head) * 2 + (slab0 >> 4) - (win_pages.zone0 >> 4)] = any;
       }
@@ -467,17 +470,26 @@ __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kerne
     if constexpr (kWindow) all_in = all_in && (pg * 64 + 63 < a.n_first || pg * 64 >= win_pages.lowest + ncols - 1);
     if (!all_in) {
       const int seen = all_see + (int)((uint32_t)row * a.grp_inv >> 16);  // column c sees c positions more
-      auto sees = [&](int pos) {
-        if constexpr (kWindow) return pos <= seen && (pos < a.n_first || pos > seen - a.window);
-        else return pos <= seen;
-      };
+      // from the lane's first token on: the last one that it sees, and within a window those between the first positions and it
+      const int base = pg * 64 + token(0), last = seen - base;
+      int hidden = 0;
+      uint32_t n_hidden = 0;
+      if constexpr (kWindow) {
+        hidden = a.n_first - base;
+        n_hidden = (uint32_t)max(max(seen - a.window, -1) - a.n_first + 1, 0);  // a sum of the two may pass 32 bits
+      }
 #pragma unroll
       for (int tt = 0; tt < NS; ++tt) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[tt][e] = sees(pg * 64 + token(tt) + e) ? x[tt][e] : -INFINITY;
+        for (int e = 0; e < 4; ++e) {
+          const int i = token(tt) - token(0) + e;
+          bool sees = i <= last;
+          if constexpr (kWindow) sees = sees && (uint32_t)(i - hidden) >= n_hidden;
+          x[tt][e] = sees ? x[tt][e] : -INFINITY;
+        }
       }
     }
-    if (a.score != nullptr && row < rows) {
+    if (!kWindow && a.score != nullptr && row < rows) {
       float* const to = a.score + ((size_t)head * rows + row) * a.score_ld + pg * 64;
 #pragma unroll
       for (int tt = 0; tt < NS; ++tt) *reinterpret_cast<rows_f32x4*>(to + token(tt)) = x[tt] * a.scale2;
