@@ -12,6 +12,10 @@
 //   launch 2, workgroups per sequence: each joins the chunks of the sequence's rows and judges the drafts, and where one is not kept forms
 //             sums of max(0, p - q) over its pieces of the vocabulary.  Left out where there are no drafts
 //   launch 3, a workgroup per sequence: looks up the piece (or the chunk of launch 1, where all drafts are kept), then the token
+//
+// Measured (us; in brackets the bytes of the logits at the rate of a copy): 32 sequences of up to 7 drafts over 128256 tokens 53 (32.2): launch 1 34, its
+// vector issue, 24 operations a value, 98 % of the cycles, at the rate of memory; launch 2 13.5 (row joins, then two exponentials a value of one row pair); launch 3
+// 5.  64 draws over 128256 17.1 (6.4): 10.5 and 6.6.  One sequence of 4 drafts over 32000 13.5 (0.2): three launches of dependent round trips.
 #include <algorithm>
 #include "cas_device.hpp"
 #include "cas_internal.hpp"

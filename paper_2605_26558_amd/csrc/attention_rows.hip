@@ -9,16 +9,25 @@
 //   grid: (runs of the prefix x blocks of all rows, then per sequence runs x blocks of its rows) x kv heads
 // A second kernel joins the partial results of a row in the order of the runs, prefix first.
 //
+// Attention within a window: the same kernel over the pages that a column of the sequence sees, those of the first positions and those of
+// the window, numbered one after the other; there is no prefix.  The rest of the page table is not looked at.  A run is as long as
+// there are places for all of the call's runs.  0 times an infinity of V would reach columns that do not see it: committed positions that only some
+// columns see (up to fifteen, in at most two groups of sixteen) are cleared of infinities and NaN in the tiles, and these are added where
+// the partial results are joined, as for vectors in flight.
+//
 // Attention weights: the partial kernel also writes the exponents of its scores, and the second launch, beside joining the
 // rows, forms the weights of all rows of a kv head from them and adds them up.  Exponents are 4 bytes per row and position,
 // a vector of K 131 in the draft form: cheaper than decoding K again.
 //
 // Measured (8 kv heads, 60 % kept, t = 4; us, both launches; in brackets the bytes of the streams at the rate of a copy): 16 sequences
-// of 4 query heads a kv head over a shared 8192 and 500 of their own, draft 30 (5.5), with shared exponents 36 (3.1); 8 of 5 columns,
-// exact, 300 of their own 42 (8.9), with shared exponents 47 (7.0); 32 of 8 query heads over 32768, exact, shared exponents 120 (29).
-// One sequence with weights: 8192 positions, exact 21.5 (7.7), draft 18 (3.7), with shared exponents 26 (6.1) and 22 (2.1); 30011 and 7
-// columns, exact 56 (28), draft 42 (14).  Bound by the vector operations of the decode: 58 to 66 % of a SIMD's cycles, the matrix
-// products and the LDS beside them (busy 21 and 41 % of the time with 256 rows).
+// of 4 query heads a kv head over a shared 8192 and 500 of their own, draft 30 (5.5), with shared exponents 34 (3.1); 8 of 5 columns,
+// exact, 300 of their own 42 (8.9), with shared exponents 46 (7.0); 32 of 8 query heads over 32768, exact, shared exponents 119 (29).
+// One sequence with weights: 8192 positions, exact 20.1 (7.7), draft 18 (3.7), with shared exponents 23 (6.1) and 20 (2.1); 30011 and 7
+// columns, exact 53 (28), draft 42 (14).  Within a window: one sequence, window 1024, draft 10.0 (0.4); 4096 and 7 columns, exact 19.4 (3.6); 16
+// sequences, 4096, draft 48 (28), exact 73; 16 of 5 columns and 8 query heads, 8192, exact, shared exponents 160 (91).
+// Bound by the vector operations of the decode: 58 to 84 % of a SIMD's cycles, the matrix products and the LDS beside them (busy 21 and
+// 41 % of the time with 256 rows); a short window of one sequence by the two launches and, in the first, four round trips that wait for each
+// other (arguments, page table, bitmap, fields).
 // Against the sequences' own decodes (cas_attention_multi), sharing / not: 2 sequences behind 703 positions 10.0 / 8.6, 4 behind 2000
 // 14.1 / 13.6, 8 of 5 columns behind 500, exact, 25 / 27, 16 behind 256 15 / 34, behind 8192 29 / 107: it pays from
 // some four sequences on, and for more whatever the prefix is.

@@ -192,8 +192,10 @@ __device__ __forceinline__ void load_window(__amdgpu_buffer_rsrc_t rs, int off, 
 // that a CU was busy with 256 rows over 32768 positions, now 31 of 189.)  The walks' writes meet more often for it (some 4 lanes in
 // place of 2), which is less.
 //
-// 128 registers a lane are what sixteen waves a CU leave.  The draft forms fit; the exact ones spill 10, 14, 9 and 1 of them at t = 4
-// (RT = 2, 4, 8, 16; with shared exponents 8, 8, 8 and 0), 31 at the most (t = 6, RT = 4).
+// 128 registers a lane are what sixteen waves a CU leave.  The draft forms fit; the exact ones spill 1, 8, 8 and 1 of them at t = 4
+// (RT = 2, 4, 8, 16; with shared exponents 20, 12, 12 and 2), 25 at the most (t = 5, RT = 4); within a window 0, 16, 16 and 0 (4, 12, 6
+// and 2), 20 at the most.  They cost time: with what only some pages need (the mask, positions that some columns see) worked out ahead of the
+// loop over pages 25 to 35 were spilled within a window, and 128 rows, exact, took 281 us for 196.
 template <int T, bool FULL, bool MX, int RT, class ARGS>
 __global__ __launch_bounds__(64 * RowsShape<RT>::kWaves, 4) void attn_rows_kernel(ARGS a) {
   constexpr bool kWindow = std::is_same<ARGS, RowsWindowArgs>::value;

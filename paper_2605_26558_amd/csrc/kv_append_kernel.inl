@@ -1,4 +1,4 @@
-// The two encoders of the cache (Sec. 5.1), shared by the kernels that append vectors as they are (kv_cache.hip) and those
+// The three encoders of the cache (Sec. 5.1), shared by the kernels that append vectors as they are (kv_cache.hip) and those
 // that turn them on the way (kv_append_rope.hip).
 #pragma once
 #include "cas_device.hpp"
@@ -13,8 +13,8 @@ namespace cas {
 // Equals of the K-th are kept in the order of the columns.  Kept values go to a list in LDS by rank, of which a lane packs
 // 16 into the 16-T half words that their fields fill; the pruned ones to their place in the row.
 // One wave per vector with ballots (kv_append_few_kernel) is bound on a full chip by the scalar unit, which the SIMDs of a CU
-// share (298 scalar instructions per vector): 1021 tokens of 8 heads 11.6 us, so 7.7, of which the search takes 2 (5.6 with one step of the
-// fifteen, 6.7 with eight: some 19 vector instructions a step and four vectors); the rest is launch, memory and packing.
+// share (298 scalar instructions per vector): 640 tokens of 8 heads would take 9 us, so 5.9, of which the search is a quarter (some 19 vector instructions
+// a step and four vectors); the rest is launch, memory and packing.
 constexpr int kAppendWaves = 4, kAppendRows = 16;
 constexpr int kKeptPitch = 136;  // values of a list of kept ones: 16-byte steps, and vectors four banks apart
 
@@ -189,6 +189,8 @@ __device__ __forceinline__ void format_four(const KvGeom& g, uint32_t* spec_pool
 // candidate's bits so far and have the next one are counted, and either they or the others stay.  Equals of the K-th are kept in the order of
 // the columns.  Kept values go to a list in LDS by rank, of which a lane packs 16 into the 16-T half words that their
 // fields fill; the pruned ones to their place in the row.
+// Of the 25 us that 8000 tokens of 8 heads take with the turn (kv_append_rope.hip) the search is 1.5, the way to the lists and the packing 4, the
+// writes 6; some 1000 vector operations for sixteen vectors, a SIMD busy with them in 78 % of the cycles.
 
 // Of a wave.  First the lists of kept values, each to a whole group of 16 and eight more (so that vectors lie in different
 // banks), and behind them the pruned values, two to a word, row by row; then, once the lists are in registers, the fields and behind them the
