@@ -131,3 +131,62 @@ def test_a_draft_model_that_is_the_target_is_kept(env):
     m = Windowed(torch, B, [40, 77], 1000, 0)
     streams, kept = _run(torch, m, [0, 1], 8, False)
     assert kept == 2 * K * 8
+
+
+def test_graphs_of_one_context_in_turn(env):
+    """A captured appending, attention and verification that share a context and its workspace, replayed in changing order over
+    new inputs, give what a context of its own gives eagerly."""
+    torch, B = env
+    ks, vocab, lens, toks = [3, 0, 5], 9001, [200, 64, 1], [3, 1, 2]
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        size = max(B.cas_accept_tokens_bytes(ks, vocab), 1 << 22)
+        shared, own = (B.Context(workspace=torch.empty(size, dtype=torch.uint8, device="cuda")) for _ in range(2))
+        caches = [B.KVCache(c, 1, 2, 15, 3, 5) for c in (shared, own)]
+        table = torch.randn(400, 64, 2, device="cuda").contiguous()
+
+        def inputs(seed):
+            g = torch.Generator(device="cuda").manual_seed(seed)
+            rnd = lambda *s, **k: torch.randn(*s, generator=g, device="cuda", **k)  # noqa: E731
+            heads = [rnd(sum(toks), h, 128) for h in (8, 2, 2)]
+            flight = [rnd(t, h, 128).bfloat16().view(torch.int16) for h in (8, 2, 2) for t in toks]
+            logits = [rnd(sum(ks) + 3, vocab), rnd(sum(ks), vocab)]
+            tokens = torch.randint(0, vocab, (sum(ks),), generator=g, device="cuda", dtype=torch.int32)
+            return heads, flight, logits, tokens, torch.rand(sum(ks) + 3, generator=g, device="cuda", dtype=torch.float64)
+
+        def calls(ctx, kv, x):
+            (q, k, v), f, (t, d), tokens, r = x
+            return [lambda: [B.cas_kv_append_rope(ctx, kv, 0, [0, 1, 2], toks, table, k, v, q=q)],
+                    lambda: B.cas_attention_window(ctx, kv, 0, [0, 1, 2], 4, 100, True, f[:3], f[3:6], f[6:]),
+                    lambda: list(B.cas_accept_tokens(ctx, t, d, tokens, ks, r)[:2])]
+
+        for kv in caches:
+            for pool in (kv.spec_pool, kv.verif_pool):
+                pool.zero_()
+            for s, n in enumerate(lens):
+                k = torch.randn(n, 2, 128, generator=torch.Generator(device="cuda").manual_seed(s), device="cuda").bfloat16().view(torch.int16)
+                B.cas_kv_set_len(kv, s, 0)
+                B.cas_kv_append(shared if kv is caches[0] else own, kv, 0, s, k, k)
+                B.cas_kv_set_len(kv, s, n)
+        held, graphs = inputs(1), []
+        for f in calls(shared, caches[0], held):
+            f()
+            stream.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=stream):
+                out = f()
+            graphs.append((g, out))
+        flat = lambda x: [t for p in x for t in (p if isinstance(p, list) else [p])]  # noqa: E731
+        for seed, order in ((2, (0, 1, 2)), (3, (2, 1, 0)), (4, (1, 2, 0)), (5, (2, 0, 1))):
+            fresh = inputs(seed)
+            for h, f in zip(flat(held), flat(fresh)):
+                h.copy_(f)
+            eager = calls(own, caches[1], fresh)
+            for i in order:
+                graphs[i][0].replay()
+                want = eager[i]()
+                stream.synchronize()
+                for a, b in zip(graphs[i][1], want):
+                    assert torch.equal(a, b), (seed, i)
+            assert torch.equal(caches[0].spec_pool, caches[1].spec_pool) and torch.equal(caches[0].verif_pool, caches[1].verif_pool), seed
