@@ -9,7 +9,7 @@
 // 64 bits throughout: tokens of a vocabulary of 10^5 are a 10^-5 th apart in that sum, and with weights and sums of 32 bits one
 // draw in some thousands falls on a neighbour of the right one.
 //   launch 1, a workgroup per chunk of a row: the chunk's maximum and its sum of exponentials under it
-//   launch 2, workgroups per sequence: each joins the chunks of the sequence's rows and judges the drafts, and where one is not kept forms
+//   launch 2, workgroups per sequence: each joins the chunks of the sequence's rows and settles which drafts are kept, and where one is not kept forms
 //             sums of max(0, p - q) over its pieces of the vocabulary.  Left out where there are no drafts
 //   launch 3, a workgroup per sequence: looks up the piece (or the chunk of launch 1, where all drafts are kept), then the token
 //
@@ -41,7 +41,7 @@ struct RowStat {
   float max;
   int first;
 };
-struct AcceptVerdict {
+struct AcceptOutcome {
   RowStat t, d;  // of the rows behind the kept drafts
   int kept, x;   // x: the draft behind them, -1 if all are kept
 };
@@ -60,7 +60,7 @@ struct AcceptArgs {
   float* q;
   AcceptPart* part;    // [rows of the target, then of the draft][chunk]
   double* rest;        // [sequence][piece]
-  AcceptVerdict* verdict;  // [sequence]
+  AcceptOutcome* outcome;  // [sequence]
   int vocab, chunks, pieces, rows;  // rows: of the target
   int each;                         // pieces of a workgroup of the second launch
   int before[kAcceptSeqs + 1];      // drafts of the sequences before
@@ -396,7 +396,7 @@ __device__ __forceinline__ int token_at(const AcceptArgs& a, const Decision& w, 
 }
 
 // The drafts that are kept, by a workgroup of the sequence each
-__device__ __forceinline__ AcceptVerdict judge(const AcceptArgs& a, const Heat& heat, int s, int d0, int k, int tid, bool tell) {
+__device__ __forceinline__ AcceptOutcome settle(const AcceptArgs& a, const Heat& heat, int s, int d0, int k, int tid, bool tell) {
   __shared__ RowStat stats[2 * kAcceptDrafts + 1];
   __shared__ int s_kept, s_x;
   const int lane = tid & 63, n_rows = a.draft ? 2 * k + 1 : k + 1;
@@ -443,14 +443,14 @@ __device__ __forceinline__ AcceptVerdict judge(const AcceptArgs& a, const Heat& 
     }
   }
   __syncthreads();
-  AcceptVerdict v;
+  AcceptOutcome v;
   v.kept = __builtin_amdgcn_readfirstlane(s_kept);
   v.x = __builtin_amdgcn_readfirstlane(s_x);
   v.t = stats[v.kept];
   v.d = stats[a.draft && v.kept < k ? k + 1 + v.kept : v.kept];
   return v;
 }
-__device__ __forceinline__ Decision decide(const AcceptArgs& a, const AcceptVerdict& v, int s, int d0, int k) {
+__device__ __forceinline__ Decision decide(const AcceptArgs& a, const AcceptOutcome& v, int s, int d0, int k) {
   Decision w;
   w.t = v.t;
   w.d = v.d;
@@ -466,8 +466,8 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_drafts_kernel(AcceptArg
   const int s = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int d0 = a.before[s], k = a.before[s + 1] - d0;
   const Heat heat(a, s);
-  const AcceptVerdict v = judge(a, heat, s, d0, k, tid, blockIdx.x == 0);
-  if (blockIdx.x == 0 && tid == 0) a.verdict[s] = v;
+  const AcceptOutcome v = settle(a, heat, s, d0, k, tid, blockIdx.x == 0);
+  if (blockIdx.x == 0 && tid == 0) a.outcome[s] = v;
   if (v.kept == k) return;  // the sums of the first launch do
   const Decision w = decide(a, v, s, d0, k);
   for (int piece = blockIdx.x * a.each, end = min(piece + a.each, a.pieces); piece < end; ++piece) {
@@ -491,9 +491,9 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_draw_kernel(AcceptArgs 
   double early = 0.0;  // the sum of the thread's piece, if pieces it will be
   if (!ALONE && tid < a.pieces) early = a.rest[(size_t)s * a.pieces + tid];
   const Heat heat(a, s);
-  AcceptVerdict v;
-  if constexpr (ALONE) v = judge(a, heat, s, d0, k, tid, false);
-  else v = a.verdict[s];
+  AcceptOutcome v;
+  if constexpr (ALONE) v = settle(a, heat, s, d0, k, tid, false);
+  else v = a.outcome[s];
   const int kept = __builtin_amdgcn_readfirstlane(v.kept);
   v.kept = kept;
   v.x = __builtin_amdgcn_readfirstlane(v.x);
@@ -553,7 +553,7 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_draw_kernel(AcceptArgs 
 
 // Where the parts of the workspace lie; 0 bytes for arguments that are refused
 struct AcceptPlan {
-  int64_t drafts = 0, rest = 0, verdict = 0, bytes = 0;
+  int64_t drafts = 0, rest = 0, outcome = 0, bytes = 0;
   int most = 0, chunks = 0, pieces = 0;
 };
 static int plan_accept(int n_seqs, const int32_t* h_k, int vocab, AcceptPlan* out) {
@@ -569,8 +569,8 @@ static int plan_accept(int n_seqs, const int32_t* h_k, int vocab, AcceptPlan* ou
   p.pieces = (vocab + kAcceptPiece - 1) / kAcceptPiece;
   auto up256 = [](int64_t b) { return (b + 255) / 256 * 256; };
   p.rest = up256((2 * p.drafts + n_seqs) * p.chunks * (int64_t)sizeof(AcceptPart));
-  p.verdict = p.rest + up256((int64_t)n_seqs * p.pieces * 8);
-  p.bytes = p.verdict + up256((int64_t)n_seqs * (int64_t)sizeof(AcceptVerdict));
+  p.outcome = p.rest + up256((int64_t)n_seqs * p.pieces * 8);
+  p.bytes = p.outcome + up256((int64_t)n_seqs * (int64_t)sizeof(AcceptOutcome));
   *out = p;
   return CAS_OK;
 }
@@ -603,7 +603,7 @@ int cas_accept_tokens(cas_ctx* ctx, int n_seqs, const int32_t* h_k, int vocab, c
   char* ws = (char*)ctx->d_ws;
   a.part = (cas::AcceptPart*)ws;
   a.rest = (double*)(ws + plan.rest);
-  a.verdict = (cas::AcceptVerdict*)(ws + plan.verdict);
+  a.outcome = (cas::AcceptOutcome*)(ws + plan.outcome);
   a.vocab = vocab; a.chunks = plan.chunks; a.pieces = plan.pieces; a.rows = (int)plan.drafts + n_seqs;
   for (int i = 0; i < n_seqs; ++i) a.before[i + 1] = a.before[i] + h_k[i];
   const int cols = plan.most + 1 + (a.draft ? plan.most : 0);
