@@ -13,9 +13,9 @@
 //             sums of max(0, p - q) over its pieces of the vocabulary.  Left out where there are no drafts
 //   launch 3, a workgroup per sequence: looks up the piece (or the chunk of launch 1, where all drafts are kept), then the token
 //
-// Measured (us; in brackets the bytes of the logits at the rate of a copy): 32 sequences of up to 7 drafts over 128256 tokens 53 (32.2): launch 1 34, its
-// vector issue, 24 operations a value, 98 % of the cycles, at the rate of memory; launch 2 13.5 (row joins, then two exponentials a value of one row pair); launch 3
-// 5.  64 draws over 128256 17.1 (6.4): 10.5 and 6.6.  One sequence of 4 drafts over 32000 13.5 (0.2): three launches of dependent round trips.
+// Measured (us; in brackets the bytes of the logits at the rate of a copy): 32 sequences of up to 7 drafts over 128256 tokens 53 (32.2): launch 1 34, at the
+// rate of memory, its vector issue, 22 operations a value, in 91 % of the cycles; launch 2 13.5 (row joins, then two exponentials a value of one row pair); launch 3
+// 5.  64 draws over 128256 17 (6.4): 10.5 and 6.6.  One sequence of 4 drafts over 32000 13.4 (0.2): three launches of dependent round trips.
 #include <algorithm>
 #include "cas_device.hpp"
 #include "cas_internal.hpp"
@@ -192,7 +192,7 @@ struct RowPart {
 
 __global__ __launch_bounds__(kAcceptThreads) void accept_rows_kernel(AcceptArgs a) {
   __shared__ float tops[kAcceptWaves];
-  __shared__ double sums[kAcceptWaves];
+  __shared__ double sums[kAcceptThreads];
   __shared__ int firsts[kAcceptWaves];
   const int chunk = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, wv = tid >> 6;
   const int d0 = a.before[s], k = a.before[s + 1] - d0;
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_rows_kernel(AcceptArgs 
 #pragma unroll
     for (int j = 0; j < 4; ++j) row.cut(4 * (tid + kAcceptThreads * j), z[j]);
   }
-  // a wave's own maximum and sum; the four are joined below
+  // a wave's own maximum, and sums of its lanes under it; they are joined below
   float m = -INFINITY;
 #pragma unroll
   for (int j = 0; j < 16; ++j) m = fmaxf(m, z[j >> 2][j & 3]);
@@ -220,7 +220,6 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_rows_kernel(AcceptArgs 
   int first = 0x7FFFFFFF;
   if (m > -INFINITY) {
     if (heat.greedy) {
-      sum = 1.0;
 #pragma unroll
       for (int j = 0; j < 16; ++j)
         if (z[j >> 2][j & 3] == m) first = min(first, chunk * kAcceptChunk + 4 * (tid + kAcceptThreads * (j >> 2)) + (j & 3));
@@ -232,32 +231,33 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_rows_kernel(AcceptArgs 
         weights(z[j], m, heat.inv, w);
         sum += (w[0] + w[1]) + (w[2] + w[3]);
       }
-      sum = lane_of(wave_upto64(sum), 63);
     }
   }
+  sums[tid] = sum;
   if ((tid & 63) == 0) {
     tops[wv] = m;
-    sums[wv] = sum;
     firsts[wv] = first;
   }
   __syncthreads();
-  if (tid != 0) return;
+  if (tid >= 64) return;
+  const float top[kAcceptWaves] = {tops[0], tops[1], tops[2], tops[3]};
   AcceptPart part;
-  part.max = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  part.max = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
   part.first = 0x7FFFFFFF;
   part.sum = 0.0;
   if (part.max > -INFINITY) {
+    if (heat.greedy) {
 #pragma unroll
-    for (int w = 0; w < kAcceptWaves; ++w) {
-      if (heat.greedy) {
-        if (tops[w] == part.max) part.first = min(part.first, firsts[w]);
-      } else {
-        part.sum += sums[w] * weight(tops[w], part.max, heat.inv);
-      }
+      for (int w = 0; w < kAcceptWaves; ++w)
+        if (top[w] == part.max) part.first = min(part.first, firsts[w]);
+      part.sum = 1.0;
+    } else {  // one wave adds the lanes up for all four: 64-bit sums over lanes are as many operations as three values' exponentials
+      double w[kAcceptWaves];
+      weights(top, part.max, heat.inv, w);
+      part.sum = lane_of(wave_upto64((sums[tid] * w[0] + sums[64 + tid] * w[1]) + (sums[128 + tid] * w[2] + sums[192 + tid] * w[3])), 63);
     }
-    if (heat.greedy) part.sum = 1.0;
   }
-  a.part[(size_t)(of_target ? d0 + s + col : a.rows + d0 + col) * a.chunks + chunk] = part;
+  if (tid == 0) a.part[(size_t)(of_target ? d0 + s + col : a.rows + d0 + col) * a.chunks + chunk] = part;
 }
 
 // Joins the chunks of a row: 16 lanes l, in a fixed order.  The last of them has the result.
