@@ -511,7 +511,10 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_draw_kernel(AcceptArgs 
       const AcceptPart p = part[c];
       if (p.max == -INFINITY) return 0.0;
       if (heat.greedy) return p.max == w.t.max && p.first == w.t.first ? 1.0 : 0.0;
-      return p.sum * weight(p.max, w.t.max, heat.inv) * w.t.scale;
+      // Drawn only where a token of it has a weight, as token_at forms it: thousands of tokens may add up to a smallest number that
+      // each of them is below
+      const double most = weight(p.max, w.t.max, heat.inv) * w.t.scale;
+      return most > 0.0 ? p.sum * most : 0.0;
     };
     double own = pieces ? early : sum_of(tid);
     Found f = threads_before(own, sums, lane, wv);

@@ -163,6 +163,29 @@ def test_numbers_at_the_ends(env):
         _check(torch, B, ctx, target, near, tokens, ks, x.view(-1), temp, (vocab, "equal"))
 
 
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("vocab", [8192, 12289])
+def test_a_chunk_whose_tokens_are_all_below_the_smallest_number_is_not_drawn(env, vocab, where):
+    """4096 tokens 740 below the others: exp(-740) / n is 0 in 64 bits (the smallest number is exp(-744.4)), 4096 times that
+    is not.  The definition gives them no weight, whatever the number; 735 below they have one."""
+    torch, B, ctx = env
+    low = {"first": slice(0, 4096), "middle": slice(4096, 8192), "last": slice(vocab - (vocab % 4096 or 4096), vocab)}[where]
+    for below, t in ((740.0, 1.0), (7.4, 0.01), (735.0, 1.0)):  # numbers away from the steps of the sums by more than their roundings
+        row = torch.zeros(vocab, device="cuda")
+        row[low] = -below
+        temp = torch.full((6,), t, device="cuda")
+        for u in (0.0, 0.3, 1.0 - 2.0 ** -40, 1.0):
+            r = torch.tensor([u] * 6, dtype=torch.float64, device="cuda")
+            z = row.expand(6, -1).contiguous()
+            none = torch.empty(0, dtype=torch.int32, device="cuda")
+            _check(torch, B, ctx, z, None, none, [0] * 6, r, temp, (vocab, where, below, u, "no drafts"))
+            # a draft that is kept, and one that is not where nothing is left of p - q
+            tokens = torch.full((3,), 8191 if where == "first" else 0, dtype=torch.int32, device="cuda")
+            for v in (0.0, 1.5):
+                r = torch.tensor([v, u] * 3, dtype=torch.float64, device="cuda")
+                _check(torch, B, ctx, z, z[:3], tokens, [1] * 3, r, temp[:3], (vocab, where, below, u, v))
+
+
 def test_drafted_tokens_outside_the_vocabulary_are_not_kept(env):
     torch, B, ctx = env
     target, near, tokens, r, temp = _case(torch, 301, [3] * 6, True, 3)
