@@ -319,7 +319,8 @@ int cas_kv_destroy(cas_kv* kv);
  * layer appends at the same positions, then cas_kv_set_len publishes them. */
 int cas_kv_append(cas_ctx* ctx, cas_kv* kv, int layer, int seq, const uint16_t* d_K,
                   const uint16_t* d_V, int n_tok);
-/* Host only: committed length of a sequence (set: also used to roll back). */
+/* Host only: committed length of a sequence (set: also used to roll back).  A sequence has room for the positions of its
+ * pages, and for no more than 2^31 - 256 of them: CAS_ENOMEM beyond, here and from the calls that add positions. */
 int cas_kv_set_len(cas_kv* kv, int seq, int32_t len);
 int cas_kv_len(const cas_kv* kv, int seq, int32_t* len);
 

@@ -266,8 +266,8 @@ static int launch_attention_group(cas_ctx* ctx, cas_kv* kv, const AttnCall* call
     const int R = c.ncols * a.grp;
     const int MT = (R + 15) / 16;
     if (MT < 1 || MT > (c.full ? 5 : 3) || c.n_new > kPT || c.n_new < c.ncols || c.ncols > kMaxCols) return CAS_EINVAL;
+    if ((int64_t)q.len + q.n_new > kv_room(kv)) return CAS_ENOMEM;
     const int pages = (q.len + q.n_new + kPT - 1) / kPT;
-    if (pages > g.max_pages_per_seq) return CAS_ENOMEM;
     q.nsplit = (pages + kPagesPerSplit - 1) / kPagesPerSplit;
     const size_t need = sizeof(float) * (size_t)q.nsplit * g.n_kv_heads * R * kPartStride;
     if (!ws || *ws_used + need > ws_bytes) return CAS_ENOMEM;
@@ -329,7 +329,7 @@ int launch_attention_runs(cas_ctx* ctx, cas_kv* kv, const AttnCall& c, int run, 
   run = std::min(run, c.ncols);
   const int max_r = run * a.grp;
   if (run < 1 || run > kPT || !c.full || c.qkv || max_r > (g.mx ? 80 : 64) || c.len < 0) return CAS_EINVAL;
-  if ((c.len + c.ncols + kPT - 1) / kPT > g.max_pages_per_seq) return CAS_ENOMEM;
+  if ((int64_t)c.len + c.ncols > kv_room(kv)) return CAS_ENOMEM;
   const size_t page_bytes = sizeof(float) * (size_t)c.n_q_heads * run * kPartStride;
   b.run_cols = run;
   a.part = (float*)ws;

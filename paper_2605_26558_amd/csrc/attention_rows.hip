@@ -352,9 +352,8 @@ static int plan_rows(const cas_kv* kv, int n_seqs, const int32_t* seqs, int pref
     if (ncols[i] < 1 || ncols[i] > 16 || n_new[i] < ncols[i] || n_new[i] > 64) return CAS_EINVAL;
     a.seq[i] = seqs[i]; a.len[i] = kv->h_len[seqs[i]]; a.ncols[i] = ncols[i]; a.n_new[i] = n_new[i];
     if (prefix_len > a.len[i]) return CAS_EINVAL;
-    const int64_t pages_i = ((int64_t)a.len[i] + a.n_new[i] + 63) / 64;
-    if (pages_i > g.max_pages_per_seq) return CAS_ENOMEM;
-    pages[i] = (int)pages_i;
+    if ((int64_t)a.len[i] + a.n_new[i] > kv_room(kv)) return CAS_ENOMEM;
+    pages[i] = (a.len[i] + a.n_new[i] + 63) / 64;
     if (window) pages[i] -= WindowPages(a.n_first, a.window, a.len[i], a.len[i] + a.n_new[i], a.ncols[i]).skip;
     a.row0[i] = (int)rows;
     rows += ncols[i] * a.grp;

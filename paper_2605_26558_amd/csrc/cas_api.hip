@@ -223,14 +223,13 @@ int cas_kv_append(cas_ctx* ctx, cas_kv* kv, int layer, int seq, const uint16_t* 
   if (!ctx || n_tok < 0 || check_seq(kv, layer, seq) != CAS_OK) return CAS_EINVAL;
   if (n_tok == 0) return CAS_OK;
   if (!d_K || !d_V) return CAS_EINVAL;
-  const int64_t cap = (int64_t)kv->desc.max_pages_per_seq * kv->desc.page_tokens;
-  if ((int64_t)kv->h_len[seq] + n_tok > cap) return CAS_ENOMEM;
+  if ((int64_t)kv->h_len[seq] + n_tok > cas::kv_room(kv)) return CAS_ENOMEM;
   return cas::launch_kv_append(ctx, kv, layer, seq, d_K, d_V, n_tok, kv->h_len[seq]);
 }
 
 int cas_kv_set_len(cas_kv* kv, int seq, int32_t len) {
   if (check_seq(kv, 0, seq) != CAS_OK || len < 0) return CAS_EINVAL;
-  if ((int64_t)len > (int64_t)kv->desc.max_pages_per_seq * kv->desc.page_tokens) return CAS_ENOMEM;
+  if (len > cas::kv_room(kv)) return CAS_ENOMEM;
   kv->h_len[seq] = len;
   return CAS_OK;
 }
@@ -246,7 +245,7 @@ int cas_kv_read(cas_ctx* ctx, cas_kv* kv, int layer, int seq, int pos0, int n_to
   if (!ctx || n_tok < 0 || pos0 < 0 || check_seq(kv, layer, seq) != CAS_OK) return CAS_EINVAL;
   if (n_tok == 0) return CAS_OK;
   if (!d_K || !d_V) return CAS_EINVAL;
-  if ((int64_t)pos0 + n_tok > (int64_t)kv->desc.max_pages_per_seq * kv->desc.page_tokens) return CAS_EINVAL;
+  if ((int64_t)pos0 + n_tok > cas::kv_room(kv)) return CAS_EINVAL;
   return cas::launch_kv_read(ctx, kv, layer, seq, pos0, n_tok, full, d_K, d_V);
 }
 

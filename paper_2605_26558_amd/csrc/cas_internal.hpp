@@ -4,6 +4,7 @@
 #include <stdint.h>
 #include "../../include/cassandra.h"
 
+#include <algorithm>
 #include <atomic>
 #include <vector>
 
@@ -56,6 +57,12 @@ struct cas_kv {
 };
 
 namespace cas {
+// Positions that a sequence has room for: those of its pages, and so few that a length stays below 2^31 with what calls add to it,
+// to round it up (to 256 at the most) or to ask a step past its end
+inline int64_t kv_room(const cas_kv* kv) {
+  return std::min<int64_t>((int64_t)kv->desc.max_pages_per_seq * kv->desc.page_tokens, 0x7FFFFF00);
+}
+
 // Kernels that ask for more than 48 KB of dynamic LDS must be allowed to, once per device and
 // kernel; one LdsLimit (a function-local static at the launch site) remembers what has been
 // granted.  Two threads racing here both make the call, which is harmless.

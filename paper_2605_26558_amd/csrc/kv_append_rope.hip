@@ -400,7 +400,7 @@ extern "C" int cas_kv_append_rope(cas_ctx* ctx, cas_kv* kv, int layer, int n_seq
     for (int j = 0; j < i; ++j)
       if (h_seqs[j] == h_seqs[i]) return CAS_EINVAL;
     a.seq[i] = h_seqs[i]; a.len[i] = kv->h_len[h_seqs[i]]; a.n[i] = h_n_tok[i];
-    if ((int64_t)a.len[i] + a.n[i] > (int64_t)kv->desc.max_pages_per_seq * kv->desc.page_tokens) return CAS_ENOMEM;
+    if ((int64_t)a.len[i] + a.n[i] > cas::kv_room(kv)) return CAS_ENOMEM;
     a.tok0[i] = (int)n_tok;
     n_tok += h_n_tok[i];
     if (n_tok >= 1 << 24) return CAS_ENOTSUP;

@@ -499,9 +499,8 @@ static size_t chunk_partials(const cas_model_cfg& c, int sub, int end) {  // of 
 // rotary table within the prompt (those passes report it where it happens).
 static int chunk_columns(const cas_ctx* ctx, const cas_model* m, const cas_kv* kv, int seq, int left) {
   const cas_model_cfg& c = m->cfg;
-  const int64_t cap = (int64_t)kv->desc.max_pages_per_seq * kv->desc.page_tokens;
   const int64_t len = kv->h_len[seq];
-  if (left < kPrefillMin || len + left > cap || len + left > c.max_pos || !ctx->d_ws) return 0;
+  if (left < kPrefillMin || len + left > kv_room(kv) || len + left > c.max_pos || !ctx->d_ws) return 0;
   const int qd = c.n_q_heads * c.head_dim, kvd = c.n_kv_heads * c.head_dim;
   if (!gemm_wide_ok(ctx, qd + 2 * kvd, c.hidden) || !gemm_wide_ok(ctx, c.hidden, qd) || !gemm_wide_ok(ctx, c.hidden, c.ffn))
     return 0;
@@ -769,8 +768,7 @@ int cas_commit(cas_ctx* ctx, cas_model* m, cas_kv* kv, int seq, int n_accepted) 
   if (check_step(ctx, m, kv, seq) != CAS_OK || n_accepted < 0 || n_accepted + 1 > m->cfg.max_cols) return CAS_EINVAL;
   const cas_model_cfg& c = m->cfg;
   const int kvd = c.n_kv_heads * c.head_dim, n = n_accepted + 1;
-  const int64_t cap = (int64_t)kv->desc.max_pages_per_seq * kv->desc.page_tokens;
-  if ((int64_t)kv->h_len[seq] + n > cap) return CAS_ENOMEM;
+  if ((int64_t)kv->h_len[seq] + n > cas::kv_room(kv)) return CAS_ENOMEM;
   // all layers in one launch: the slots of a sequence are [layer][max_cols][kv heads * 128]
   const size_t slots = (size_t)seq * c.n_layers * c.max_cols * kvd;
   int rc = cas::launch_kv_append_layers(ctx, kv, 0, c.n_layers, (size_t)c.max_cols * kvd, seq, m->knew + slots,

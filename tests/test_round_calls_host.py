@@ -52,6 +52,34 @@ def test_workspace_of_a_window_goes_by_what_is_seen():
     B._lib().cas_kv_destroy(kv.h)
 
 
+def test_lengths_stay_below_32_bits():
+    """A page table that would reach past 2^31 positions: no call takes a length whose sums with what it adds would not fit."""
+    from paper_2605_26558_amd import binding as B
+    lib, room = B._lib(), 2 ** 31 - 256
+    kv = _kv(B, per_seq=1 << 27)
+    for length in (2 ** 31 - 1, 2 ** 31 - 64, room + 1):
+        assert lib.cas_kv_set_len(kv.h, 0, length) == B.CAS_ENOMEM, length
+    ctx, data = C.create_string_buffer(4096), 4096   # looked at before a launch only, which no call here reaches
+    one = lambda *v: (C.c_int32 * len(v))(*v)  # noqa: E731
+    part = C.byref(B.cas_rope_part(data, data, 256, 256, 2, 0, 0, 0))
+    append = lambda seq, n, n_pos=0: lib.cas_kv_append_rope(ctx, kv.h, 0, 1, one(seq), one(n), data, n_pos, 64, 0, None, None, part, part)  # noqa: E731
+    ptr = (C.c_void_p * 1)(data)
+    window = lambda new: lib.cas_attention_window(ctx, kv.h, 0, 1, one(0), 0, 8, 1, ptr, one(1), 2, ptr, ptr, one(new), ptr)  # noqa: E731
+    for short in (0, 1, 63):
+        assert lib.cas_kv_set_len(kv.h, 0, room - short) == B.CAS_OK
+        assert B.cas_attention_window_bytes(kv, [0], 4, 100, [1], 8, [short + 1]) == 0 and window(short + 1) == B.CAS_ENOMEM
+        assert B.cas_attention_shared_bytes(kv, [0], 0, [1], 8, [short + 1]) == 0
+        assert append(0, short + 1) == append(0, 2 ** 31 - 1) == B.CAS_ENOMEM
+        assert lib.cas_kv_append(ctx, kv.h, 0, 0, data, data, short + 1) == lib.cas_kv_append(ctx, kv.h, 0, 0, data, data, 2 ** 31 - 1) == B.CAS_ENOMEM
+        assert lib.cas_kv_read(ctx, kv.h, 0, 0, room - short, short + 1, 1, data, data) == B.CAS_EINVAL
+        if short:  # what fits: as much workspace as at any other length, and no refusal
+            assert append(0, short) == B.CAS_OK
+            here = B.cas_attention_window_bytes(kv, [0], 4, 100, [1], 8, [short])
+            B.cas_kv_set_len(kv, 1, (room - short) % 64 + 6400)
+            assert here == B.cas_attention_window_bytes(kv, [1], 4, 100, [1], 8, [short]) > 0
+    lib.cas_kv_destroy(kv.h)
+
+
 @pytest.fixture
 def wrappers(monkeypatch):
     """The binding with tensors that say they are on the GPU and a context that is none: a call whose arguments the wrapper takes
