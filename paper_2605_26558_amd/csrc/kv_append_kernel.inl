@@ -170,15 +170,18 @@ __device__ __forceinline__ void format_four(const KvGeom& g, uint32_t* spec_pool
     if (16 * k < g.pw) vp[k] = st.pruned[64 * k + lane];
   }
   auto flush = [&](uint32_t v, uint32_t* to, int words, int i) {
-    if (keep(i, words)) to[row * words + i] = v;
+    if (keep(i, words)) to[i] = v;
   };
-  flush(vb, ts, 4, lane);
-  if constexpr (MX) flush(ve, ts + 256, 1, lane);
+  uint32_t* const spec = ts + g.spec_off + row * g.sw;
+  uint32_t* const lo = tv + row * g.lw;
+  uint32_t* const pruned = tv + 64 * g.lw + row * g.pw;
+  flush(vb, ts + row * 4, 4, lane);
+  if constexpr (MX) flush(ve, ts + 256 + row, 1, lane);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    if (16 * k < g.sw) flush(vs[k], ts + g.spec_off, g.sw, 64 * k + lane);
-    if (k < 2 && 16 * k < g.lw) flush(vl[k & 1], tv, g.lw, 64 * k + lane);
-    if (16 * k < g.pw) flush(vp[k], tv + 64 * g.lw, g.pw, 64 * k + lane);
+    if (16 * k < g.sw) flush(vs[k], spec, g.sw, 64 * k + lane);
+    if (k < 2 && 16 * k < g.lw) flush(vl[k & 1], lo, g.lw, 64 * k + lane);
+    if (16 * k < g.pw) flush(vp[k], pruned, g.pw, 64 * k + lane);
   }
 }
 
