@@ -122,15 +122,17 @@ int launch_kv_append_layers(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, 
     return CAS_OK;
   }
   const int groups = (pos0 + n_tok - 1) / kAppendRows - pos0 / kAppendRows + 1, fours = (pos0 + n_tok - 1) / 4 - pos0 / 4 + 1;
-  // Of sixteen from 36 vectors per CU on (72 over shared exponents).  us, four / sixteen: 512 tokens of 8 heads 5.06 / 5.32, 640 5.93 / 5.45,
-  // 1021 7.1 / 6.6, 4096 19.0 / 11.8; over shared exponents 768 6.5 / 7.1, 1021 7.7 / 7.8, 1500 10.0 / 9.4, 4096 21.5 / 15.1.
+  // Of sixteen from 48 vectors per CU on (80 over shared exponents), from 36 where the first row is the first of sixteen (others are written
+  // row by row).  us, four / sixteen, 8 heads, from such a row and from others: 512 tokens 5.4 / 5.6 and 6.1 / 6.6, 576 6.2 / 5.6 and 6.2 / 6.6, 736
+  // 6.3 / 5.8 and 6.3 / 6.7, 768 6.3 / 5.8 and 7.1 / 6.7, 1021 7.6 / 7.4 and 8.3 / 8.1, 4096 18.6 / 11.8 and 19.2 / 13.2; over shared exponents 1152 9.1 / 9.0
+  // and 9.0 / 9.6, 1300 10.1 / 9.5 and 10.1 / 9.7, 4096 21.5 / 15.2 and 22.4 / 17.2.
   // And only where its waves are filled well enough: a commit is a few rows of many layers.  A wave of sixteen takes as long as some 1.7 of four (2 over
   // shared exponents), and a single group is one wave of its workgroup.  126 layers of 8 heads, waves of four / groups of sixteen that the
   // tokens touch: 1 / 1 5.8 / 8.3, 2 / 1 7.5 / 8.7, 2 / 2 9.1 / 11.2, 3 / 2 12.2 / 11.2, 5 / 2 18.0 / 12.0, whole groups 11.2 / 7.9; 48 layers of 32 heads
   // 8.0 / 13.1, 11.0 / 13.6, 12.0 / 17.5, 16.9 / 17.6, 24.9 / 18.6, 15.1 / 11.8, over shared exponents 8.6 / 16.8, 12.3 / 16.9, 13.2 / 23.6,
   // 19.9 / 23.7, 29.6 / 24.7, 17.3 / 15.8; three fours in one group 9.4 / 8.9, 13.1 / 14.0 and 14.9 / 17.3
   const bool filled = groups > 1 ? 2 * fours >= 5 * groups : n_tok == kAppendRows;
-  const bool many = filled && (int64_t)n_tok * g.n_kv_heads * 2 * n_layers >= (int64_t)(g.mx ? 72 : 36) * ctx->num_cu;
+  const bool many = filled && (int64_t)n_tok * g.n_kv_heads * 2 * n_layers >= (int64_t)(g.mx ? 80 : pos0 % kAppendRows ? 48 : 36) * ctx->num_cu;
   const dim3 grid(many ? (groups + kAppendWaves - 1) / kAppendWaves : groups, g.n_kv_heads, 2 * n_layers);
 #define CAS_LAUNCH(TV)                                                                                              \
   case TV:                                                                                                          \
