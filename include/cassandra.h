@@ -455,7 +455,8 @@ int cas_rope(cas_ctx* ctx, const float* d_table, int n_pos, int rot, int layout,
  * h_q: NULL or the part of the queries, as for cas_rope.  d_table, n_pos, rot (2..128) and layout as for cas_rope.  d_pos: int32, the
  * rotary position of each token, or NULL for its place in the cache.  A token whose rotary position is outside 0 .. n_pos-1 is
  * padding: nothing is written for it, its place in the cache keeps what it holds.
- * Bits are those of cas_rope followed by cas_kv_append; alignment, aliasing and limits as for cas_rope, page table entries outside the
+ * Bits are those of cas_rope followed by cas_kv_append (infinities and NaN included; where both products of a turned channel
+ * are NaN, either may come out); alignment, aliasing and limits as for cas_rope, page table entries outside the
  * pool as for cas_kv_append.  No length changes: cas_kv_set_len once all layers are done.  CAS_ENOMEM where a sequence has no room for its
  * tokens.  CAS_EINVAL unless the context's device is current. */
 int cas_kv_append_rope(cas_ctx* ctx, cas_kv* kv, int layer, int n_seqs, const int32_t* h_seqs, const int32_t* h_n_tok,

@@ -266,16 +266,29 @@ __device__ __forceinline__ int quad_before(int v, int j) {  // of the lanes befo
 }
 
 // The wave's vectors: columns 32 j + i and 32 j + 16 + i of vector lane / 4 in the halves of w[i], j = lane & 3.  They become rows row0 ..
-// row0 + 15 of the tile of (layer, page, K or V, head), those whose bit of `rows` is set.
+// row0 + 15 of the tile of (layer, page, K or V, head), those whose bit of `rows` is set.  quiet: NaN are made quiet.
 template <int T, bool MX>
-__device__ __forceinline__ void format_rows(const KvGeom& g, uint32_t* spec_pool, uint32_t* verif_pool, RowsStage& st, const uint32_t (&w)[16],
-                                            int lane, int layer, int page, int kv, int head, int row0, uint32_t rows) {
+__device__ __forceinline__ void format_rows(const KvGeom& g, uint32_t* spec_pool, uint32_t* verif_pool, RowsStage& st, uint32_t (&w)[16],
+                                            int lane, int layer, int page, int kv, int head, int row0, uint32_t rows, bool quiet = false) {
   constexpr int FW = MX ? 9 - T : 16 - T;
   const int r = lane >> 2, j = lane & 3;
   uint32_t plane[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) plane[i] = w[i];
   bit_planes(plane);
+  if (quiet) {
+    uint32_t nan = 0xFFFFFFFFu, low = 0u;
+#pragma unroll
+    for (int bit = 7; bit < 15; ++bit) nan &= plane[bit];
+#pragma unroll
+    for (int bit = 0; bit < 6; ++bit) low |= plane[bit];
+    nan &= low;
+    if (__builtin_amdgcn_ballot_w64(nan != 0u)) {
+      plane[6] |= nan;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] |= (nan >> i & 0x00010001u) << 6;
+    }
+  }
   // columns as large as the K-th in the bits so far, larger ones, and how many of the former are still to be taken
   uint32_t alive = 0xFFFFFFFFu, kept = 0;
   int spare = g.K - 1;  // to be taken but for one: below 0 where that is none

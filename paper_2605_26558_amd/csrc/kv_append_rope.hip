@@ -4,7 +4,8 @@
 //
 //   y_a = x_a cos - x_b sin,  y_b = x_b cos + x_a sin      (fp32, an operation at a time, rounded to bf16 once)
 //
-// Every operation is the one that cas_rope does, so the bits are those of cas_rope followed by cas_kv_append.
+// Every operation is the one that cas_rope does, so the bits are those of cas_rope followed by cas_kv_append, infinities and NaN
+// included, unless both products of a sum are NaN: which of two an addition passes on goes by the order of its operands, the compiler's choice.
 //
 // What has to move: the projections once, the dense queries and the encoded vectors once.  Measured (60 % kept, t = 4; us; in brackets these bytes at the rate
 // of a copy): 3 tokens of 48 heads 4.1 (0.02) and 101 of 80 heads in 32 sequences 6.6 (1.3), the launch and three round trips (arguments,
@@ -64,6 +65,11 @@ struct Pairing {
   }
 };
 
+// x + p, or x - p for minus = the sign bit (the first of a pair).  The sign goes to the product, as a subtraction's does, and not to
+// one of its factors: of a NaN the factor, or infinity times 0, it would come out otherwise.
+__device__ __forceinline__ float plus(float x, float p, uint32_t minus) { return x + __uint_as_float(__float_as_uint(p) ^ minus); }
+constexpr uint32_t kMinus = 0x80000000u;
+
 // A wave per vector: lane l has channels l and l + 64.  For few tokens, where the time of one wave from end to end counts.
 __global__ __launch_bounds__(64 * kAppendWaves) void rope_append_few_kernel(RopeAppendArgs a) {
   __shared__ uint32_t stages[kAppendWaves][3 * 64 + 8];  // as in kv_append_few_kernel
@@ -91,7 +97,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void rope_append_few_kernel(Rope
   if (turn) {
     const float2* cs = reinterpret_cast<const float2*>(a.angles) + (size_t)p * a.half;
     const float2 c0 = cs[p0.pair], c1 = cs[p1.pair];
-    const float y0 = x0 * c0.x + o0 * (p0.first ? -c0.y : c0.y), y1 = x1 * c1.x + o1 * (p1.first ? -c1.y : c1.y);
+    const float y0 = plus(x0 * c0.x, o0 * c0.y, p0.first ? kMinus : 0u), y1 = plus(x1 * c1.x, o1 * c1.y, p1.first ? kMinus : 0u);
     x0 = p0.turns ? y0 : x0;
     x1 = p1.turns ? y1 : x1;
   }
@@ -129,6 +135,12 @@ __device__ __forceinline__ void request(uint64_t row, int c, bool fp32, uint32_t
 }
 __device__ __forceinline__ float low_value(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_value(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// bf16 values that do not turn, as the conversion leaves them that turned and fp32 values go through: a NaN quiet
+__device__ __forceinline__ void quiet(uint32_t (&w)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = two_bf16(low_value(w[i]), high_value(w[i]));
+}
 
 // How the partners of eight channels from a multiple of eight on are reached: half a vector away, in the same words, eight that follow one
 // another, or one by one
@@ -175,31 +187,31 @@ struct EightAngles {
       }
     }
   }
-  // w: channels c0 .. c0 + 7, two to a word; o: their partners; SECOND: of the second half (HOW = kHalfAway)
-  template <bool SECOND = false>
-  __device__ __forceinline__ void turn(const RopeAppendArgs& a, int c0, const uint32_t (&o)[4], uint32_t (&w)[4]) const {
+  // w: channels c0 .. c0 + 7, two to a word; o: their partners; first: whether they are the first of their pairs (HOW = kHalfAway)
+  __device__ __forceinline__ void turn(const RopeAppendArgs& a, int c0, const uint32_t (&o)[4], uint32_t (&w)[4], bool first = false) const {
     const Pairing all(c0, a.half, false);  // eight channels that follow one another are alike but for kSingles
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint32_t x = o[i];  // y_a = x_a cos + (-x_b) sin
+      uint32_t minus0, minus1;
       bool turns = true;
       if constexpr (HOW == kHalfAway) {
-        x ^= SECOND ? 0u : 0x80008000u;
+        minus0 = minus1 = first ? kMinus : 0u;
       } else if constexpr (HOW == kNeighbours) {
-        x ^= 0x00008000u;
+        minus0 = kMinus;
+        minus1 = 0u;
         turns = c0 + 2 * i < 2 * a.half;  // an even number of channels turns
       } else if constexpr (HOW == kEights) {
-        x ^= all.first ? 0x80008000u : 0u;
+        minus0 = minus1 = all.first ? kMinus : 0u;
         turns = all.turns;
       } else {
         const Pairing p0(c0 + 2 * i, a.half, false), p1(c0 + 2 * i + 1, a.half, false);
-        x ^= (p0.first ? 0x8000u : 0u) | (p1.first ? 0x80000000u : 0u);
+        minus0 = p0.first ? kMinus : 0u;
+        minus1 = p1.first ? kMinus : 0u;
         turns = p0.turns;
       }
-      const float y0 = low_value(w[i]) * c[2 * i] + low_value(x) * s[2 * i];
-      const float y1 = high_value(w[i]) * c[2 * i + 1] + high_value(x) * s[2 * i + 1];
-      const uint32_t y = two_bf16(y0, y1);
-      w[i] = turns ? y : w[i];
+      const float x0 = low_value(w[i]), x1 = high_value(w[i]);
+      const float y0 = plus(x0 * c[2 * i], low_value(o[i]) * s[2 * i], minus0), y1 = plus(x1 * c[2 * i + 1], high_value(o[i]) * s[2 * i + 1], minus1);
+      w[i] = two_bf16(turns ? y0 : x0, turns ? y1 : x1);
     }
   }
 };
@@ -249,7 +261,9 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
       }
     };
     if (!part.turn) {
-      heads([](uint32_t (&)[4]) {});
+      heads([&](uint32_t (&w)[4]) {
+        if (!part.fp32) quiet(w);
+      });
       return;
     }
     with_partners(a, [&](auto H) {
@@ -260,7 +274,7 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
         uint32_t o[4];
         if constexpr (how == kHalfAway) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[i], 0x128, 0xf, 0xf, true) ^ (l < 8 ? 0u : 0x80008000u);  // row_ror:8
+          for (int i = 0; i < 4; ++i) o[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[i], 0x128, 0xf, 0xf, true);  // row_ror:8
         } else {
           const VectorRow row(st, q);
           if constexpr (how >= kEights) {
@@ -270,7 +284,7 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
           partners<how>(a, 8 * l, row, w, o);
           if constexpr (how >= kEights) share();
         }
-        cs.turn(a, 8 * l, o, w);
+        cs.turn(a, 8 * l, o, w, l < 8);
       });
     });
     return;
@@ -307,8 +321,8 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
           cs.load(a, at, c0 + 32 * k);
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[i] = x[k][i];
-          cs.turn(a, c0 + 32 * k, x[k + 2], x[k]);
-          cs.template turn<true>(a, c0 + 32 * k, o, x[k + 2]);
+          cs.turn(a, c0 + 32 * k, x[k + 2], x[k], true);
+          cs.turn(a, c0 + 32 * k, o, x[k + 2], false);
           asm volatile("" ::: "memory");  // the angles of all at once do not fit the registers
         }
       } else {
@@ -330,6 +344,11 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
       }
     });
   }
+  const bool loud = !part.turn && !part.fp32;  // see quiet(); what the cache alone gets is looked through on bit planes, a third of the operations
+  if (loud && part.y) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) quiet(x[k]);
+  }
   if (part.y && (rows >> r & 1)) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -342,7 +361,7 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
     w[2 * i] = low_pair(x[i >> 2][i & 3], x[2 + (i >> 2)][i & 3]);
     w[2 * i + 1] = high_pair(x[i >> 2][i & 3], x[2 + (i >> 2)][i & 3]);
   }
-  format_rows<T, MX>(g, a.spec_pool, a.verif_pool, st, w, lane, a.layer, page, kv, head, posw & 63, rows);
+  format_rows<T, MX>(g, a.spec_pool, a.verif_pool, st, w, lane, a.layer, page, kv, head, posw & 63, rows, loud && !part.y);
 }
 
 static int launch_rope_append(cas_ctx* ctx, RopeAppendArgs& a, int n_seqs) {

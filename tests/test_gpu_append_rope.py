@@ -140,6 +140,59 @@ def test_words_are_those_of_the_two_calls(env, n_kv, n_q, lens, toks, keep, t, m
         assert torch.equal(three.spec_pool, two.spec_pool) and torch.equal(three.verif_pool, two.verif_pool), what
 
 
+@pytest.mark.parametrize("mode", [0, 2])
+@pytest.mark.parametrize("fp32", [False, True])
+@pytest.mark.parametrize("rot,layout", [(128, 0), (128, 1), (96, 0), (96, 1), (62, 0), (16, 0), (2, 0)])
+def test_special_values_turn_alike_whatever_the_call_holds(env, rot, layout, fp32, mode):
+    """Infinities, NaN of both signs, zeros, subnormal and largest numbers as partners of each other, at angles among which sin or
+    cos is 0: one call with few tokens, one with many, and the two calls they stand for.  Of two products that are both NaN
+    either may come out, and infinity times 0 is one: a NaN has finite partners here."""
+    torch, B, ctx = env
+    n_kv, n_q, n_tok = 8, 8, 480   # 18 vectors a token: from 342 (over shared exponents 456) on sixteen to a wave
+    special = [0x0000, 0x8000, 0x3F80, 0xBFC0, 0x7F80, 0xFF80, 0x7FC0, 0xFFC5, 0x7F81, 0xFFA3, 0x7F7F, 0xFF7F, 0x0001, 0x8003, 0x0080, 0x7F00]
+    nan, large = (lambda w: w & 0x7FFF > 0x7F80), (lambda w: w & 0x7FFF >= 0x7F80)
+    pairs = torch.tensor([(a, b) for a in special for b in special if not (nan(a) and large(b) or large(a) and nan(b))], dtype=torch.int32)
+    g = torch.Generator().manual_seed(rot + layout)
+    half = rot // 2
+    x = torch.randint(0, 65536, (n_tok, n_q + 2 * n_kv, 128), generator=g, dtype=torch.int32)   # channels behind rot: anything
+    a = torch.arange(half)
+    ia, ib = (a, a + half) if layout == 0 else (2 * a, 2 * a + 1)
+    p = pairs[torch.randint(0, len(pairs), (n_tok, n_q + 2 * n_kv, half), generator=g)]
+    x[..., ia], x[..., ib] = p[..., 0], p[..., 1]
+    x = x.to(torch.int16).cuda()
+    if fp32:  # with bits below bf16: numbers that round up to infinity among them, and NaN that have nothing above
+        low = torch.randint(0, 65536, x.shape, generator=g, dtype=torch.int32).cuda()
+        x = ((x.int() << 16) | low).view(torch.float32)
+        x = torch.where(torch.rand(x.shape, generator=g).cuda() < 0.5, x, (x.view(torch.int32) & -65536).view(torch.float32))
+        # an infinity with bits below is a NaN, and the largest bf16 number with enough of them rounds to infinity
+        rounded = x.bfloat16()
+        one, other = rounded[..., ia.cuda()], rounded[..., ib.cuda()]
+        both = torch.isnan(one) & ~torch.isfinite(other) | torch.isnan(other) & ~torch.isfinite(one)
+        x[..., ia.cuda()] = torch.where(both, 1.0, x[..., ia.cuda()])
+    q, k, v = x[:, :n_q], x[:, n_q:n_q + n_kv], x[:, n_q + n_kv:]
+    table = torch.rand(40, half, 2, generator=g).cuda() * 2 - 1
+    for i, cs in enumerate(((1.0, 0.0), (0.0, 1.0), (-1.0, -0.0), (-0.0, -1.0), (1.0, 1.0))):
+        table[i] = torch.tensor(cs)
+    pos = (torch.arange(n_tok, dtype=torch.int32) % 40).cuda()
+    turn = (rot != 16, True, rot != 62)
+    few, many, alone, two = _caches(torch, B, ctx, 4, n_kv, [7], [n_tok], 600, 4, mode)
+    outs = [[torch.full(y.shape, 9, dtype=torch.int16, device="cuda") for y in (q, k, v)] for _ in range(2)]
+    call = lambda kv, n, i, o: B.cas_kv_append_rope(ctx, kv, 1, [0], [n], table, k[i:i + n], v[i:i + n], q=q[i:i + n], pos=pos[i:i + n].contiguous(),  # noqa: E731
+                                                    layout=layout, turn=turn, q_out=o[0][i:i + n], k_out=o[1][i:i + n], v_out=o[2][i:i + n])
+    call(many, n_tok, 0, outs[0])
+    for i in range(0, n_tok, 48):
+        B.cas_kv_set_len(few, 0, 7 + i)
+        call(few, 48, i, outs[1])
+    want = _apart(torch, B, ctx, two, 1, [n_tok], table, q, k, v, pos, layout, turn)
+    assert bool(((want[0] & 0x7FFF) > 0x7F80).any()) and bool(((want[0] & 0x7FFF) == 0x7F80).any())
+    for kv, o, what in ((many, outs[0], "many"), (few, outs[1], "few")):
+        for y, ref, part in zip(o, want, "qkv"):
+            assert torch.equal(y, ref), (what, part)
+        assert torch.equal(kv.spec_pool, two.spec_pool) and torch.equal(kv.verif_pool, two.verif_pool), what
+    B.cas_kv_append_rope(ctx, alone, 1, [0], [n_tok], table, k, v, q=q, pos=pos, layout=layout, turn=turn)   # no dense keys and values
+    assert torch.equal(alone.spec_pool, two.spec_pool) and torch.equal(alone.verif_pool, two.verif_pool)
+
+
 @pytest.mark.parametrize("n_tok", [5, 700])
 @pytest.mark.parametrize("layout", [0, 1])
 def test_what_the_cache_holds_against_the_rotation_in_64_bits(env, n_tok, layout):
