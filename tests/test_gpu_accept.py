@@ -186,6 +186,37 @@ def test_a_chunk_whose_tokens_are_all_below_the_smallest_number_is_not_drawn(env
                 _check(torch, B, ctx, z, z[:3], tokens, [1] * 3, r, temp[:3], (vocab, where, below, u, v))
 
 
+@pytest.mark.parametrize("vocab", [1048577, (1 << 22) - 3, 1 << 22])
+def test_vocabularies_of_more_than_256_chunks(env, vocab):
+    """More chunks (4096 tokens) and pieces (2048) than a workgroup of the draw has threads: the token in the first of them, in
+    later rounds and at the very end, out of p, of p - q with known drafts, and of p behind a certain draft."""
+    torch, B, ctx = env
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    flat = torch.randn(3, vocab, generator=g, device="cuda") * 0.5
+    high = flat.clone()
+    high[:, vocab - 3000:] += 16.0      # nearly all of it in the last chunk or two
+    low = flat.clone()
+    low[:, 5:9] += 20.0
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    f64 = lambda *v: torch.tensor(v, dtype=torch.float64, device="cuda")  # noqa: E731
+    for z, what in ((flat, "flat"), (high, "high"), (low, "low")):
+        for us in ((0.0, 0.2503, 1.0 - 2.0 ** -30), (0.51, 0.7507, 0.99)):
+            _check(torch, B, ctx, z, None, none, [0, 0, 0], f64(*us), None, (vocab, what, us, "draw"))
+        for u in (0.0, 0.3001, 0.6002, 0.9995):
+            tokens = torch.tensor([vocab - 2], dtype=torch.int32, device="cuda")
+            near = torch.randn(1, vocab, generator=g, device="cuda") * 0.5
+            for r in (1.0, 0.0):   # dropped (r above p / q unless the target is much the surer), kept
+                _check(torch, B, ctx, z[:2], near, tokens, [1], f64(r, u), None, (vocab, what, u, r, "known"))
+                _check(torch, B, ctx, z[:2], None, tokens, [1], f64(r, u), None, (vocab, what, u, r, "certain"))
+    # greedy: the first of the largest, in a late chunk
+    flat[0, vocab - 5] = flat[0, vocab - 2] = 60.0
+    flat[1, 1048576 - 1] = 70.0
+    for r in (1.0, 0.0):
+        tokens = torch.tensor([vocab - 5], dtype=torch.int32, device="cuda")
+        _check(torch, B, ctx, flat[:2], None, tokens, [1], f64(r, 0.5), torch.zeros(1, device="cuda"), (vocab, "greedy", r))
+    _check(torch, B, ctx, flat, None, none, [0, 0, 0], f64(0.1, 0.5, 0.9), torch.zeros(3, device="cuda"), (vocab, "greedy draw"))
+
+
 def test_drafted_tokens_outside_the_vocabulary_are_not_kept(env):
     torch, B, ctx = env
     target, near, tokens, r, temp = _case(torch, 301, [3] * 6, True, 3)

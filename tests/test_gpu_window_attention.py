@@ -204,6 +204,47 @@ def test_what_a_column_does_not_see_does_not_reach_it(env, full, mode):
 
 
 @pytest.mark.parametrize("full,mode", [(True, 0), (False, 0), (True, 2), (False, 2)])
+@pytest.mark.parametrize("grp", [1, 4, 8, 16, 48])
+def test_edges_of_windows_in_every_kind_of_workgroup(env, grp, full, mode):
+    """2, 4, 8 and 16 tiles of rows, and several workgroups for the rows of a sequence (48): infinities and NaN among the positions
+    that only some of sixteen columns see, in one page, over the border of two, in the last pages and far from them."""
+    torch, B, ctx = env
+    for length, new, first, window in ((333, 16, 0, 64), (333, 20, 70, 77), (255, 16, 0, 17), (2000, 16, 5, 910), (2000, 40, 0, 1000), (1100, 16, 0, 600)):
+        cols, total = 16, length + new
+        lowest = total - cols + 1 - window
+        edge = [p for p in range(max(lowest, first), min(lowest + cols - 1, length))]
+
+        def plant(s, k, v):
+            for p in range(max(first, lowest - 70), max(first, min(lowest, length))):  # nobody sees these
+                k[p], v[p] = (0x7F80, 0x7FC0) if p % 2 else (0x7FC0, 0xFF80)
+            for i, p in enumerate(edge):
+                if i % 4 != 1:
+                    v[p, i % 2, i::19] = 0x7F80 if i % 2 else 0xFF80
+                if i % 7 == 5:
+                    v[p, :, 3 * i] = 0x7FC0
+
+        print("case", grp, full, mode, length, new, first, window, flush=True)
+        kv = _cache(torch, B, ctx, 2, [length, 90], mode=mode, plant=lambda s, k, v: plant(s, k, v) if s == 0 else None)
+        q, kn, vn = _inputs(torch, [cols, 1], [new, 1], 2 * grp, 2)
+        out = B.cas_attention_window(ctx, kv, 0, [1, 0], first, window, full, q[::-1], kn[::-1], vn[::-1])[1]
+        kc, vc = B.cas_kv_read(ctx, kv, 0, 0, 0, length, full)
+        k, v = (torch.cat([a.view(torch.bfloat16), b[0]]) for a, b in ((kc, kn), (vc, vn)))
+        bad = ~torch.isfinite(k).all(2).all(1)
+        k = torch.where(bad[:, None, None], 0.0, k)  # in the scores of positions that are masked
+        ref, tol = _reference(torch, k, v, torch.arange(total, device="cuda"), torch.arange(total - cols, total, device="cuda"), q[0], first, window)
+        # infinities and NaN are the largest magnitudes of their vectors, so they are kept, and in a draft too
+        assert bool((~torch.isfinite(ref)).any()) and bool(torch.isfinite(ref).any())
+        _check(torch, out, ref, tol, (grp, length, new, first, window))
+
+
+@pytest.mark.parametrize("n_kv,grp,lens,cols,news,full,keep,t,mode", [
+    (1, 16, [400, 3000], [16, 9], [16, 20], True, 600, 4, 2), (1, 48, [700], [16], [16], True, 700, 3, 2), (2, 17, [1500], [15], [15], True, 600, 6, 2),
+    (1, 20, [900, 64], [13, 16], [13, 64], True, 500, 5, 0)])
+def test_many_rows_exact(env, n_kv, grp, lens, cols, news, full, keep, t, mode):
+    test_outputs_against_64_bits(env, n_kv, grp, lens, cols, news, full, keep, t, mode)
+
+
+@pytest.mark.parametrize("full,mode", [(True, 0), (False, 0), (True, 2), (False, 2)])
 def test_an_infinity_that_every_column_sees_stays_in_its_channel(env, full, mode):
     """(Under a shared exponent the other values of its 32 channels lose their bits; they are what cas_kv_read gives.)"""
     torch, B, ctx = env
