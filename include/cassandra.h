@@ -570,7 +570,8 @@ int cas_kv_evict(cas_ctx* ctx, cas_kv* kv, int layer0, int n_layers, int seq, in
  * w_0 + .. + w_i > u * (sum of w), the last one with w_i > 0 if rounding leaves none.  -infinity and NaN among the logits
  * have probability 0 (so a caller rules tokens out), and of a row that holds +infinity only these count, alike.  A row without any
  * token gives -1.  A drafted token outside the vocabulary is not kept.
- * Probabilities, sums and comparisons are 64-bit; sums are in an order that depends on vocab alone.
+ * Probabilities, sums and comparisons are 64-bit, each exponential within 4e-14 of itself; sums are in an order that depends on vocab
+ * alone.  No output may overlap an input.
  * d_n_accepted: int32 [n_seqs]; d_out: int32 [n_seqs][ld_out], ld_out above every h_k: the kept drafts, the token behind them, -1 up
  * to ld_out.  d_p, d_q: NULL or float [sum of h_k], the probabilities of the drafted tokens.  Pointers need the
  * alignment of their elements only.  h_k = 0 is plain sampling, which is how drafts are drawn in the first place.

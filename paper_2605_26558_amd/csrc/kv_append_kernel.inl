@@ -13,7 +13,7 @@ namespace cas {
 // Equals of the K-th are kept in the order of the columns.  Kept values go to a list in LDS by rank, of which a lane packs
 // 16 into the 16-T half words that their fields fill; the pruned ones to their place in the row.
 // One wave per vector with ballots (kv_append_few_kernel) is bound on a full chip by the scalar unit, which the SIMDs of a CU
-// share (298 scalar instructions per vector): 640 tokens of 8 heads would take 9 us, so 5.9, of which the search is a quarter (some 19 vector instructions
+// share (298 scalar instructions per vector): 512 tokens of 8 heads would take 6.8 us, so 5.6, of which the search is a quarter (some 19 vector instructions
 // a step and four vectors); the rest is launch, memory and packing.
 constexpr int kAppendWaves = 4, kAppendRows = 16;
 constexpr int kKeptPitch = 136;  // values of a list of kept ones: 16-byte steps, and vectors four banks apart
