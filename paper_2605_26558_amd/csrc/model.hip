@@ -305,7 +305,7 @@ static int forward(cas_ctx* ctx, cas_model* m, cas_kv* kv, const ColGroup* grp, 
     if (g.seq < 0 || g.seq >= kv->desc.max_seqs || g.seq >= model_seqs(c) || g.ncols < 1 || g.slot0 < 0)
       return CAS_EINVAL;
     if (g.ncols > seq_cols_max(c)) return CAS_EINVAL;
-    if (kv->h_len[g.seq] + g.slot0 + g.ncols > c.max_pos || g.slot0 + g.ncols > c.max_cols) return CAS_EINVAL;
+    if (g.slot0 > c.max_cols - g.ncols || kv->h_len[g.seq] + g.slot0 + g.ncols > c.max_pos) return CAS_EINVAL;
     for (int j = 0; j < i; ++j)
       if (grp[j].seq == g.seq) return CAS_EINVAL;  // one run per sequence and pass
     ncols += g.ncols;
@@ -718,7 +718,7 @@ int cas_draft_step(cas_ctx* ctx, cas_model* m, cas_kv* kv, int seq, const int32_
 
 int cas_verify_step(cas_ctx* ctx, cas_model* m, cas_kv* kv, int seq, const int32_t* d_tokens, int k,
                     int32_t* d_target, float* d_logits) {
-  if (check_step(ctx, m, kv, seq) != CAS_OK || !d_tokens || k < 0) return CAS_EINVAL;
+  if (check_step(ctx, m, kv, seq) != CAS_OK || !d_tokens || k < 0 || k >= m->cfg.max_cols) return CAS_EINVAL;
   const cas::ColGroup g{seq, k + 1, 0};
   return cas::forward(ctx, m, kv, &g, 1, d_tokens, true, d_target, d_logits);
 }
@@ -741,7 +741,7 @@ static int verify_groups(cas_ctx* ctx, cas_model* m, cas_kv* kv, int n_seqs, con
   cas::ColGroup g[16];
   for (int s = 0, off = 0; s < n_seqs;) {
     int ng = 0, cols = 0;
-    while (s + ng < n_seqs && ng < 16 && cols + h_k[s + ng] + 1 <= m->cfg.max_cols) {
+    while (s + ng < n_seqs && ng < 16 && h_k[s + ng] < m->cfg.max_cols - cols) {
       g[ng] = cas::ColGroup{h_seqs[s + ng], h_k[s + ng] + 1, 0};
       cols += h_k[s + ng] + 1;
       ++ng;
@@ -765,7 +765,7 @@ int cas_verify_step_multi(cas_ctx* ctx, cas_model* m, cas_kv* kv, int n_seqs, co
 }
 
 int cas_commit(cas_ctx* ctx, cas_model* m, cas_kv* kv, int seq, int n_accepted) {
-  if (check_step(ctx, m, kv, seq) != CAS_OK || n_accepted < 0 || n_accepted + 1 > m->cfg.max_cols) return CAS_EINVAL;
+  if (check_step(ctx, m, kv, seq) != CAS_OK || n_accepted < 0 || n_accepted >= m->cfg.max_cols) return CAS_EINVAL;
   const cas_model_cfg& c = m->cfg;
   const int kvd = c.n_kv_heads * c.head_dim, n = n_accepted + 1;
   if ((int64_t)kv->h_len[seq] + n > cas::kv_room(kv)) return CAS_ENOMEM;
@@ -780,7 +780,7 @@ int cas_commit(cas_ctx* ctx, cas_model* m, cas_kv* kv, int seq, int n_accepted) 
 
 int cas_spec_round(cas_ctx* ctx, cas_model* m, cas_kv* kv, int seq, int32_t pending, int k, int32_t* h_out,
                    int32_t* n_accepted) {
-  if (check_step(ctx, m, kv, seq) != CAS_OK || !h_out || !n_accepted || k < 0 || k + 1 > m->cfg.max_cols)
+  if (check_step(ctx, m, kv, seq) != CAS_OK || !h_out || !n_accepted || k < 0 || k >= m->cfg.max_cols)
     return CAS_EINVAL;
   CAS_HIP(ctx, hipMemcpyAsync(m->tok, &pending, sizeof(int32_t), hipMemcpyHostToDevice, ctx->stream));
   for (int i = 0; i < k; ++i) {
@@ -804,8 +804,8 @@ int cas_spec_round_multi(cas_ctx* ctx, cas_model* m, cas_kv* kv, int n_seqs, con
                          const int32_t* h_pending, int k, int32_t* h_out, int32_t* h_n_accepted) {
   if (!ctx || !m || !kv || n_seqs < 1 || n_seqs > 4 || !h_seqs || !h_pending || !h_out || !h_n_accepted || k < 0)
     return CAS_EINVAL;
+  if (k >= m->cfg.max_cols) return CAS_EINVAL;
   const int steps = k + 1, total = steps * n_seqs;
-  if (steps > m->cfg.max_cols) return CAS_EINVAL;
   if (kv->desc.n_layers != m->cfg.n_layers || kv->desc.n_kv_heads != m->cfg.n_kv_heads) return CAS_EINVAL;
   int32_t* step_major = m->tok;                      // [steps][n_seqs]
   int32_t* seq_major = m->tok + 4 * m->cfg.max_cols;   // [n_seqs][steps]
@@ -898,7 +898,7 @@ int cas_dense_decode_step(cas_ctx* ctx, cas_model* m, const cas_dense_layer* h_l
                           int32_t* d_token_out, float* d_logits) {
   if (!ctx || !m || !h_layers || !d_lm_head || !d_kcache || !d_vcache || !d_token_in || len < 0) return CAS_EINVAL;
   const cas_model_cfg& c = m->cfg;
-  if (len + 1 > c.max_pos) return CAS_EINVAL;
+  if (len >= c.max_pos) return CAS_EINVAL;
   const int qd = c.n_q_heads * c.head_dim, kvd = c.n_kv_heads * c.head_dim;
   hipStream_t st = ctx->stream;
   float* logits = d_logits ? d_logits : m->logits;

@@ -80,6 +80,36 @@ def test_lengths_stay_below_32_bits():
     lib.cas_kv_destroy(kv.h)
 
 
+def test_numbers_of_tokens_near_the_end_of_32_bits_are_refused():
+    """A commit of 2^31 - 1 accepted drafts, and passes of as many columns: refused before anything is launched, lengths as they were."""
+    from paper_2605_26558_amd import binding as B
+    lib, kv, data, most = B._lib(), _kv(B, n_kv=1), 4096, 2 ** 31 - 1
+    cfg = B.cas_model_cfg(256, 1, 1, 1, 128, 256, 300, 8, 512, 1e-5, 2)
+    size = C.c_size_t()
+    assert lib.cas_model_act_bytes(C.byref(cfg), C.byref(size)) == B.CAS_OK
+
+    def tensor(rows, cols):
+        t = B.cas_tensor()
+        t.desc.rows, t.desc.cols, t.d_spec, t.d_verif = rows, cols, data, data
+        return t
+    layers = (B.cas_layer_weights * 1)(B.cas_layer_weights(tensor(384, 256), tensor(256, 128), tensor(512, 256), tensor(256, 256), data, data))
+    w, m = B.cas_model_weights(layers, tensor(300, 256), data, data, data), C.c_void_p()
+    assert lib.cas_model_create(C.byref(cfg), C.byref(w), data, size.value, C.byref(m)) == B.CAS_OK
+    ctx, n, one = C.create_string_buffer(4096), C.c_int32(), lambda *v: (C.c_int32 * len(v))(*v)
+    out = one(*[0] * 64)
+    B.cas_kv_set_len(kv, 0, 5)
+    for big in (most, most - 1, 8):
+        assert lib.cas_commit(ctx, m, kv.h, 0, big) == B.CAS_EINVAL
+        assert B.cas_kv_len(kv, 0) == 5
+        assert lib.cas_draft_step(ctx, m, kv.h, 0, data, big, data, None) == B.CAS_EINVAL
+        assert lib.cas_verify_step(ctx, m, kv.h, 0, data, big, data, None) == B.CAS_EINVAL
+        assert lib.cas_verify_step_multi(ctx, m, kv.h, 2, one(0, 1), one(big, 1), data, data) == B.CAS_EINVAL
+        assert lib.cas_spec_round(ctx, m, kv.h, 0, 1, big, out, C.byref(n)) == B.CAS_EINVAL
+        assert lib.cas_spec_round_multi(ctx, m, kv.h, 2, one(0, 1), one(1, 1), big, out, out) == B.CAS_EINVAL
+    lib.cas_model_destroy(m)
+    lib.cas_kv_destroy(kv.h)
+
+
 @pytest.fixture
 def wrappers(monkeypatch):
     """The binding with tensors that say they are on the GPU and a context that is none: a call whose arguments the wrapper takes
