@@ -366,24 +366,27 @@ __global__ __launch_bounds__(64 * kAppendWaves, 6) void rope_append_kernel(RopeA
 
 static int launch_rope_append(cas_ctx* ctx, RopeAppendArgs& a, int n_seqs) {
   const KvGeom& g = a.g;
-  // Up to 24 vectors of K and V per CU (32 over shared exponents) a wave takes each, above sixteen; four of a token's queries are
-  // one of these.  us, one / sixteen a wave, tokens of 8 heads bf16 without queries: 256 5.3 / 6.5, 384 6.5 / 6.5, 512 7.8 / 6.6, 1021
-  // 13.0 / 7.9; fp32 with 32 query heads: 192 6.7 / 6.9, 256 7.6 / 7.2, 512 12.5 / 8.3, 1021 23.4 / 10.8; over shared exponents 384 7.0 /
-  // 8.3, 512 8.3 / 8.3, 640 9.6 / 8.3 and 320 9.2 / 9.0, 384 10.5 / 9.4
-  if ((int64_t)a.n_tok * (g.n_kv_heads * 2 + a.n_q / 4) <= (int64_t)(g.mx ? 32 : 24) * ctx->num_cu) {
-    const dim3 grid((a.n_tok + kAppendWaves - 1) / kAppendWaves, a.n_q + 2 * g.n_kv_heads);
-    hipLaunchKernelGGL(rope_append_few_kernel, grid, dim3(64 * kAppendWaves), 0, ctx->stream, a);
-    CAS_HIP(ctx, hipGetLastError());
-    return CAS_OK;
-  }
   int64_t groups = 0;
   for (int i = 0; i < n_seqs; ++i) {
     a.group0[i] = (int)groups;
     if (a.n[i] > 0) groups += (a.len[i] + a.n[i] - 1) / kAppendRows - a.len[i] / kAppendRows + 1;
   }
   for (int i = n_seqs; i < kRopeAppendSeqs; ++i) a.group0[i] = 0x7FFFFFFF;
+  const int64_t units = groups * g.n_kv_heads * 2, vectors = (int64_t)a.n_tok * (g.n_kv_heads * 2 + a.n_q / 4);
+  // A wave a vector up to 20 vectors of K and V per CU (four of a token's queries count as one) and three more for each wave that the groups of
+  // sixteen rows would make per CU, however few of their rows are new; 26 and 3.5 over shared exponents.  us, one / sixteen a wave: tokens of 8
+  // heads bf16 without queries from a whole group on: 256 5.3 / 6.5, 384 6.5 / 6.5, 512 7.8 / 6.6, 1021 13.0 / 7.9; fp32 with 32 query heads: 192 6.7 / 6.9,
+  // 256 7.6 / 7.2, 512 12.5 / 8.3; over shared exponents 384 7.0 / 8.3, 512 8.3 / 8.3, 640 9.6 / 8.3 and 320 9.2 / 9.0, 384 10.5 / 9.4.  32 sequences, fp32, tokens
+  // each and heads of q, k and v: 12 of 32 + 8 + 8 10.4 / 9.3, 6 of 16 + 16 + 16 8.2 / 10.1, 12 12.5 / 11.1, 4 of 32 + 32 + 32 9.2 / 12.3, 8 16.0 / 13.7, 2 of 64
+  // + 64 + 64 9.2 / 15.8, 4 15.7 / 16.9, 6 22.6 / 19.0; over shared exponents 10.8 / 10.7, 8.6 / 11.9, 13.1 / 12.8, 9.6 / 15.1, 16.7 / 16.2, 9.6 / 20.1, 16.3 /
+  // 21.1, 23.7 / 23.7
+  if (g.mx ? 2 * vectors <= 52 * ctx->num_cu + 7 * units : vectors <= 20 * ctx->num_cu + 3 * units) {
+    const dim3 grid((a.n_tok + kAppendWaves - 1) / kAppendWaves, a.n_q + 2 * g.n_kv_heads);
+    hipLaunchKernelGGL(rope_append_few_kernel, grid, dim3(64 * kAppendWaves), 0, ctx->stream, a);
+    CAS_HIP(ctx, hipGetLastError());
+    return CAS_OK;
+  }
   a.q_blocks = a.n_q > 0 ? std::max(1, std::min((a.n_q + 4 * kAppendWaves - 1) / (4 * kAppendWaves), 1024 / a.n_tok)) : 0;
-  const int64_t units = groups * g.n_kv_heads * 2;
   if (units > 0x7FFFFFFF) return CAS_ENOTSUP;
   a.units = (int)units;
   a.append_blocks = (int)((units + kAppendWaves - 1) / kAppendWaves);

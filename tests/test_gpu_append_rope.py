@@ -140,6 +140,14 @@ def test_words_are_those_of_the_two_calls(env, n_kv, n_q, lens, toks, keep, t, m
         assert torch.equal(three.spec_pool, two.spec_pool) and torch.equal(three.verif_pool, two.verif_pool), what
 
 
+@pytest.mark.parametrize("n_kv,n_q,lens,toks,keep,t,mode,rot,layout,fp32", [  # few tokens each of many sequences, many heads: either side of the limit
+    (64, 4, [7 * i for i in range(32)], [2] * 32, 600, 4, 0, 128, 0, True), (64, 4, [7 * i for i in range(32)], [7] * 32, 600, 4, 0, 128, 0, True),
+    (32, 32, [5 * i for i in range(32)], [4] * 32, 600, 3, 2, 128, 1, False), (32, 32, [5 * i for i in range(32)], [11] * 32, 600, 3, 2, 128, 1, False),
+    (16, 16, [16 * i for i in range(32)], [6] * 32, 500, 2, 0, 96, 0, False), (16, 16, [16 * i + 9 for i in range(32)], [15, 0] * 16, 500, 2, 2, 62, 0, True)])
+def test_words_of_batches_with_many_heads(env, n_kv, n_q, lens, toks, keep, t, mode, rot, layout, fp32):
+    test_words_are_those_of_the_two_calls(env, n_kv, n_q, lens, toks, keep, t, mode, rot, layout, fp32)
+
+
 @pytest.mark.parametrize("mode", [0, 2])
 @pytest.mark.parametrize("fp32", [False, True])
 @pytest.mark.parametrize("rot,layout", [(128, 0), (128, 1), (96, 0), (96, 1), (62, 0), (16, 0), (2, 0)])
